@@ -73,6 +73,8 @@ extern "C" {
 #define LDA_ERR_HIP (-4)         /* the HIP runtime reported an error        */
 #define LDA_ERR_ALIGN (-5)       /* a pointer is not 4-byte aligned          */
 #define LDA_ERR_WORKSPACE (-6)   /* routing workspace too small or mismatched */
+#define LDA_ERR_VALUE (-7)       /* an element type, a probability or a row
+                                    stride out of range                      */
 
 /* Largest number of topics the kernels accept. */
 #define LDA_MAX_K 4096
@@ -458,6 +460,141 @@ int lda_count_topics_indexed(const int64_t *doc_offsets, const int32_t *word_id,
 int lda_draw_routed_scratch(const float *theta, const float *phi, const int32_t *doc_id,
                             const int32_t *word_id, const float *u, int32_t *z, int64_t N,
                             int32_t M, int32_t V, int32_t K, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Operators around the tokens of a language model: the embedding of the words
+ * and its gradient, dropout, the rules on logits, and the draw of the next
+ * token.  They share the word ids, the counter-based generator and the
+ * conventions above (ownership, streams, errors; nothing is allocated, nothing
+ * waits, every call may be captured into a graph).
+ *
+ * Element types of tables, activations and logits.  Arithmetic is fp32 and is
+ * rounded once, to the element type of the output.
+ */
+#define LDA_F32 0
+#define LDA_BF16 1
+#define LDA_F16 2
+
+/*
+ * Rows: a matrix argument is a pointer and the distance between its rows in
+ * elements (ld_*); a row's elements are contiguous.  An input's rows may lie
+ * at any distance of 0 or more (0: one row for all), an output's at its width
+ * or more (LDA_ERR_VALUE otherwise).  Pointers are aligned to their element
+ * (LDA_ERR_ALIGN), no more: rows of odd length and views are taken as they are.
+ *
+ * Dropout: with probability p (0 <= p < 1, else LDA_ERR_VALUE; 0: none) an
+ * element is 0, whatever it was; otherwise it is multiplied by the reciprocal
+ * of the probability of keeping it.  p is rounded to q / 65536, q = round(65536
+ * p) but at most 65535, and the factor belongs to that.  Element (row, col) is
+ * kept if a 16-bit number is at least q: of Philox4x32-10 with key (seed mod
+ * 2^32, seed >> 32) and counter (col / 8, row, step, 1), half col % 2 (low half
+ * first) of output word (col % 8) / 2.  Nothing is stored: the same seed and
+ * step give the same mask in the backward pass.
+ */
+
+/*
+ * The embedding: out[n] = table[word_id[n]] * scale, then dropout (row n).
+ * table [V][D] and out [N][D] are of element type `dtype`; word_id int32 [N].
+ * A word outside [0, V) gives a row of zeros (padding, say).  N = 0 is a no-op;
+ * N above LDA_MAX_N is LDA_ERR_UNSUPPORTED.  table and out may be of any size;
+ * they may not overlap.
+ */
+int lda_embed(const void *table, int64_t ld_table, const int32_t *word_id, void *out,
+              int64_t ld_out, int64_t N, int32_t V, int32_t D, int32_t dtype, double scale,
+              double p, uint64_t seed, uint32_t step, void *stream);
+
+/*
+ * The embedding's gradient: out[v] = scale * (sum over the tokens n with
+ * word_id[n] = v, in order, of what dropout kept of grad[n], times its factor),
+ * for every row of the table: rows without tokens are set to zero.  With
+ * `accumulate` the sums are added to what out holds and rows without tokens
+ * are not touched.  scale, p, seed and step as in lda_embed.  grad [N][D] is of
+ * type grad_dtype; out [V][D] of type out_dtype, the same type or LDA_F32 (else
+ * LDA_ERR_UNSUPPORTED).  Tokens whose word lies outside [0, V) are left out.
+ * The tokens are sorted by word and summed in fp32 in an order that depends on
+ * word_id alone: the same call gives the same bits.  grad may be one row for
+ * all tokens (ld_grad = 0: the gradient of a broadcast).  `workspace`: device
+ * memory, 8-byte aligned, of at least lda_embed_grad_workspace_bytes(N, V, D)
+ * bytes (LDA_ERR_WORKSPACE), free to use again once the call's kernels are
+ * done; not needed if N = 0.  N above LDA_COUNT_MAX_N is LDA_ERR_UNSUPPORTED
+ * (and 0 workspace bytes).
+ */
+size_t lda_embed_grad_workspace_bytes(int64_t N, int32_t V, int32_t D);
+int lda_embed_grad(const void *grad, int64_t ld_grad, const int32_t *word_id, void *out,
+                   int64_t ld_out, int64_t N, int32_t V, int32_t D, int32_t grad_dtype,
+                   int32_t out_dtype, double scale, double p, uint64_t seed, uint32_t step,
+                   int32_t accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Dropout of `rows` rows of `cols` elements, and (being linear) the gradient
+ * of that: given the gradient of the output and the same seed and step it
+ * gives the gradient of the input.  out may be x itself (same ld).  rows up to
+ * LDA_MAX_N, cols up to LDA_DROPOUT_MAX_COLS.
+ */
+#define LDA_DROPOUT_MAX_COLS 17179869184LL
+int lda_dropout(const void *x, int64_t ld_x, void *out, int64_t ld_out, int64_t rows,
+                int64_t cols, int32_t dtype, double p, uint64_t seed, uint32_t step,
+                void *stream);
+
+/*
+ * Rules on the logits of B sequences (a host struct of device pointers; a NULL
+ * pointer is a rule that does not apply).  For token v of row b, in this order
+ * and in fp32:
+ *   x = x > 0 ? x / repetition[b] : x * repetition[b]   if v is in the history
+ *   x = x - frequency[b] * c                            c: uses of v among the
+ *   x = x - presence[b]      if c > 0                      generated tokens
+ *   x = x + bias[b][v]
+ *   x = -inf                 if bit v % 32 of mask[b][v / 32] is 0
+ * history is int32 [B][capacity], row b holding lengths[b] tokens (at most
+ * capacity; a negative length counts as 0), the first prompt[b] of them the
+ * prompt (NULL: 0) and the rest generated; tokens outside [0, V) are ignored.
+ * lengths, prompt int32 [B]; repetition, frequency, presence fp32 [B]; bias
+ * fp32 rows, ld_bias apart; mask 32-bit words, ld_mask apart (0: one row for
+ * all).  The order of the history does not matter.
+ */
+typedef struct lda_logit_rules {
+  const int32_t *history;
+  int64_t ld_history, capacity;
+  const int32_t *lengths, *prompt;
+  const float *repetition, *frequency, *presence;
+  const float *bias;
+  int64_t ld_bias;
+  const int32_t *mask;
+  int64_t ld_mask;
+} lda_logit_rules;
+
+/* The rules applied: out [B][V] of logits [B][V]'s type; out may be logits
+ * itself (same ld).  rules NULL: none.  B up to LDA_LOGITS_MAX_ROWS. */
+#define LDA_LOGITS_MAX_ROWS 2147483647LL
+int lda_penalise_logits(const void *logits, int64_t ld_logits, void *out, int64_t ld_out,
+                        int64_t B, int32_t V, int32_t dtype, const lda_logit_rules *rules,
+                        void *stream);
+
+/*
+ * One token per row, under the rules (the logits are read, not changed):
+ * z[b] (int32) and prob[b] (fp32), the probability with which it was drawn.
+ * With x the row's logits after the rules and max their largest, token v has
+ * the weight exp((x_v - max) / temperature[b]), or 0 where that is below
+ * min_p[b].  temperature fp32 [B] (NULL: 1); where it is not above 0 the row
+ * takes its largest logit, the lowest token among equals, with prob 1.  min_p
+ * fp32 [B] (NULL or not above 0: none; above 1 as 1).  A NaN logit is never
+ * drawn; logits of +inf share the draw.  A row with nothing to draw (all -inf)
+ * gives z = -1 and prob = 0.
+ * The random numbers depend on seed[b] (int64) and position[b] (int32, the
+ * place of the new token, say) only, not on the row's place in the batch:
+ * y(i, d) = the first word of Philox4x32-10 with key (seed mod 2^32, seed >>
+ * 32) and counter (i, position, 0, d), E(i, d) = -log(1 - (y + 1/2) / 2^32).
+ * The row's group of 1024 tokens is the one with the smallest E(group, 2) / (sum
+ * of the group's weights), its token the one of that group with the smallest
+ * E(v, 3) / w_v, the lowest among equals: an exact draw by the weights.
+ * `workspace`: device memory, 8-byte aligned, at least
+ * lda_draw_logits_workspace_bytes(B, V) bytes (LDA_ERR_WORKSPACE).
+ */
+size_t lda_draw_logits_workspace_bytes(int64_t B, int32_t V);
+int lda_draw_logits(const void *logits, int64_t ld_logits, int64_t B, int32_t V, int32_t dtype,
+                    const lda_logit_rules *rules, const float *temperature, const float *min_p,
+                    const int64_t *seed, const int32_t *position, int32_t *z, float *prob,
+                    void *workspace, size_t workspace_bytes, void *stream);
 
 /* The W (butterfly width) the library uses for K, or LDA_ERR_UNSUPPORTED /
  * LDA_ERR_SHAPE for a K it rejects. */

@@ -8,9 +8,10 @@ import subprocess
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-# the draw library: its C ABI with the default build of the kernels, and the
-# build for tables past 4 GiB (lda_draw_wide.hip)
-SRC = [os.path.join(PKG, "csrc", "lda_draw.hip"), os.path.join(PKG, "csrc", "lda_draw_wide.hip")]
+# the draw library: its C ABI with the default build of the kernels, the build
+# for tables past 4 GiB (lda_draw_wide.hip), and the token operators
+SRC = [os.path.join(PKG, "csrc", name)
+       for name in ("lda_draw.hip", "lda_draw_wide.hip", "lda_tokens.hip")]
 LIB = os.path.join(PKG, "liblda_draw.so")
 PROBE_SRC = os.path.join(PKG, "csrc", "probe.hip")
 PROBE_LIB = os.path.join(PKG, "liblda_probe.so")

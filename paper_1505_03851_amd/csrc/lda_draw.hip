@@ -34,6 +34,7 @@
 #include <mutex>
 
 #include "lda_draw.h"
+#include "status.hpp"
 #include "tuning.hpp"
 #include "sources.hpp"
 #include "naive.hpp"
@@ -89,6 +90,12 @@ int finish_launch() {
   }
   return LDA_OK;
 }
+
+}  // namespace
+
+int launch_status() { return finish_launch(); }
+
+namespace {
 
 template <int KMAX>
 void launch_naive(const float *theta, const float *phi, DocSource d, const int32_t *w,
@@ -877,6 +884,8 @@ extern "C" const char *lda_status_string(int status) {
     case LDA_ERR_ALIGN: return "a pointer is not aligned (4 bytes; 8 for offsets and workspaces)";
     case LDA_ERR_WORKSPACE:
       return "routing workspace too small, or the route does not belong to these tokens";
+    case LDA_ERR_VALUE:
+      return "a value out of range (an element type, a probability or a row stride)";
     default: return "unknown status";
   }
 }
@@ -885,4 +894,4 @@ extern "C" const char *lda_last_hip_error(void) {
   return hipGetErrorString(g_last_hip);
 }
 
-extern "C" int lda_version(void) { return 300; }
+extern "C" int lda_version(void) { return 400; }

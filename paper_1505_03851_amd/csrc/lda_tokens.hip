@@ -1,0 +1,388 @@
+// Host side and C ABI of the operators around a language model's tokens
+// (gfx950): argument checks, launch shapes and launches.
+//
+// lda_embed            rows of a table by word, scaled and dropped out.
+// lda_dropout          dropout of any rows, and of their gradient.
+// lda_embed_grad       the table's gradient by sorted tokens.
+// lda_penalise_logits  penalties for repeated tokens, biases, masks.
+// lda_draw_logits      one token per row of logits under those rules.
+//
+// Device code: elements.hpp (element types), keep_bits.hpp (the dropout
+// mask), token_rows.hpp, token_grad.hpp, logits.hpp.
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+#include <stdint.h>
+
+#include "lda_draw.h"
+#include "status.hpp"
+#include "token_rows.hpp"
+#include "token_grad.hpp"
+#include "logits.hpp"
+
+namespace lda {
+namespace {
+
+// A launch holds fewer than 2^32 work-items; kernels stride over the rest.
+constexpr int64_t kMaxBlocks = 1 << 20;
+
+unsigned grid_of(int64_t tiles) {
+  return (unsigned)(tiles < 1 ? 1 : tiles < kMaxBlocks ? tiles : kMaxBlocks);
+}
+
+bool aligned(const void *p, int bytes) {
+  return !(reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1));
+}
+
+int dtype_size(int32_t dtype) {
+  switch (dtype) {
+    case LDA_F32: return 4;
+    case LDA_BF16:
+    case LDA_F16: return 2;
+    default: return 0;
+  }
+}
+
+bool probability(double p) { return p >= 0.0 && p < 1.0; }
+
+// The mask's threshold of 2^16, and the factor of what is kept.
+Dropout make_dropout(double p, uint64_t seed, uint32_t step, double scale, float *factor) {
+  const double q = fmin(65535.0, rint(65536.0 * p));
+  *factor = (float)(scale * (65536.0 / (65536.0 - q)));
+  return Dropout{(uint32_t)q, step, (uint32_t)seed, (uint32_t)(seed >> 32)};
+}
+
+template <typename T, bool GATHER>
+int launch_rows(const void *x, int64_t ldx, const int32_t *word_id, void *out, int64_t ldo,
+                int64_t N, int32_t V, int64_t D, double scale, double p, uint64_t seed,
+                uint32_t step, hipStream_t s) {
+  float factor;
+  const Dropout drop = make_dropout(p, seed, step, scale, &factor);
+  // the lanes of a row: the power of two that covers its 8-column units, up to
+  // the workgroup
+  const int64_t units = (D + 7) / 8;
+  int lanes_log2 = 0;
+  while ((1 << lanes_log2) < kRowThreads && (1 << lanes_log2) < units) ++lanes_log2;
+  const int64_t col_tiles = (units + (1 << lanes_log2) - 1) >> lanes_log2;
+  const int64_t rows = (int64_t)(kRowThreads >> lanes_log2) * kRowsEach;
+  const int64_t tiles = (N + rows - 1) / rows * col_tiles;
+  using S = typename T::store;
+  if (drop.q)
+    rows_kernel<T, GATHER, true><<<grid_of(tiles), kRowThreads, 0, s>>>(
+        (const S *)x, ldx, word_id, (S *)out, ldo, N, V, D, factor, drop, lanes_log2,
+        (uint32_t)col_tiles, tiles);
+  else
+    rows_kernel<T, GATHER, false><<<grid_of(tiles), kRowThreads, 0, s>>>(
+        (const S *)x, ldx, word_id, (S *)out, ldo, N, V, D, factor, drop, lanes_log2,
+        (uint32_t)col_tiles, tiles);
+  return launch_status();
+}
+
+// What lda_embed_grad keeps in the caller's workspace, and how the work is cut.
+struct GradLayout {
+  int passes, bits;        // of the sort
+  int64_t sort_chunks;
+  int width;               // columns of a lane
+  uint32_t col_tiles;      // tiles of 64 width columns
+  uint32_t chunk, chunks;  // sorted positions of a wavefront
+  int64_t ld_part;
+  size_t key[2], index[2], hist, total, crossing, part, bytes;
+};
+
+GradLayout grad_layout(int64_t N, int32_t V, int32_t D) {
+  GradLayout L;
+  int need = 1;  // bits of V, the key of tokens without a word
+  while (need < 31 && V >> need) ++need;
+  L.passes = (need + kSortMaxBits - 1) / kSortMaxBits;
+  L.bits = (need + L.passes - 1) / L.passes;
+  L.sort_chunks = (N + kSortChunk - 1) / kSortChunk;
+  L.width = D > 256 ? 8 : D > 128 ? 4 : D > 64 ? 2 : 1;
+  L.col_tiles = (uint32_t)((D + 64 * L.width - 1) / (64 * L.width));
+  // enough wavefronts to fill the chip, then longer runs
+  L.chunk = 8;
+  while (L.chunk < 128 && (N / L.chunk) * L.col_tiles > 8192) L.chunk *= 2;
+  L.chunks = (uint32_t)((N + L.chunk - 1) / L.chunk);
+  L.ld_part = ((int64_t)D + 7) & ~(int64_t)7;
+  size_t at = 0;
+  auto take = [&](size_t b) {
+    const size_t o = at;
+    at += (b + 255) & ~(size_t)255;
+    return o;
+  };
+  for (int i = 0; i < 2; ++i) {
+    L.key[i] = take(4 * (size_t)N);
+    L.index[i] = take(4 * (size_t)N);
+  }
+  L.hist = take(4 * (size_t)L.sort_chunks << L.bits);
+  L.total = take(4 * (size_t)kSortMaxBins);
+  L.crossing = take(4 * ((size_t)L.chunks + 1));
+  L.part = take(4 * (size_t)(2 * (uint64_t)L.chunks) * (size_t)L.ld_part);
+  L.bytes = at;
+  return L;
+}
+
+template <typename TG, typename TO, int W>
+void launch_reduce(const void *grad, int64_t ldg, void *out, int64_t ldo, int32_t D, float factor,
+                   const Dropout &drop, bool accumulate, const GradLayout &L, const GradPlan &g,
+                   hipStream_t s) {
+  using SG = typename TG::store;
+  using SO = typename TO::store;
+  const unsigned grid = (unsigned)(((uint64_t)L.chunks * L.col_tiles + 3) / 4);
+  if (drop.q)
+    reduce_kernel<TG, TO, W, true><<<grid, 256, 0, s>>>((const SG *)grad, ldg, (SO *)out, ldo, D,
+                                                        factor, drop, accumulate, L.col_tiles, g);
+  else
+    reduce_kernel<TG, TO, W, false><<<grid, 256, 0, s>>>((const SG *)grad, ldg, (SO *)out, ldo, D,
+                                                         factor, drop, accumulate, L.col_tiles, g);
+  if (L.chunks > 1)
+    join_kernel<TO, W><<<1024, 256, 0, s>>>((SO *)out, ldo, D, factor, accumulate, L.col_tiles, g);
+}
+
+template <typename TG, typename TO>
+int launch_grad(const void *grad, int64_t ldg, const int32_t *word_id, void *out, int64_t ldo,
+                int64_t N, int32_t V, int32_t D, double scale, double p, uint64_t seed,
+                uint32_t step, bool accumulate, void *workspace, hipStream_t s) {
+  using SO = typename TO::store;
+  if (!accumulate)
+    clear_rows_kernel<TO><<<grid_of(((int64_t)V * ((D + 7) / 8) + 255) / 256), 256, 0, s>>>(
+        (SO *)out, ldo, V, D);
+  if (N == 0) return launch_status();
+  float factor;
+  const Dropout drop = make_dropout(p, seed, step, scale, &factor);
+  const GradLayout L = grad_layout(N, V, D);
+  char *w = (char *)workspace;
+  uint32_t *hist = (uint32_t *)(w + L.hist), *total = (uint32_t *)(w + L.total);
+  uint32_t *crossing = (uint32_t *)(w + L.crossing);
+  const unsigned chunks = (unsigned)L.sort_chunks;
+  const uint32_t *key = nullptr, *index = nullptr;
+  for (int pass = 0; pass < L.passes; ++pass) {
+    uint32_t *key_out = (uint32_t *)(w + L.key[pass & 1]);
+    uint32_t *index_out = (uint32_t *)(w + L.index[pass & 1]);
+    const int shift = pass * L.bits;
+    sort_hist_kernel<<<chunks, kSortThreads, 0, s>>>(word_id, key, N, V, shift, L.bits, hist,
+                                                     pass == 0 ? crossing : nullptr);
+    const bool scan = chunks > 16;
+    if (scan)
+      sort_scan_kernel<<<((1u << L.bits) + 63) / 64, kSortThreads, 0, s>>>(hist, total, chunks,
+                                                                           1 << L.bits);
+    sort_scatter_kernel<<<chunks, kSortThreads, 0, s>>>(word_id, key, index, N, V, shift, L.bits,
+                                                        hist, scan ? total : nullptr, key_out,
+                                                        index_out);
+    key = key_out;
+    index = index_out;
+  }
+  const GradPlan g{key,     index,    (uint32_t)N, (uint32_t)V, L.chunk, L.chunks,
+                   (float *)(w + L.part), L.ld_part, crossing};
+  switch (L.width) {
+    case 8: launch_reduce<TG, TO, 8>(grad, ldg, out, ldo, D, factor, drop, accumulate, L, g, s); break;
+    case 4: launch_reduce<TG, TO, 4>(grad, ldg, out, ldo, D, factor, drop, accumulate, L, g, s); break;
+    case 2: launch_reduce<TG, TO, 2>(grad, ldg, out, ldo, D, factor, drop, accumulate, L, g, s); break;
+    default: launch_reduce<TG, TO, 1>(grad, ldg, out, ldo, D, factor, drop, accumulate, L, g, s);
+  }
+  return launch_status();
+}
+
+// tokens a workgroup takes of a row: the most groups that still give every
+// compute unit two workgroups
+int slice_of(int64_t B, int64_t V) {
+  int slice = 16 * kGroup;
+  while (slice > kGroup && B * ((V + slice - 1) / slice) < 512) slice /= 2;
+  return slice;
+}
+
+int make_rules(const lda_logit_rules *r, int64_t B, int32_t V, Rules *out) {
+  *out = Rules{};
+  if (!r) return LDA_OK;
+  const void *ptrs[] = {r->history, r->lengths, r->prompt, r->repetition, r->frequency,
+                        r->presence, r->bias, r->mask};
+  for (const void *p : ptrs)
+    if (!aligned(p, 4)) return LDA_ERR_ALIGN;
+  if (r->history) {
+    if (!r->lengths) return LDA_ERR_NULL;
+    if (r->capacity < 0) return LDA_ERR_SHAPE;
+    if (r->ld_history < r->capacity) return LDA_ERR_VALUE;
+  }
+  if (r->bias && r->ld_bias != 0 && r->ld_bias < V) return LDA_ERR_VALUE;
+  if (r->mask && r->ld_mask != 0 && r->ld_mask < ((int64_t)V + 31) / 32) return LDA_ERR_VALUE;
+  *out = Rules{r->history,    r->ld_history, r->lengths, r->prompt,
+               r->repetition, r->frequency,  r->presence, r->bias,
+               r->ld_bias,    (const uint32_t *)r->mask,  r->ld_mask, r->capacity};
+  return LDA_OK;
+}
+
+template <typename T>
+int launch_penalise(const void *logits, int64_t ld, void *out, int64_t ldo, int64_t B, int32_t V,
+                    const Rules &r, hipStream_t s) {
+  using S = typename T::store;
+  const int slice = slice_of(B, V);
+  const int64_t slices = ((int64_t)V + slice - 1) / slice, tiles = B * slices;
+  penalise_kernel<T><<<grid_of(tiles), kLogitThreads, r.history ? 4 * slice : 0, s>>>(
+      (const S *)logits, ld, (S *)out, ldo, V, r, slice, (uint32_t)slices, tiles);
+  return launch_status();
+}
+
+template <typename T>
+int launch_draw(const void *logits, int64_t ld, int64_t B, int32_t V, const Rules &r,
+                const float *temperature, const float *min_p, const int64_t *seed,
+                const int32_t *position, int32_t *z, float *prob, GroupSum *groups,
+                hipStream_t s) {
+  using S = typename T::store;
+  const int slice = slice_of(B, V);
+  const int64_t slices = ((int64_t)V + slice - 1) / slice, tiles = B * slices;
+  const uint32_t per_row = (uint32_t)(((int64_t)V + kGroup - 1) / kGroup);
+  const size_t lds = r.history ? 4 * slice : 0;
+  group_kernel<T, false><<<grid_of(tiles), kLogitThreads, lds, s>>>(
+      (const S *)logits, ld, V, r, temperature, min_p, groups, per_row, slice, (uint32_t)slices,
+      tiles);
+  if (min_p)
+    group_kernel<T, true><<<grid_of(tiles), kLogitThreads, lds, s>>>(
+        (const S *)logits, ld, V, r, temperature, min_p, groups, per_row, slice, (uint32_t)slices,
+        tiles);
+  draw_kernel<T><<<grid_of(B), kLogitThreads, 0, s>>>((const S *)logits, ld, B, V, r, temperature,
+                                                      min_p, seed, position, groups, per_row, z,
+                                                      prob);
+  return launch_status();
+}
+
+}  // namespace
+}  // namespace lda
+
+using namespace lda;
+
+extern "C" int lda_embed(const void *table, int64_t ld_table, const int32_t *word_id, void *out,
+                         int64_t ld_out, int64_t N, int32_t V, int32_t D, int32_t dtype,
+                         double scale, double p, uint64_t seed, uint32_t step, void *stream) {
+  if (N < 0 || V <= 0 || D <= 0) return LDA_ERR_SHAPE;
+  if (N > LDA_MAX_N) return LDA_ERR_UNSUPPORTED;
+  const int size = dtype_size(dtype);
+  if (!size || !probability(p) || ld_table < 0 || ld_out < D) return LDA_ERR_VALUE;
+  if (N == 0) return LDA_OK;
+  if (!table || !word_id || !out) return LDA_ERR_NULL;
+  if (!aligned(table, size) || !aligned(out, size) || !aligned(word_id, 4)) return LDA_ERR_ALIGN;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  switch (dtype) {
+    case LDA_F32:
+      return launch_rows<F32, true>(table, ld_table, word_id, out, ld_out, N, V, D, scale, p, seed,
+                                    step, s);
+    case LDA_BF16:
+      return launch_rows<Bf16, true>(table, ld_table, word_id, out, ld_out, N, V, D, scale, p, seed,
+                                     step, s);
+    default:
+      return launch_rows<F16, true>(table, ld_table, word_id, out, ld_out, N, V, D, scale, p, seed,
+                                    step, s);
+  }
+}
+
+extern "C" int lda_dropout(const void *x, int64_t ld_x, void *out, int64_t ld_out, int64_t rows,
+                           int64_t cols, int32_t dtype, double p, uint64_t seed, uint32_t step,
+                           void *stream) {
+  if (rows < 0 || cols <= 0) return LDA_ERR_SHAPE;
+  if (rows > LDA_MAX_N || cols > LDA_DROPOUT_MAX_COLS) return LDA_ERR_UNSUPPORTED;
+  const int size = dtype_size(dtype);
+  if (!size || !probability(p) || ld_x < 0 || ld_out < cols) return LDA_ERR_VALUE;
+  if (rows == 0) return LDA_OK;
+  if (!x || !out) return LDA_ERR_NULL;
+  if (!aligned(x, size) || !aligned(out, size)) return LDA_ERR_ALIGN;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  switch (dtype) {
+    case LDA_F32:
+      return launch_rows<F32, false>(x, ld_x, nullptr, out, ld_out, rows, 1, cols, 1.0, p, seed,
+                                     step, s);
+    case LDA_BF16:
+      return launch_rows<Bf16, false>(x, ld_x, nullptr, out, ld_out, rows, 1, cols, 1.0, p, seed,
+                                      step, s);
+    default:
+      return launch_rows<F16, false>(x, ld_x, nullptr, out, ld_out, rows, 1, cols, 1.0, p, seed,
+                                     step, s);
+  }
+}
+
+extern "C" size_t lda_embed_grad_workspace_bytes(int64_t N, int32_t V, int32_t D) {
+  if (N <= 0 || V <= 0 || D <= 0 || N > LDA_COUNT_MAX_N) return 0;
+  return grad_layout(N, V, D).bytes;
+}
+
+extern "C" int lda_embed_grad(const void *grad, int64_t ld_grad, const int32_t *word_id, void *out,
+                              int64_t ld_out, int64_t N, int32_t V, int32_t D, int32_t grad_dtype,
+                              int32_t out_dtype, double scale, double p, uint64_t seed,
+                              uint32_t step, int32_t accumulate, void *workspace,
+                              size_t workspace_bytes, void *stream) {
+  if (N < 0 || V <= 0 || D <= 0) return LDA_ERR_SHAPE;
+  if (N > LDA_COUNT_MAX_N) return LDA_ERR_UNSUPPORTED;
+  const int size = dtype_size(grad_dtype), out_size = dtype_size(out_dtype);
+  if (!size || !out_size || !probability(p) || ld_grad < 0 || ld_out < D) return LDA_ERR_VALUE;
+  if (out_dtype != LDA_F32 && out_dtype != grad_dtype) return LDA_ERR_UNSUPPORTED;
+  if (!out) return LDA_ERR_NULL;
+  if (N > 0 && (!grad || !word_id || !workspace)) return LDA_ERR_NULL;
+  if (!aligned(out, out_size) || !aligned(grad, size) || !aligned(word_id, 4) ||
+      !aligned(workspace, 8))
+    return LDA_ERR_ALIGN;
+  if (workspace_bytes < lda_embed_grad_workspace_bytes(N, V, D)) return LDA_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+#define LDA_GRAD(TG, TO)                                                                       \
+  launch_grad<TG, TO>(grad, ld_grad, word_id, out, ld_out, N, V, D, scale, p, seed, step,      \
+                      accumulate != 0, workspace, s)
+  if (grad_dtype == LDA_F32) return LDA_GRAD(F32, F32);
+  if (grad_dtype == LDA_BF16)
+    return out_dtype == LDA_F32 ? LDA_GRAD(Bf16, F32) : LDA_GRAD(Bf16, Bf16);
+  return out_dtype == LDA_F32 ? LDA_GRAD(F16, F32) : LDA_GRAD(F16, F16);
+#undef LDA_GRAD
+}
+
+extern "C" int lda_penalise_logits(const void *logits, int64_t ld_logits, void *out,
+                                   int64_t ld_out, int64_t B, int32_t V, int32_t dtype,
+                                   const lda_logit_rules *rules, void *stream) {
+  if (B < 0 || V <= 0) return LDA_ERR_SHAPE;
+  if (B > LDA_LOGITS_MAX_ROWS) return LDA_ERR_UNSUPPORTED;
+  const int size = dtype_size(dtype);
+  if (!size || ld_logits < 0 || ld_out < V) return LDA_ERR_VALUE;
+  Rules r;
+  if (const int bad = make_rules(rules, B, V, &r)) return bad;
+  if (B == 0) return LDA_OK;
+  if (!logits || !out) return LDA_ERR_NULL;
+  if (!aligned(logits, size) || !aligned(out, size)) return LDA_ERR_ALIGN;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  switch (dtype) {
+    case LDA_F32: return launch_penalise<F32>(logits, ld_logits, out, ld_out, B, V, r, s);
+    case LDA_BF16: return launch_penalise<Bf16>(logits, ld_logits, out, ld_out, B, V, r, s);
+    default: return launch_penalise<F16>(logits, ld_logits, out, ld_out, B, V, r, s);
+  }
+}
+
+extern "C" size_t lda_draw_logits_workspace_bytes(int64_t B, int32_t V) {
+  if (B <= 0 || V <= 0 || B > LDA_LOGITS_MAX_ROWS) return 0;
+  return sizeof(GroupSum) * (size_t)B * (size_t)(((int64_t)V + kGroup - 1) / kGroup);
+}
+
+extern "C" int lda_draw_logits(const void *logits, int64_t ld_logits, int64_t B, int32_t V,
+                               int32_t dtype, const lda_logit_rules *rules,
+                               const float *temperature, const float *min_p, const int64_t *seed,
+                               const int32_t *position, int32_t *z, float *prob, void *workspace,
+                               size_t workspace_bytes, void *stream) {
+  if (B < 0 || V <= 0) return LDA_ERR_SHAPE;
+  if (B > LDA_LOGITS_MAX_ROWS) return LDA_ERR_UNSUPPORTED;
+  const int size = dtype_size(dtype);
+  if (!size || ld_logits < 0) return LDA_ERR_VALUE;
+  Rules r;
+  if (const int bad = make_rules(rules, B, V, &r)) return bad;
+  if (B == 0) return LDA_OK;
+  if (!logits || !seed || !position || !z || !prob || !workspace) return LDA_ERR_NULL;
+  if (!aligned(logits, size) || !aligned(temperature, 4) || !aligned(min_p, 4) ||
+      !aligned(seed, 8) || !aligned(position, 4) || !aligned(z, 4) || !aligned(prob, 4) ||
+      !aligned(workspace, 8))
+    return LDA_ERR_ALIGN;
+  if (workspace_bytes < lda_draw_logits_workspace_bytes(B, V)) return LDA_ERR_WORKSPACE;
+  GroupSum *g = static_cast<GroupSum *>(workspace);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  switch (dtype) {
+    case LDA_F32:
+      return launch_draw<F32>(logits, ld_logits, B, V, r, temperature, min_p, seed, position, z,
+                              prob, g, s);
+    case LDA_BF16:
+      return launch_draw<Bf16>(logits, ld_logits, B, V, r, temperature, min_p, seed, position, z,
+                               prob, g, s);
+    default:
+      return launch_draw<F16>(logits, ld_logits, B, V, r, temperature, min_p, seed, position, z,
+                              prob, g, s);
+  }
+}

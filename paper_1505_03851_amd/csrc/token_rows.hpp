@@ -1,0 +1,62 @@
+// Rows of activations: the embedding lookup (gathered, scaled, dropped out)
+// and the dropout of any rows.
+//
+//   embed    out[n][c] = table[word_id[n]][c] * f * kept(n, c)
+//   dropout  out[n][c] = x[n][c] * f * kept(n, c)
+//
+// with f = scale / P(kept) in float, one rounding to the tensor's type; what is
+// not kept is 0 whatever it was (an infinity or NaN too), and a word outside
+// [0, V) gives a row of zeros.  Both are bound by memory: each lane takes 8
+// columns of kRowsEach rows, all loads before the first store.
+#pragma once
+
+#include "elements.hpp"
+#include "keep_bits.hpp"
+
+namespace lda {
+
+constexpr int kRowThreads = 256;
+constexpr int kRowsEach = 4;  // rows of one lane, loaded together
+
+// A workgroup covers (256 >> lanes_log2) * kRowsEach rows and
+// 8 << lanes_log2 columns; `col_tiles` such tiles cover a row.
+template <typename T, bool GATHER, bool DROP>
+__global__ __launch_bounds__(kRowThreads) void rows_kernel(
+    const typename T::store *__restrict__ x, int64_t ldx, const int32_t *__restrict__ word_id,
+    typename T::store *out, int64_t ldo, int64_t N, int32_t V, int64_t D, float factor,
+    Dropout drop, int lanes_log2, uint32_t col_tiles, int64_t tiles) {
+  const int lane = (int)threadIdx.x & ((1 << lanes_log2) - 1);
+  const int slot = (int)threadIdx.x >> lanes_log2;
+  const int slots = kRowThreads >> lanes_log2;
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int64_t row_tile = tile / col_tiles;
+    const int64_t col = (((tile - row_tile * col_tiles) << lanes_log2) + lane) * 8;
+    if (col >= D) continue;
+    const int n = D - col < 8 ? (int)(D - col) : 8;
+    const int64_t first = row_tile * slots * kRowsEach + slot;
+    float v[kRowsEach][8];
+#pragma unroll
+    for (int r = 0; r < kRowsEach; ++r) {
+      const int64_t row = first + (int64_t)r * slots;
+      int64_t from = row;
+      bool there = row < N;
+      if (GATHER && there) {
+        const int32_t w = word_id[row];
+        there = (uint32_t)w < (uint32_t)V;
+        from = w;
+      }
+      load_elements<T, 8>(x + (there ? from * ldx + col : 0), there ? n : 0, v[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < kRowsEach; ++r) {
+      const int64_t row = first + (int64_t)r * slots;
+      if (row >= N) break;
+      const uint32_t kept = DROP ? keep_bits((uint32_t)(col >> 3), (uint32_t)row, drop) : 0xFFu;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[r][j] = !DROP || (kept >> j & 1) ? v[r][j] * factor : 0.0f;
+      store_elements<T, 8>(out + row * ldo + col, n, v[r]);
+    }
+  }
+}
+
+}  // namespace lda

@@ -1,0 +1,658 @@
+"""The token operators against the oracle in 64 bits.
+
+Tolerances, from the arithmetic (eps = 2^-24, half a unit of float; u the half
+unit of the output's type: 2^-24, 2^-8, 2^-11 relative for float, bfloat16 and
+half, and 2^-25 absolute for half's subnormal numbers):
+  * embed, dropout: the factor and the product are rounded, then the output:
+    |x| (2 eps + u);
+  * embed_grad: a sum of n terms in any order: (n + 2) eps sum |terms|, then the
+    output;
+  * penalise: at most six roundings of numbers up to the largest on the way:
+    6 eps of it, then the output;
+  * draw: a token may differ from the oracle's only where the two best keys are
+    nearer to each other than the roundings of the keys: weights that are off by
+    the logit's error over the temperature, group sums by 40 eps, variates by 8
+    eps.  Its probability is held to the same, twice.
+"""
+import numpy as np
+import pytest
+
+from oracle import tokens as ref
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+UNIT = {"float32": (2.0 ** -24, 0.0), "bfloat16": (2.0 ** -8, 0.0), "float16": (2.0 ** -11, 2.0 ** -25)}
+TYPES = list(UNIT)
+
+
+def _lda():
+    import paper_1505_03851_amd as lda
+    return lda
+
+
+def _torch_type(name):
+    import torch
+    return getattr(torch, name)
+
+
+def _gpu(a, dtype=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(_torch_type(dtype))
+
+
+def _np(t):
+    return t.double().cpu().numpy() if t.is_floating_point() else t.cpu().numpy()
+
+
+def _close(got, want, slack, dtype, what=""):
+    """|got - want| within slack plus the output's half unit, the same
+    infinities and NaN."""
+    unit, least = UNIT[dtype]
+    fine = np.isfinite(want)
+    assert np.array_equal(np.isfinite(got), fine), what
+    assert np.array_equal(got[~fine], want[~fine], equal_nan=True), what
+    bound = slack + (np.abs(want) + slack) * unit + least
+    off = np.abs(got[fine] - want[fine]) - bound[fine]
+    assert off.size == 0 or off.max() <= 0, (what, off.max())
+
+
+def _rounded(a, dtype):
+    """The numbers the GPU is given, in 64 bits."""
+    import torch
+    return torch.from_numpy(a).to(_torch_type(dtype)).double().numpy()
+
+
+def _wide(a, dtype, pad, at):
+    """``a`` as a view into a wider buffer: rows ``pad`` apart and starting at
+    any element."""
+    import torch
+    buf = torch.full((a.shape[0] + 1, a.shape[1] + pad), float("nan"), device="cuda",
+                     dtype=_torch_type(dtype))
+    view = buf[:a.shape[0], at:at + a.shape[1]]
+    view.copy_(torch.from_numpy(a))
+    return view, buf
+
+
+# ---- embed and dropout
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V,D,p", [(1, 1, 1, 0.0), (1, 3, 8, 0.5), (5, 2, 7, 0.1), (33, 70, 64, 0.0),
+                                     (17, 40, 65, 0.3), (130, 1000, 257, 0.1), (64, 33, 1000, 0.0),
+                                     (7, 9, 2049, 0.2), (3, 5, 4096, 0.1), (1000, 100, 100, 0.6),
+                                     (300, 50, 3, 0.4)])
+def test_embed(dtype, N, V, D, p):
+    g = np.random.default_rng(N * 7 + D)
+    table = _rounded(g.normal(0, 0.05, (V, D)), dtype)
+    ids = g.integers(0, V, N).astype(np.int32)
+    ids[::5] = g.choice([-1, V, V + 5, -2 ** 31, 2 ** 31 - 1], len(ids[::5]))
+    seed, step = 0x123456789ABCDEF, 77
+    got = _lda().embed(_gpu(table, dtype), _gpu(ids), scale=3.7, p=p, seed=seed, step=step)
+    want = ref.embed(table, ids, 3.7, p, seed, step)
+    _close(_np(got), want, np.abs(want) * 2 * EPS, dtype, (dtype, N, V, D, p))
+    if p:
+        assert np.array_equal(_np(got) == 0, want == 0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,p", [(1, 1, 0.5), (1, 100_001, 0.1), (300, 1001, 0.2), (2, 8, 0.9),
+                                         (63, 515, 1e-7), (5, 4096, 0.999999), (40_000, 3, 0.25)])
+def test_dropout(dtype, rows, cols, p):
+    g = np.random.default_rng(cols)
+    x = _rounded(g.normal(0, 1, (rows, cols)), dtype)
+    x.flat[::97] = [np.inf, -np.inf, np.nan][rows % 3]
+    seed, step = 2 ** 64 - 3, 2 ** 32 - 1
+    got = _lda().dropout(_gpu(x, dtype), p, seed, step)
+    want = ref.dropout(x, p, seed, step)
+    _close(_np(got), want, np.abs(want) * 2 * EPS, dtype, (dtype, rows, cols, p))
+    # the same mask from any shape with these rows, and in place
+    t = _gpu(x, dtype)
+    assert _lda().dropout(t, p, seed, step, out=t) is t
+    assert np.array_equal(_np(t), _np(got), equal_nan=True)
+
+
+def test_dropout_shapes():
+    import torch
+    lda = _lda()
+    x = torch.randn(6, 5, 77, device="cuda")
+    y = lda.dropout(x, 0.3, 9, 2)
+    assert torch.equal(y.view(30, 77), lda.dropout(x.view(30, 77), 0.3, 9, 2))
+    v = torch.randn(1000, device="cuda")
+    assert torch.equal(lda.dropout(v, 0.3, 9), lda.dropout(v[None], 0.3, 9)[0])
+    assert lda.dropout(torch.empty(0, 5, device="cuda"), 0.3, 9).shape == (0, 5)
+    assert torch.equal(lda.dropout(v, 0.0, 9), v)
+    assert not torch.equal(lda.dropout(v, 0.3, 9, 1), lda.dropout(v, 0.3, 9, 2))
+    assert not torch.equal(lda.dropout(v, 0.3, 9, 1), lda.dropout(v, 0.3, 10, 1))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pad,at", [(1, 1), (5, 3), (8, 0), (16, 8), (64, 7)])
+def test_rows_at_any_distance(dtype, pad, at):
+    import torch
+    lda = _lda()
+    g = np.random.default_rng(pad)
+    N, V, D = 50, 23, 203
+    ids = _gpu(g.integers(0, V, N).astype(np.int32))
+    table = _rounded(g.normal(0, 1, (V, D)), dtype)
+    dense = _gpu(table, dtype)
+    view, _ = _wide(table, dtype, pad, at)
+    out, buf = _wide(np.zeros((N, D)), dtype, pad, at)
+    want = lda.embed(dense, ids, 2.0, 0.2, 5, 6)
+    assert lda.embed(view, ids, 2.0, 0.2, 5, 6, out=out) is out
+    assert torch.equal(out, want)
+    assert int(torch.isfinite(buf).sum()) == N * D  # nothing outside the view
+    rows, buf = _wide(np.zeros((V, D)), dtype, pad, at)
+    assert torch.equal(lda.dropout(view, 0.4, 3, out=rows), lda.dropout(dense, 0.4, 3))
+    assert int(torch.isfinite(buf).sum()) == V * D
+    total, buf = _wide(np.zeros((V, D)), dtype, pad, at)
+    lda.embed_grad(out, ids, V, 2.0, 0.2, 5, 6, out=total)
+    assert torch.equal(total, lda.embed_grad(want, ids, V, 2.0, 0.2, 5, 6))
+    assert int(torch.isfinite(buf).sum()) == V * D
+    # one row for all
+    one = dense[:1].expand(N, D)
+    assert torch.equal(lda.embed_grad(one, ids, V), lda.embed_grad(one.contiguous(), ids, V))
+
+
+# ---- the embedding's gradient
+
+
+def _ids(kind, N, V, g):
+    if kind == "zipf":
+        return np.minimum(g.zipf(1.2, N) - 1, V - 1).astype(np.int32)
+    if kind == "one":
+        return np.full(N, V - 1, dtype=np.int32)
+    if kind == "none":
+        return np.full(N, -1, dtype=np.int32)
+    ids = g.integers(0, V, N).astype(np.int32)
+    if kind == "holes":
+        ids[g.random(N) < 0.5] = V
+        ids[g.random(N) < 0.1] = -7
+    return ids
+
+
+@pytest.mark.parametrize("dtype,out", [("float32", "float32"), ("bfloat16", "bfloat16"),
+                                       ("bfloat16", "float32"), ("float16", "float16"),
+                                       ("float16", "float32")])
+@pytest.mark.parametrize("kind,N,V,D,p", [
+    ("uniform", 1, 1, 1, 0.0), ("uniform", 1, 5, 9, 0.3), ("uniform", 7, 3, 64, 0.0),
+    ("one", 8, 4, 130, 0.1), ("one", 9, 4, 300, 0.0), ("holes", 100, 30, 65, 0.2),
+    ("none", 50, 6, 100, 0.0), ("zipf", 4096, 1000, 100, 0.0), ("zipf", 4097, 1023, 33, 0.1),
+    ("zipf", 5000, 1024, 129, 0.0), ("holes", 9001, 70_000, 20, 0.0), ("one", 20_000, 2, 17, 0.0),
+    ("zipf", 20_000, 50_000, 260, 0.1), ("holes", 70_001, 300, 64, 0.0),
+    ("uniform", 90_000, 2_000_000, 2, 0.0), ("zipf", 3000, 100, 1000, 0.3)])
+def test_embed_grad(dtype, out, kind, N, V, D, p):
+    lda = _lda()
+    g = np.random.default_rng(N + V + D)
+    ids = _ids(kind, N, V, g)
+    grad = _rounded(g.normal(0, 1, (N, D)), dtype)
+    seed, step = 99, 3
+    want, size, tokens = ref.embed_grad(grad, ids, V, 1.7, p, seed, step)
+    slack = (tokens[:, None] + 2) * EPS * size
+    args = (_gpu(grad, dtype), _gpu(ids), V, 1.7, p, seed, step)
+    got = lda.embed_grad(*args, dtype=_torch_type(out))
+    _close(_np(got), want, slack, out, (dtype, out, kind, N, V, D))
+    # the same bits again, whatever the workspace held
+    import torch
+    ws = torch.full((lda.embed_grad_workspace_bytes(N, V, D),), 0xA5, dtype=torch.uint8, device="cuda")
+    again = lda.embed_grad(*args, out=torch.full_like(got, 5.0), workspace=ws)
+    assert torch.equal(again, got)
+    # added to what is there; rows without tokens keep it
+    old = _rounded(g.normal(0, 1, (V, D)), out)
+    both = lda.embed_grad(*args, out=_gpu(old, out), accumulate=True)
+    _close(_np(both), want + old, slack + EPS * np.abs(old) * 2, out, "accumulate")
+    assert np.array_equal(_np(both)[tokens == 0], old[tokens == 0])
+
+
+def test_embed_grad_of_no_tokens():
+    import torch
+    lda = _lda()
+    none = torch.empty(0, 12, device="cuda")
+    ids = torch.empty(0, dtype=torch.int32, device="cuda")
+    out = torch.full((5, 12), 3.0, device="cuda")
+    assert torch.equal(lda.embed_grad(none, ids, 5, out=out, accumulate=True),
+                       torch.full_like(out, 3.0))
+    assert not lda.embed_grad(none, ids, 5, out=out).any()
+    assert lda.embed(out, ids).shape == (0, 12)
+
+
+def test_embed_grad_against_differences():
+    """The derivative of L = sum(C * embed(T)) along a direction, from L in 64
+    bits at T + h R and T - h R: L is linear, so the difference is the derivative
+    up to the roundings of the outputs (at most 2 eps |C| |out| each)."""
+    import torch
+    lda = _lda()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    N, V, D, h = 3000, 700, 96, 0.5
+    T, R = (torch.randn(V, D, device="cuda", generator=g) for _ in range(2))
+    C = torch.randn(N, D, device="cuda", generator=g)
+    ids = torch.randint(-3, V + 3, (N,), device="cuda", generator=g, dtype=torch.int32)
+    args = dict(scale=1.3, p=0.25, seed=8, step=1)
+    up, down = (lda.embed(T + s * R, ids, **args).double() for s in (h, -h))
+    slope = float((C.double() * (up - down)).sum() / (2 * h))
+    G = lda.embed_grad(C, ids, V, **args)
+    mine = float((G.double() * ((T + h * R).double() - (T - h * R).double())).sum() / (2 * h))
+    bound = float((C.double().abs() * (up.abs() + down.abs())).sum()) * 2 * EPS / (2 * h)
+    _, size, tokens = ref.embed_grad(_np(C), _np(ids), V, 1.3, 0.25, 8, 1)
+    bound += float(((tokens[:, None] + 3) * EPS * size * np.abs(_np(R))).sum())
+    assert abs(slope - mine) <= bound, (slope, mine, bound)
+
+
+def test_dropout_gradient_against_differences():
+    """The same for dropout, whose gradient is itself."""
+    import torch
+    lda = _lda()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    x, r, c = (torch.randn(200, 333, device="cuda", generator=g) for _ in range(3))
+    up, down = (lda.dropout(x + s * r, 0.3, 6, 7).double() for s in (0.5, -0.5))
+    slope = float((c.double() * (up - down)).sum())
+    step = (x + 0.5 * r).double() - (x - 0.5 * r).double()
+    mine = float((lda.dropout(c, 0.3, 6, 7).double() * step).sum())
+    bound = float((c.double().abs() * (up.abs() + down.abs() + step.abs() / 0.7)).sum()) * 2 * EPS
+    assert abs(slope - mine) <= bound, (slope, mine, bound)
+
+
+# ---- rules on logits, and the draw
+
+
+def _case(B, V, cap, seed, rules=True, dtype="float32"):
+    g = np.random.default_rng([B, V, cap, seed])
+    x = g.normal(0, 2.5, (B, V))
+    x[np.arange(B)[:, None], g.integers(0, V, (B, min(V, 12)))] += 8
+    case = dict(x=_rounded(x, dtype), rules={}, oracle={})
+    f32 = lambda a: a.astype(np.float32)  # noqa: E731
+    if rules and cap:
+        r = dict(history=g.integers(-2, V + 3, (B, cap)).astype(np.int32),
+                 lengths=g.integers(0, cap + 1, B).astype(np.int32))
+        r["history"][:, ::3] = np.argsort(-x, 1)[:, :1]  # a likely token, often
+        r["lengths"][:1] = cap
+        r["lengths"][B // 2:B // 2 + 1] = cap + 9  # clamped
+        if B > 4:
+            r["lengths"][3], r["lengths"][4] = 0, -5
+        r["prompt"] = (g.random(B) * cap).astype(np.int32)
+        r["repetition"] = f32(g.uniform(0.8, 1.5, B))
+        r["frequency"] = f32(g.uniform(-0.2, 0.5, B))
+        r["presence"] = f32(g.uniform(-0.1, 0.6, B))
+        case["rules"].update(r)
+    if rules:
+        bias = f32(np.where(g.random((B, V)) < 0.05, g.normal(0, 3, (B, V)), 0))
+        bias[g.random((B, V)) < 0.01] = -np.inf
+        case["rules"]["bias"] = bias[0] if seed % 2 else bias
+        ok = g.random((B, V)) < g.random((B, 1))
+        ok[::3] = True
+        if B > 2:
+            ok[2] = False  # nothing is allowed
+        if B > 5:
+            ok[5] = np.arange(V) == V - 1  # the last token alone
+        case["rules"]["mask"] = ok[0] if seed % 3 == 1 else ok
+    case["oracle"] = dict(case["rules"])
+    return case
+
+
+def _gpu_rules(rules):
+    out = {k: _gpu(v) for k, v in rules.items() if k != "mask"}
+    if "mask" in rules:
+        out["mask"] = _gpu(ref.mask_words(rules["mask"]))
+    return out
+
+
+SHAPES = [(1, 1, 0), (1, 7, 3), (3, 31, 1), (7, 300, 40), (6, 1023, 100), (2, 1024, 0), (8, 1025, 17),
+          (5, 2500, 700), (9, 8193, 300), (300, 1500, 20), (4, 33_001, 5000), (7, 50_000, 64)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,V,cap", SHAPES)
+def test_penalise(dtype, B, V, cap):
+    import torch
+    lda = _lda()
+    for seed in (0, 1):
+        c = _case(B, V, cap, seed, dtype=dtype)
+        want, size = ref.penalise(c["x"], **c["oracle"])
+        x = _gpu(c["x"], dtype)
+        got = lda.penalise_logits(x, **_gpu_rules(c["rules"]))
+        _close(_np(got), want, 6 * EPS * size, dtype, (dtype, B, V, cap, seed))
+        assert lda.penalise_logits(x, **_gpu_rules(c["rules"]), out=x) is x  # in place
+        assert torch.equal(x, got)
+
+
+def test_penalise_subsets_and_special_values():
+    """Each rule alone; NaN, infinities and the type's lowest value; a masked
+    place is -inf whatever it held."""
+    lda = _lda()
+    c = _case(6, 700, 50, 2)
+    x = c["x"]
+    x[:, 5], x[:, 6], x[:, 7], x[:, 8] = np.nan, np.inf, -np.inf, np.finfo(np.float32).min
+    base = {k: c["rules"][k] for k in ("history", "lengths")}
+    for extra in ((), ("prompt",), ("repetition",), ("frequency",), ("presence",),
+                  ("prompt", "presence"), ("repetition", "frequency", "presence")):
+        r = dict(base, **{k: c["rules"][k] for k in extra})
+        want, size = ref.penalise(x, **r)
+        _close(_np(lda.penalise_logits(_gpu(x, "float32"), **_gpu_rules(r))), want, 6 * EPS * size,
+               "float32", extra)
+    for k in ("bias", "mask"):
+        r = {k: c["rules"][k]}
+        want, size = ref.penalise(x, **r)
+        _close(_np(lda.penalise_logits(_gpu(x, "float32"), **_gpu_rules(r))), want, 6 * EPS * size,
+               "float32", k)
+    assert np.array_equal(_np(lda.penalise_logits(_gpu(x, "float32"))), x, equal_nan=True)
+
+
+def _check_draw(c, dtype, temperature, min_p, seed, position, what):
+    """(z, prob) of the GPU against the oracle's rows; the rows that hang on
+    rounding may differ, and there are few."""
+    lda = _lda()
+    B, V = c["x"].shape
+    f32 = lambda a: None if a is None else _gpu(np.asarray(a, dtype=np.float32))  # noqa: E731
+    z, prob = lda.draw_logits(_gpu(c["x"], dtype), _gpu(np.asarray(seed, dtype=np.int64)),
+                              _gpu(np.asarray(position, dtype=np.int32)), f32(temperature),
+                              f32(min_p), **_gpu_rules(c["rules"]))
+    z, prob = _np(z), _np(prob)
+    x, size = ref.penalise(c["x"], **c["oracle"])
+    near = 0
+    for b in range(B):
+        t = 1.0 if temperature is None else float(np.float32(temperature[b]))
+        m = 0.0 if min_p is None else float(np.float32(min_p[b]))
+        want, wp, margin = ref.draw(x[b], t, m, int(seed[b]), int(position[b]))
+        fine = np.isfinite(x[b])
+        err = 48 * EPS
+        if t > 0 and fine.any():
+            err += 2 * (6 + 2) * EPS * size[b][fine].max() / t
+        if margin <= err:
+            near += 1
+            continue
+        assert z[b] == want, (what, b, z[b], want, margin)
+        assert abs(prob[b] - wp) <= 2 * err * wp, (what, b, prob[b], wp)
+    assert near <= 0.02 * B + 1, (what, near)
+    return z, prob
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,V,cap", SHAPES)
+def test_draw(dtype, B, V, cap):
+    g = np.random.default_rng(B + V)
+    seed = g.integers(-2 ** 63, 2 ** 63, B)
+    position = g.integers(-2 ** 31, 2 ** 31, B)
+    t = g.uniform(0.2, 2.0, B)
+    t[g.random(B) < 0.2] = 0.0
+    m = np.where(g.random(B) < 0.4, 0.0, g.uniform(0.001, 0.5, B))
+    plain = _case(B, V, cap, 0, rules=False, dtype=dtype)
+    _check_draw(plain, dtype, None, None, seed, position, "plain")
+    _check_draw(plain, dtype, t, None, seed, position, "temperature")
+    for s in (0, 1):
+        _check_draw(_case(B, V, cap, s, dtype=dtype), dtype, t, m, seed, position, "rules")
+
+
+def test_draw_special_rows():
+    """Greedy ties take the lowest token; NaN is never drawn; +inf shares the
+    draw; nothing to draw gives -1; extreme temperatures and floors."""
+    V = 2500
+    rows, temps, floors = [], [], []
+
+    def row(values, t=1.0, m=0.0, fill=-np.inf):
+        x = np.full(V, fill)
+        for i, v in values.items():
+            x[i] = v
+        rows.append(x)
+        temps.append(t)
+        floors.append(m)
+
+    row({1500: 3.0, 1501: 3.0, 2400: 3.0}, t=0.0)          # greedy tie
+    row({7: 1.0}, t=0.0, fill=0.0)
+    row({}, t=1.0)                                          # nothing
+    row({}, t=0.0)
+    row({100: np.nan})                                      # nothing but NaN
+    row({100: np.nan, 2000: -5.0})
+    row({3: np.inf, 1200: np.inf, 9: 50.0})                 # two of +inf
+    row({3: np.inf, 1200: np.inf}, t=0.0)
+    row({5: np.finfo(np.float32).min})                      # the lowest value alone
+    row({5: np.finfo(np.float32).min, 6: 0.0}, t=1e-30)
+    row({2: 1.0, 3: 1.5}, t=1e-38, fill=0.0)
+    row({2: 1.0, 3: 1.5}, t=np.inf)                         # even odds
+    row({2: 1.0, 3: 1.5}, t=-1.0, fill=0.0)                 # as 0
+    row({2: 1.0, 3: 1.5}, t=np.nan, fill=0.0)
+    row({2: 1.0, 3: 1.0, 4: 0.9}, m=1.0, fill=0.0)          # only the likeliest
+    row({2: 1.0, 3: 1.0, 4: 0.9}, m=7.0, fill=0.0)
+    row({2: 60.0}, m=1e-30, fill=0.0)
+    n = 40
+    x = np.repeat(np.array(rows), n, 0)
+    t, m = np.repeat(temps, n), np.repeat(floors, n)
+    g = np.random.default_rng(0)
+    c = dict(x=x, rules={}, oracle={})
+    t_ref = np.where(np.isnan(t), 0.0, t)
+    z, prob = _check_draw(c, "float32", t_ref, m, g.integers(0, 2 ** 63, len(x)), np.arange(len(x)), "")
+    z, prob = z.reshape(-1, n), prob.reshape(-1, n)
+    assert (z[0] == 1500).all() and (prob[0] == 1).all() and (z[1] == 7).all()
+    for r in (2, 3, 4):
+        assert (z[r] == -1).all() and (prob[r] == 0).all()
+    assert (z[5] == 2000).all() and set(z[6]) == {3, 1200} and (prob[6] == 0.5).all()
+    assert (z[7] == 3).all() and (z[8] == 5).all() and (z[9] == 6).all() and (z[10] == 3).all()
+    assert set(z[11]) == {2, 3} and (prob[11] == 0.5).all() and (z[12] == 3).all()
+    for r in (14, 15):
+        assert set(z[r]) == {2, 3} and (prob[r] == 0.5).all()
+    lda = _lda()
+    one = np.zeros(len(x), dtype=np.int64)
+    nan = lda.draw_logits(_gpu(x, "float32"), _gpu(one), _gpu(one.astype(np.int32)),
+                          _gpu(t.astype(np.float32)))[0].cpu().numpy().reshape(-1, n)
+    assert (nan[13] == 3).all()
+
+
+def test_draw_does_not_depend_on_the_batch():
+    """A row's token hangs on its logits, seed and position: alone, in a batch,
+    or at another place in it."""
+    import torch
+    lda = _lda()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    B, V = 200, 5000
+    x = torch.randn(B, V, device="cuda", generator=g) * 3
+    seed = torch.randint(0, 2 ** 62, (B,), device="cuda", generator=g)
+    pos = torch.arange(B, device="cuda", dtype=torch.int32)
+    z, p = lda.draw_logits(x, seed, pos)
+    order = torch.randperm(B, device="cuda", generator=g)
+    z2, p2 = lda.draw_logits(x[order], seed[order], pos[order])
+    assert torch.equal(z2, z[order]) and torch.equal(p2, p[order])
+    for b in (0, 99, 199):
+        z1, p1 = lda.draw_logits(x[b:b + 1], seed[b:b + 1], pos[b:b + 1])
+        assert torch.equal(z1, z[b:b + 1]) and torch.equal(p1, p[b:b + 1])
+
+
+def test_draw_follows_the_weights():
+    """200,000 draws from one row of 3,000 tokens: chi-square over the tokens
+    expected 50 times and more, the rest as one."""
+    import torch
+    lda = _lda()
+    g = np.random.default_rng(3)
+    x = (g.normal(0, 2.0, 3000)).astype(np.float32)
+    n = 200_000
+    rows = _gpu(x)[None].expand(n, 3000)
+    z, _ = lda.draw_logits(rows, torch.full((n,), 17, device="cuda"),
+                           torch.arange(n, dtype=torch.int32, device="cuda"))
+    w = np.exp(x.astype(np.float64))
+    want = n * w / w.sum()
+    got = np.bincount(_np(z), minlength=3000).astype(np.float64)
+    big = want >= 50
+    want = np.append(want[big], want[~big].sum())
+    got = np.append(got[big], got[~big].sum())
+    chi, cells = ((got - want) ** 2 / want).sum(), len(want) - 1
+    assert abs(chi - cells) < 6 * np.sqrt(2 * cells), (chi, cells)
+
+
+@pytest.mark.parametrize("pad,at", [(1, 1), (8, 0), (24, 5)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_logits_rows_at_any_distance(dtype, pad, at):
+    """A slice of a padded vocabulary; history, bias and mask rows apart too."""
+    import torch
+    lda = _lda()
+    c = _case(9, 2051, 33, 0, dtype=dtype)
+    r = _gpu_rules(c["rules"])
+    dense = _gpu(c["x"], dtype)
+    view, _ = _wide(c["x"], dtype, pad, at)
+    wide = dict(r)
+    for k in ("history", "bias", "mask"):
+        buf = torch.full((r[k].shape[0], r[k].shape[1] + pad), 77, device="cuda", dtype=r[k].dtype)
+        buf[:, at:at + r[k].shape[1]] = r[k]
+        wide[k] = buf[:, at:at + r[k].shape[1]]
+    out, buf = _wide(np.zeros(c["x"].shape), dtype, pad, at)
+    want = lda.penalise_logits(dense, **r)
+    lda.penalise_logits(view, **wide, out=out)
+    assert torch.equal(out, want)
+    assert int((~torch.isnan(buf)).sum()) == out.numel()
+    seed, pos = torch.arange(9, device="cuda"), torch.arange(9, dtype=torch.int32, device="cuda")
+    for a, b in zip(lda.draw_logits(view, seed, pos, **wide), lda.draw_logits(dense, seed, pos, **r)):
+        assert torch.equal(a, b)
+
+
+# ---- streams, graphs, refusals, sizes
+
+
+def _calls():
+    """(name, inputs that change from replay to replay, the call) of every
+    operator at a size with several workgroups."""
+    import torch
+    lda = _lda()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+
+    def ints(hi, *shape):
+        return torch.randint(0, hi, shape, device="cuda", generator=g, dtype=torch.int32)
+
+    N, V, D, B, W = 20_000, 3000, 200, 16, 20_000
+    ids, rows = ints(V, N), torch.randn(N, D, device="cuda", generator=g)
+    table = torch.randn(V, D, device="cuda", generator=g)
+    x = torch.randn(B, W, device="cuda", generator=g) * 3
+    history, lengths = ints(W, B, 300), ints(300, B)
+    freq, floor = torch.rand(B, device="cuda", generator=g), torch.full((B,), 0.01, device="cuda")
+    seed, pos = ints(1 << 30, B).long(), ints(1 << 30, B)
+    rules = dict(history=history, lengths=lengths, frequency=freq)
+    return {
+        "embed": ([ids, table], lambda s=None: [lda.embed(table, ids, 2.0, 0.1, 3, stream=s)]),
+        "embed_grad": ([ids, rows], lambda s=None: [lda.embed_grad(rows, ids, V, 2.0, 0.1, 3, stream=s)]),
+        "dropout": ([rows], lambda s=None: [lda.dropout(rows, 0.1, 3, stream=s)]),
+        "penalise": ([x, history], lambda s=None: [lda.penalise_logits(x, **rules, stream=s)]),
+        "draw": ([x, history, pos], lambda s=None: list(
+            lda.draw_logits(x, seed, pos, min_p=floor, **rules, stream=s))),
+    }
+
+
+@pytest.mark.parametrize("name", ["embed", "embed_grad", "dropout", "penalise", "draw"])
+def test_side_stream(name):
+    import torch
+    _, call = _calls()[name]
+    want = call()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = call(side)
+    with torch.cuda.stream(side):
+        inside = call()
+    side.synchronize()
+    for a, b, c in zip(want, got, inside):
+        assert torch.equal(a, b) and torch.equal(a, c)
+
+
+@pytest.mark.parametrize("name", ["embed", "embed_grad", "dropout", "penalise", "draw"])
+def test_graph(name):
+    """Captured once and replayed on new inputs, eager work in between."""
+    import torch
+    inputs, call = _calls()[name]
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = call()
+    for k in range(4):
+        for t in inputs:
+            t.copy_(t.flip(0) if k % 2 else t.roll(1 + k, 0))
+        want = call()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, outs):
+            assert torch.equal(a, b), (name, k)
+
+
+def test_refusals_on_the_gpu():
+    import torch
+    lda = _lda()
+    x = torch.zeros(4, 40, device="cuda")
+    i = torch.zeros(4, dtype=torch.int32, device="cuda")
+    h = torch.zeros(4, 6, dtype=torch.int32, device="cuda")
+    f = torch.zeros(4, device="cuda")
+    s = torch.zeros(4, dtype=torch.int64, device="cuda")
+    bad = [
+        lambda: lda.embed(x, i.long()), lambda: lda.embed(x.double(), i), lambda: lda.embed(x[0], i),
+        lambda: lda.embed(x.t(), i), lambda: lda.embed(x, i.cpu()), lambda: lda.embed(x, i, p=1.0),
+        lambda: lda.embed(x, i, out=x[:3]), lambda: lda.embed(x, i, out=x.half()),
+        lambda: lda.embed(x, i, out=x[:1].expand(4, 40)), lambda: lda.embed(x, i[::2]),
+        lambda: lda.embed_grad(x, i[:3], 9), lambda: lda.embed_grad(x, i, 9, accumulate=True),
+        lambda: lda.embed_grad(x, i, 9, dtype=torch.float16),
+        lambda: lda.embed_grad(x.half(), i, 9, dtype=torch.bfloat16),
+        lambda: lda.embed_grad(x, i, 9, out=torch.zeros(9, 41, device="cuda")),
+        lambda: lda.embed_grad(x, i, 9, out=torch.zeros(9, 40, device="cuda"), dtype=torch.float16),
+        lambda: lda.embed_grad(x, i, 9, workspace=f), lambda: lda.embed_grad(x.t(), i, 9),
+        lambda: lda.dropout(x, 1.0, 1), lambda: lda.dropout(x, -0.5, 1),
+        lambda: lda.dropout(x.long(), 0.5, 1), lambda: lda.dropout(x.t(), 0.5, 1),
+        lambda: lda.dropout(x, 0.5, 1, out=x[:2]), lambda: lda.dropout(x, 0.5, 1, out=x.half()),
+        lambda: lda.dropout(x.view(2, 2, 40).transpose(0, 1), 0.5, 1),
+        lambda: lda.penalise_logits(x, history=h), lambda: lda.penalise_logits(x, lengths=i),
+        lambda: lda.penalise_logits(x, repetition=f), lambda: lda.penalise_logits(x, h[:3], i),
+        lambda: lda.penalise_logits(x, h.long(), i), lambda: lda.penalise_logits(x, h, i[:2]),
+        lambda: lda.penalise_logits(x, h, i, repetition=f.double()),
+        lambda: lda.penalise_logits(x, bias=f), lambda: lda.penalise_logits(x, bias=x.half()),
+        lambda: lda.penalise_logits(x, mask=i), lambda: lda.penalise_logits(x, mask=x),
+        lambda: lda.penalise_logits(x, mask=h), lambda: lda.penalise_logits(x, out=x[:2]),
+        lambda: lda.draw_logits(x, i, i), lambda: lda.draw_logits(x, s, s),
+        lambda: lda.draw_logits(x, s[:2], i), lambda: lda.draw_logits(x, s, i, f[:3]),
+        lambda: lda.draw_logits(x, s, i, min_p=f.half()), lambda: lda.draw_logits(x, s, i, out=(s, f)),
+        lambda: lda.draw_logits(x, s, i, workspace=f),
+    ]
+    for k, call in enumerate(bad):
+        with pytest.raises((TypeError, ValueError)):
+            call()
+            print("not refused:", k)
+    small = torch.empty(8, dtype=torch.uint8, device="cuda")
+    for call in (lambda: lda.embed_grad(x, i, 9, workspace=small),
+                 lambda: lda.draw_logits(x, s, i, workspace=small)):
+        with pytest.raises(lda.LdaError) as e:
+            call()
+        assert e.value.status == lda.STATUS["LDA_ERR_WORKSPACE"]
+    torch.cuda.synchronize()
+
+
+def test_past_32_bits():
+    """Tables, gradients and logits of more than 2^32 elements: the last rows."""
+    import torch
+    lda = _lda()
+    V, D = 540_000, 8192
+    table = torch.zeros(V, D, dtype=torch.bfloat16, device="cuda")
+    table[-1] = torch.arange(D, device="cuda") % 128
+    ids = torch.tensor([V - 1, 0, V - 1], dtype=torch.int32, device="cuda")
+    got = lda.embed(table, ids, 0.5)
+    assert torch.equal(got[0].float(), (torch.arange(D, device="cuda") % 128) * 0.5)
+    assert torch.equal(got[0], got[2]) and not got[1].any()
+    out = lda.embed_grad(got, ids, V, out=table)  # overwrites the table
+    assert torch.equal(out[-1].float(), (torch.arange(D, device="cuda") % 128).float())
+    assert not out[1:-1].any() and not out[0].any()
+    del table, out
+    torch.cuda.empty_cache()
+    y = torch.ones(V, D, dtype=torch.float16, device="cuda")
+    lda.dropout(y, 0.5, 1, out=y)
+    last = ref.dropout(np.ones((1, D)), 0.5, 1, 0)
+    f = ref.keep_factor(1, D, 0.5, 1, 0)
+    assert np.array_equal(_np(y[:1]), last) and f.max() == 2.0
+    assert 0.45 < float((y[-1] != 0).float().mean()) < 0.55
+    del y
+    torch.cuda.empty_cache()
+    B, W = 35_000, 131_072
+    x = torch.zeros(B, W, dtype=torch.bfloat16, device="cuda")
+    x[-1, -3] = 40.0
+    seed = torch.zeros(B, dtype=torch.int64, device="cuda")
+    z, p = lda.draw_logits(x, seed, torch.arange(B, dtype=torch.int32, device="cuda"))
+    assert int(z[-1]) == W - 3 and float(p[-1]) > 0.999
+    assert abs(float(p[0]) * W - 1) < 1e-4 and len(torch.unique(z)) > 25_000
+    bias = torch.zeros(W, device="cuda")
+    bias[-3] = 2.0
+    lda.penalise_logits(x, bias=bias, out=x)
+    assert float(x[-1, -3]) == 42.0 and float(x[0, -3]) == 2.0 and not x[:, -2:].any()
