@@ -124,61 +124,86 @@ GradLayout grad_layout(int64_t N, int32_t V, int32_t D) {
 template <typename TG, typename TO, int W>
 void launch_reduce(const void *grad, int64_t ldg, void *out, int64_t ldo, int32_t D, float factor,
                    const Dropout &drop, bool accumulate, const GradLayout &L, const GradPlan &g,
-                   hipStream_t s) {
+                   const uint32_t *key, const uint32_t *index, char *w, hipStream_t s) {
   using SG = typename TG::store;
   using SO = typename TO::store;
+  float *part = (float *)(w + L.part);
+  uint32_t *crossing = (uint32_t *)(w + L.crossing);
   const unsigned grid = (unsigned)(((uint64_t)L.chunks * L.col_tiles + 3) / 4);
   if (drop.q)
     reduce_kernel<TG, TO, W, true><<<grid, 256, 0, s>>>((const SG *)grad, ldg, (SO *)out, ldo, D,
-                                                        factor, drop, accumulate, L.col_tiles, g);
+                                                        factor, drop, accumulate, L.col_tiles, g,
+                                                        key, index, part, crossing);
   else
     reduce_kernel<TG, TO, W, false><<<grid, 256, 0, s>>>((const SG *)grad, ldg, (SO *)out, ldo, D,
-                                                         factor, drop, accumulate, L.col_tiles, g);
+                                                         factor, drop, accumulate, L.col_tiles, g,
+                                                         key, index, part, crossing);
   if (L.chunks > 1)
-    join_kernel<TO, W><<<1024, 256, 0, s>>>((SO *)out, ldo, D, factor, accumulate, L.col_tiles, g);
+    join_kernel<TO, W><<<512, kJoinWaves * 64, 0, s>>>((SO *)out, ldo, D, factor, accumulate,
+                                                       L.col_tiles, g, key, part, crossing);
 }
 
 template <typename TG, typename TO>
 int launch_grad(const void *grad, int64_t ldg, const int32_t *word_id, void *out, int64_t ldo,
                 int64_t N, int32_t V, int32_t D, double scale, double p, uint64_t seed,
                 uint32_t step, bool accumulate, void *workspace, hipStream_t s) {
-  using SO = typename TO::store;
-  if (!accumulate)
-    clear_rows_kernel<TO><<<grid_of(((int64_t)V * ((D + 7) / 8) + 255) / 256), 256, 0, s>>>(
-        (SO *)out, ldo, V, D);
-  if (N == 0) return launch_status();
+  const int64_t size = (int64_t)sizeof(typename TO::store);
+  const GradLayout L = grad_layout(N, V, D);
+  const unsigned chunks = (unsigned)L.sort_chunks;
+  // each launch of the sort sets its share of the rows to zero
+  const bool dense = ldo == D;
+  ClearShare clear{(char *)out, size * ldo, size * D * (dense ? (int64_t)V : 1),
+                   dense ? 1 : (int64_t)V, 0, N == 0 || chunks == 1 ? 1u : 2u * L.passes, chunks};
+  const int64_t units = (clear.width + 15) / 16 * clear.rows / clear.parts;
+  const int64_t clear_blocks = accumulate ? 0 : (units + kSortThreads - 1) / kSortThreads;
+  const unsigned extra = (unsigned)(clear_blocks < 1024 ? clear_blocks : 1024);
+  if (N == 0) {
+    if (extra) clear_kernel<<<extra, kSortThreads, 0, s>>>(clear);
+    return launch_status();
+  }
   float factor;
   const Dropout drop = make_dropout(p, seed, step, scale, &factor);
-  const GradLayout L = grad_layout(N, V, D);
   char *w = (char *)workspace;
   uint32_t *hist = (uint32_t *)(w + L.hist), *total = (uint32_t *)(w + L.total);
   uint32_t *crossing = (uint32_t *)(w + L.crossing);
-  const unsigned chunks = (unsigned)L.sort_chunks;
   const uint32_t *key = nullptr, *index = nullptr;
-  for (int pass = 0; pass < L.passes; ++pass) {
+  if (chunks == 1) {
+    uint32_t *key_out = (uint32_t *)(w + L.key[0]), *index_out = (uint32_t *)(w + L.index[0]);
+    sort_chunk_kernel<<<1 + extra, kSortThreads, 0, s>>>(word_id, (int32_t)N, V, L.passes, L.bits,
+                                                         key_out, index_out, crossing, clear);
+    key = key_out;
+    index = index_out;
+  }
+  for (int pass = 0; chunks > 1 && pass < L.passes; ++pass) {
     uint32_t *key_out = (uint32_t *)(w + L.key[pass & 1]);
     uint32_t *index_out = (uint32_t *)(w + L.index[pass & 1]);
     const int shift = pass * L.bits;
-    sort_hist_kernel<<<chunks, kSortThreads, 0, s>>>(word_id, key, N, V, shift, L.bits, hist,
-                                                     pass == 0 ? crossing : nullptr);
+    clear.part = 2 * pass;
+    sort_hist_kernel<<<chunks + extra, kSortThreads, 0, s>>>(
+        word_id, key, N, V, shift, L.bits, hist, pass == 0 ? crossing : nullptr, clear);
+    // from 17 chunks on a launch of its own sums the chunks before each
     const bool scan = chunks > 16;
     if (scan)
       sort_scan_kernel<<<((1u << L.bits) + 63) / 64, kSortThreads, 0, s>>>(hist, total, chunks,
                                                                            1 << L.bits);
-    sort_scatter_kernel<<<chunks, kSortThreads, 0, s>>>(word_id, key, index, N, V, shift, L.bits,
-                                                        hist, scan ? total : nullptr, key_out,
-                                                        index_out);
+    clear.part = 2 * pass + 1;
+    sort_scatter_kernel<<<chunks + extra, kSortThreads, 0, s>>>(
+        word_id, key, index, N, V, shift, L.bits, hist, scan ? total : nullptr, key_out, index_out,
+        clear);
     key = key_out;
     index = index_out;
   }
-  const GradPlan g{key,     index,    (uint32_t)N, (uint32_t)V, L.chunk, L.chunks,
-                   (float *)(w + L.part), L.ld_part, crossing};
+  const GradPlan g{(uint32_t)N, (uint32_t)V, L.chunk, L.chunks, L.ld_part};
+#define LDA_REDUCE(W)                                                                           \
+  launch_reduce<TG, TO, W>(grad, ldg, out, ldo, D, factor, drop, accumulate, L, g, key, index,  \
+                           w, s)
   switch (L.width) {
-    case 8: launch_reduce<TG, TO, 8>(grad, ldg, out, ldo, D, factor, drop, accumulate, L, g, s); break;
-    case 4: launch_reduce<TG, TO, 4>(grad, ldg, out, ldo, D, factor, drop, accumulate, L, g, s); break;
-    case 2: launch_reduce<TG, TO, 2>(grad, ldg, out, ldo, D, factor, drop, accumulate, L, g, s); break;
-    default: launch_reduce<TG, TO, 1>(grad, ldg, out, ldo, D, factor, drop, accumulate, L, g, s);
+    case 8: LDA_REDUCE(8); break;
+    case 4: LDA_REDUCE(4); break;
+    case 2: LDA_REDUCE(2); break;
+    default: LDA_REDUCE(1);
   }
+#undef LDA_REDUCE
   return launch_status();
 }
 

@@ -26,6 +26,35 @@ constexpr int kSortChunk = kSortThreads * kSortEach;  // tokens of one workgroup
 constexpr int kSortMaxBits = 10;                      // bits of a digit
 constexpr int kSortMaxBins = 1 << kSortMaxBits;
 
+// The share of the gradient's rows that a sorting launch sets to zero, in its
+// workgroups past those that sort: the sort is a chain of short launches bound
+// by latency, the clearing one long store, and the two do not touch the same
+// memory, so each launch of the chain carries a part of it.
+struct ClearShare {
+  char *out;
+  int64_t ld, width, rows;  // in bytes; dense rows are given as one
+  uint32_t part, parts;
+  uint32_t blocks;  // workgroups that sort
+};
+
+__device__ __forceinline__ void clear_share(const ClearShare &c) {
+  const int64_t units = (c.width + 15) >> 4, all = units * c.rows;
+  const int64_t end = all * (c.part + 1) / c.parts;
+  const words4 zero = {};
+  for (int64_t i = all * c.part / c.parts + (int64_t)(blockIdx.x - c.blocks) * kSortThreads +
+                   threadIdx.x;
+       i < end; i += (int64_t)(gridDim.x - c.blocks) * kSortThreads) {
+    const int64_t row = c.rows == 1 ? 0 : i / units;
+    const int64_t at = (i - row * units) << 4;
+    char *p = c.out + row * c.ld + at;
+    if (c.width - at >= 16) {
+      *reinterpret_cast<words4_any *>(p) = zero;
+    } else {
+      for (int64_t j = 0; j < c.width - at; j += 2) *reinterpret_cast<half_any *>(p + j) = 0;
+    }
+  }
+}
+
 // a token's key: its word, or V (sorted last, given no gradient) outside [0, V)
 __device__ __forceinline__ uint32_t sort_key(const int32_t *word_id, const uint32_t *key,
                                              int64_t i, int32_t V) {
@@ -37,38 +66,29 @@ __device__ __forceinline__ uint32_t sort_key(const int32_t *word_id, const uint3
 // hist[chunk][digit]: the tokens of each chunk with each digit
 __global__ __launch_bounds__(kSortThreads) void sort_hist_kernel(
     const int32_t *__restrict__ word_id, const uint32_t *__restrict__ key, int64_t N, int32_t V,
-    int shift, int bits, uint32_t *__restrict__ hist, uint32_t *crossing) {
+    int shift, int bits, uint32_t *__restrict__ hist, uint32_t *crossing, ClearShare clear) {
   __shared__ uint32_t count[kSortMaxBins];
+  if (blockIdx.x >= clear.blocks) {
+    clear_share(clear);
+    return;
+  }
   const int bins = 1 << bits;
   if (crossing && blockIdx.x == 0 && threadIdx.x == 0) *crossing = 0;
-  for (int b = threadIdx.x; b < bins; b += kSortThreads) count[b] = 0;
-  __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * kSortChunk;
+  uint32_t k[kSortEach];
 #pragma unroll
   for (int r = 0; r < kSortEach; ++r) {
     const int64_t i = first + r * kSortThreads + threadIdx.x;
-    if (i < N) atomicAdd(&count[sort_key(word_id, key, i, V) >> shift & (bins - 1)], 1u);
+    k[r] = i < N ? sort_key(word_id, key, i, V) : 0;
   }
+  for (int b = threadIdx.x; b < bins; b += kSortThreads) count[b] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < kSortEach; ++r)
+    if (first + r * kSortThreads + threadIdx.x < N) atomicAdd(&count[k[r] >> shift & (bins - 1)], 1u);
   __syncthreads();
   for (int b = threadIdx.x; b < bins; b += kSortThreads)
     hist[(int64_t)blockIdx.x * bins + b] = count[b];
-}
-
-// Exclusive sum of one value per thread over the workgroup, by thread index.
-__device__ __forceinline__ uint32_t block_exclusive_sum(uint32_t v, uint32_t *wave_sums) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t s = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t o = __shfl_up(s, d);
-    if (lane >= d) s += o;
-  }
-  if (lane == 63) wave_sums[wave] = s;
-  __syncthreads();
-  uint32_t before = 0;
-  for (int w = 0; w < wave; ++w) before += wave_sums[w];
-  __syncthreads();
-  return before + s - v;
 }
 
 // Many chunks: hist[c][b] becomes the tokens of digit b in the chunks before c,
@@ -83,8 +103,10 @@ __global__ __launch_bounds__(kSortThreads) void sort_scan_kernel(uint32_t *hist,
   const uint32_t from = wave * each < chunks ? wave * each : chunks;
   const uint32_t to = from + each < chunks ? from + each : chunks;
   uint32_t s = 0;
-  if (b < bins)
+  if (b < bins) {
+#pragma unroll 8
     for (uint32_t c = from; c < to; ++c) s += hist[(int64_t)c * bins + b];
+  }
   sums[wave][lane] = s;
   __syncthreads();
   uint32_t before = 0, all = 0;
@@ -94,28 +116,111 @@ __global__ __launch_bounds__(kSortThreads) void sort_scan_kernel(uint32_t *hist,
   }
   if (b >= bins) return;
   if (wave == 0) total[b] = all;
-  for (uint32_t c = from; c < to; ++c) {
-    const uint32_t h = hist[(int64_t)c * bins + b];
-    hist[(int64_t)c * bins + b] = before;
-    before += h;
+  constexpr int U = 8;
+  for (uint32_t c = from; c < to; c += U) {
+    uint32_t h[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) h[u] = c + u < to ? hist[(int64_t)(c + u) * bins + b] : 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (c + u < to) hist[(int64_t)(c + u) * bins + b] = before;
+      before += h[u];
+    }
   }
 }
 
+// Exclusive sum of one value per thread over the workgroup, by thread index.
+__device__ __forceinline__ uint32_t block_exclusive_sum(uint32_t v, uint32_t *wave_sums) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t s = v;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = __shfl_up(s, d);
+    if (lane >= d) s += o;
+  }
+  if (lane == 63) wave_sums[wave] = s;
+  __syncthreads();
+  uint32_t before = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) before += w < wave ? wave_sums[w] : 0;
+  __syncthreads();
+  return before + s - v;
+}
+
+struct SortLds {
+  uint32_t base[kSortMaxBins];
+  uint16_t count[kSortWaves][kSortMaxBins];
+  uint32_t wave_sums[kSortWaves];
+};
+
+// Ranks by one digit of a chunk's tokens, of which a wavefront holds 64
+// kSortEach neighbours, 64 to a round (token `first + 64 r` of the `n` in the
+// chunk): rank[r] is the number of tokens of the same digit before the token in
+// its wavefront, and count[wave][digit] becomes the number in the wavefronts
+// before it.  Returns thread b's tokens of digit b in the whole chunk.
+__device__ __forceinline__ uint32_t rank_chunk(SortLds &s, const uint32_t (&k)[kSortEach], int n,
+                                               int first, int shift, int bits,
+                                               uint32_t (&rank)[kSortEach]) {
+  const int bins = 1 << bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int b = lane; b < bins; b += 64) s.count[wave][b] = 0;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int r = 0; r < kSortEach; ++r) {
+    const bool there = first + 64 * r < n;
+    const uint32_t digit = k[r] >> shift & (bins - 1);
+    uint64_t same = __ballot(there);
+    for (int b = 0; b < bits; ++b) {
+      const uint64_t set = __ballot(digit >> b & 1);
+      same &= digit >> b & 1 ? set : ~set;
+    }
+    const uint64_t below = same & ((1ull << lane) - 1);
+    const uint32_t prior = s.count[wave][digit];
+    rank[r] = prior + __popcll(below);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (there && below == 0) s.count[wave][digit] = (uint16_t)(prior + __popcll(same));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+  uint32_t all = 0;
+  if ((int)threadIdx.x < bins) {
+    uint32_t c[kSortWaves];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) c[w] = s.count[w][threadIdx.x];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      s.count[w][threadIdx.x] = (uint16_t)all;
+      all += c[w];
+    }
+  }
+  return all;
+}
+
 // The tokens of one chunk to their places by one digit: the chunk's base for
-// the digit, and the token's rank among the chunk's tokens of that digit, by
-// wavefront (a wavefront holds 64 kSortEach neighbours), round and lane.
+// the digit, the wavefront's and the token's rank in it.
 __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(
     const int32_t *__restrict__ word_id, const uint32_t *__restrict__ key,
     const uint32_t *__restrict__ index, int64_t N, int32_t V, int shift, int bits,
     const uint32_t *__restrict__ hist, const uint32_t *__restrict__ total,
-    uint32_t *__restrict__ key_out,
-    uint32_t *__restrict__ index_out) {
-  __shared__ uint32_t base[kSortMaxBins];
-  __shared__ uint16_t count[kSortWaves][kSortMaxBins];
-  __shared__ uint32_t wave_sums[kSortWaves];
-  const int bins = 1 << bits;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int b = lane; b < bins; b += 64) count[wave][b] = 0;
+    uint32_t *__restrict__ key_out, uint32_t *__restrict__ index_out, ClearShare clear) {
+  __shared__ SortLds s;
+  if (blockIdx.x >= clear.blocks) {
+    clear_share(clear);
+    return;
+  }
+  const int bins = 1 << bits, wave = threadIdx.x >> 6;
+  const int64_t start = (int64_t)blockIdx.x * kSortChunk;
+  const int n = N - start < kSortChunk ? (int)(N - start) : kSortChunk;
+  const int first = wave * 64 * kSortEach + (threadIdx.x & 63);
+  uint32_t k[kSortEach], from[kSortEach], rank[kSortEach];
+#pragma unroll
+  for (int r = 0; r < kSortEach; ++r) {
+    const int i = first + 64 * r;
+    k[r] = i < n ? sort_key(word_id, key, start + i, V) : 0;
+    from[r] = i < n && index ? index[start + i] : (uint32_t)(start + i);
+  }
   // this digit's tokens of all chunks (to place the digit) and of earlier
   // chunks: from sort_scan_kernel, or (few chunks) summed here
   uint32_t all = 0, before = 0;
@@ -123,80 +228,92 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(
     all = total[threadIdx.x];
     before = hist[(int64_t)blockIdx.x * bins + threadIdx.x];
   } else if ((int)threadIdx.x < bins) {
-    for (uint32_t c = 0; c < gridDim.x; ++c) {
+#pragma unroll 8
+    for (uint32_t c = 0; c < clear.blocks; ++c) {
       const uint32_t h = hist[(int64_t)c * bins + threadIdx.x];
       all += h;
       before += c < blockIdx.x ? h : 0;
     }
   }
-  const uint32_t place = block_exclusive_sum(all, wave_sums);
-  if ((int)threadIdx.x < bins) base[threadIdx.x] = place + before;
-  const int64_t first = (int64_t)blockIdx.x * kSortChunk + wave * 64 * kSortEach + lane;
-  uint32_t k[kSortEach], rank[kSortEach];
-#pragma unroll
-  for (int r = 0; r < kSortEach; ++r) {
-    const int64_t i = first + 64 * r;
-    k[r] = i < N ? sort_key(word_id, key, i, V) : 0;
-    const uint32_t digit = k[r] >> shift & (bins - 1);
-    uint64_t same = __ballot(i < N);
-    for (int b = 0; b < bits; ++b) {
-      const uint64_t set = __ballot(digit >> b & 1);
-      same &= digit >> b & 1 ? set : ~set;
-    }
-    const uint64_t below = same & ((1ull << lane) - 1);
-    const uint32_t prior = count[wave][digit];
-    rank[r] = prior + __popcll(below);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    if (i < N && below == 0) count[wave][digit] = (uint16_t)(prior + __popcll(same));
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
-  __syncthreads();
-  for (int b = threadIdx.x; b < bins; b += kSortThreads) {
-    uint32_t s = 0;
-    for (int w = 0; w < kSortWaves; ++w) {
-      const uint32_t c = count[w][b];
-      count[w][b] = (uint16_t)s;
-      s += c;
-    }
-  }
+  rank_chunk(s, k, n, first, shift, bits, rank);
+  const uint32_t place = block_exclusive_sum(all, s.wave_sums);
+  if ((int)threadIdx.x < bins) s.base[threadIdx.x] = place + before;
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < kSortEach; ++r) {
-    const int64_t i = first + 64 * r;
-    if (i >= N) break;
+    if (first + 64 * r >= n) break;
     const uint32_t digit = k[r] >> shift & (bins - 1);
-    const uint32_t at = base[digit] + count[wave][digit] + rank[r];
+    const uint32_t at = s.base[digit] + s.count[wave][digit] + rank[r];
     key_out[at] = k[r];
-    index_out[at] = index ? index[i] : (uint32_t)i;
+    index_out[at] = from[r];
   }
 }
 
-// rows [0, V) of `out` to zero, D elements each
-template <typename T>
-__global__ __launch_bounds__(256) void clear_rows_kernel(typename T::store *out, int64_t ldo,
-                                                         int32_t V, int32_t D) {
-  const int64_t cols = (D + 7) / 8, units = cols * V;
-  const float zero[8] = {};
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < units;
-       i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / cols;
-    const int32_t col = (int32_t)(i - row * cols) * 8;
-    store_elements<T, 8>(out + row * ldo + col, D - col, zero);
+// One chunk: every pass in one workgroup, through LDS.
+__global__ __launch_bounds__(kSortThreads) void sort_chunk_kernel(
+    const int32_t *__restrict__ word_id, int32_t N, int32_t V, int passes, int bits,
+    uint32_t *__restrict__ key_out, uint32_t *__restrict__ index_out, uint32_t *crossing,
+    ClearShare clear) {
+  __shared__ SortLds s;
+  __shared__ uint32_t keys[kSortChunk];
+  __shared__ uint16_t indices[kSortChunk];
+  if (blockIdx.x >= clear.blocks) {
+    clear_share(clear);
+    return;
+  }
+  if (threadIdx.x == 0) *crossing = 0;
+  const int wave = threadIdx.x >> 6;
+  const int first = wave * 64 * kSortEach + (threadIdx.x & 63);
+  uint32_t k[kSortEach], from[kSortEach], rank[kSortEach];
+#pragma unroll
+  for (int r = 0; r < kSortEach; ++r) {
+    const int i = first + 64 * r;
+    k[r] = i < N ? sort_key(word_id, nullptr, i, V) : 0;
+    from[r] = (uint32_t)i;
+  }
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * bits;
+    const uint32_t all = rank_chunk(s, k, N, first, shift, bits, rank);
+    const uint32_t place = block_exclusive_sum(all, s.wave_sums);
+    if ((int)threadIdx.x < 1 << bits) s.base[threadIdx.x] = place;
+    __syncthreads();
+    const bool last = pass + 1 == passes;
+#pragma unroll
+    for (int r = 0; r < kSortEach; ++r) {
+      if (first + 64 * r >= N) break;
+      const uint32_t digit = k[r] >> shift & ((1 << bits) - 1);
+      const uint32_t at = s.base[digit] + s.count[wave][digit] + rank[r];
+      if (last) {
+        key_out[at] = k[r];
+        index_out[at] = from[r];
+      } else {
+        keys[at] = k[r];
+        indices[at] = (uint16_t)from[r];
+      }
+    }
+    __syncthreads();
+    if (last) break;
+#pragma unroll
+    for (int r = 0; r < kSortEach; ++r) {
+      const int i = first + 64 * r;
+      k[r] = i < N ? keys[i] : 0;
+      from[r] = i < N ? indices[i] : 0;
+    }
+    __syncthreads();
   }
 }
 
-// The sorted tokens and what is left of them.
+// Nothing to sort: clearing alone.
+__global__ __launch_bounds__(kSortThreads) void clear_kernel(ClearShare clear) {
+  clear_share(clear);
+}
+
+// How the sorted positions are cut, and where the words that cross a cut are
+// kept.
 struct GradPlan {
-  const uint32_t *key, *index;  // [N], by word and then by token
-  uint32_t N;
-  uint32_t V;
+  uint32_t N, V;
   uint32_t chunk, chunks;  // sorted positions of a wavefront, and how many
-  float *part;             // [2 chunks][ld_part]
   int64_t ld_part;
-  uint32_t *crossing;  // [0]: how many, then the chunks in which a word that
-                       // goes past the chunk's end begins
 };
 
 template <typename TO, int W>
@@ -211,13 +328,17 @@ __device__ __forceinline__ void write_row(typename TO::store *out, int64_t ldo, 
   store_elements<TO, W>(p, n, sum);
 }
 
-// One wavefront: `chunk` sorted positions, 64 W columns.
+// One wavefront: `chunk` sorted positions (a multiple of U), 64 W columns.  The
+// words, rows and ends of runs are the same for all lanes, so they are read and
+// compared in scalar registers; a lane's work is W conversions and additions a
+// row, and U rows are in flight together.  crossing[0] counts the chunks in
+// which a word that goes past the chunk's end begins, listed after it.
 template <typename TG, typename TO, int W, bool DROP>
-__global__ __launch_bounds__(256) void reduce_kernel(const typename TG::store *__restrict__ grad,
-                                                     int64_t ldg, typename TO::store *out,
-                                                     int64_t ldo, int32_t D, float factor,
-                                                     Dropout drop, bool accumulate,
-                                                     uint32_t col_tiles, GradPlan g) {
+__global__ __launch_bounds__(256) void reduce_kernel(
+    const typename TG::store *__restrict__ grad, int64_t ldg, typename TO::store *__restrict__ out,
+    int64_t ldo, int32_t D, float factor, Dropout drop, bool accumulate, uint32_t col_tiles,
+    GradPlan g, const uint32_t *__restrict__ key, const uint32_t *__restrict__ index,
+    float *__restrict__ part, uint32_t *__restrict__ crossing) {
   constexpr int U = 8;  // rows loaded together
   const int lane = threadIdx.x & 63;
   const uint32_t item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
@@ -226,89 +347,103 @@ __global__ __launch_bounds__(256) void reduce_kernel(const typename TG::store *_
   const uint32_t tile = item - c * col_tiles;
   const int32_t col = (int32_t)(tile * 64 + lane) * W;
   const int n = D - col < W ? (D - col > 0 ? D - col : 0) : W;
+  const typename TG::store *mine = grad + (n ? col : 0);
   const uint32_t begin = c * g.chunk;
   const uint32_t end = g.N - begin < g.chunk ? g.N : begin + g.chunk;
-  bool began_here = begin == 0 || g.key[begin - 1] != g.key[begin];
+  uint32_t word = key[begin];
+  bool began_here = begin == 0 || key[begin - 1] != word;
   float sum[W] = {};
   for (uint32_t p = begin; p < end; p += U) {
     float v[U][W];
-    uint32_t row[U];
+    uint32_t row[U], next[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint32_t at = p + u < end ? p + u : end - 1;
-      row[u] = g.index[at];
-      load_elements<TG, W>(grad + (int64_t)row[u] * ldg + (n ? col : 0), n, v[u]);
+      row[u] = index[p + u < end ? p + u : end - 1];
+      next[u] = p + u + 1 < g.N ? key[p + u + 1] : g.V;  // the word after
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_elements<TG, W>(mine + (int64_t)row[u] * ldg, n, v[u]);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (p + u >= end) break;
-      const uint32_t word = g.key[p + u];
       if (word >= g.V) return;  // from here on only tokens without a word
       uint32_t kept = 0;
       if (DROP) kept = keep_bits((uint32_t)col >> 3, row[u], drop) >> (col & 7);
 #pragma unroll
       for (int j = 0; j < W; ++j) sum[j] += !DROP || (kept >> j & 1) ? v[u][j] : 0.0f;
-      const bool goes_on = p + u + 1 < g.N && g.key[p + u + 1] == word;
+      const bool goes_on = next[u] == word;
       if (goes_on && p + u + 1 < end) continue;
       if (began_here && !goes_on) {
         if (n) write_row<TO, W>(out, ldo, word, col, n, factor, accumulate, sum);
       } else {
-        float *slot = g.part + (int64_t)(2 * c + (began_here ? 1 : 0)) * g.ld_part + col;
+        float *slot = part + (int64_t)(2 * c + (began_here ? 1 : 0)) * g.ld_part + col;
         if (n) store_elements<F32, W>(slot, W, sum);
-        if (began_here && tile == 0 && lane == 0)
-          g.crossing[1 + atomicAdd(g.crossing, 1u)] = c;
+        if (began_here && tile == 0 && lane == 0) crossing[1 + atomicAdd(crossing, 1u)] = c;
       }
       began_here = true;
+      word = next[u];
 #pragma unroll
       for (int j = 0; j < W; ++j) sum[j] = 0.0f;
     }
   }
 }
 
-// The words that cross chunks: each one's parts added in order.  The four
-// wavefronts of a workgroup take a quarter of the parts each.
+constexpr int kJoinWaves = 8;
+
+// The words that cross chunks: each one's parts added in order, a run of them
+// by each wavefront of the workgroup.
 template <typename TO, int W>
-__global__ __launch_bounds__(256) void join_kernel(typename TO::store *out, int64_t ldo, int32_t D,
-                                                   float factor, bool accumulate,
-                                                   uint32_t col_tiles, GradPlan g) {
-  __shared__ float quarter[3][64 * W];
+__global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(
+    typename TO::store *__restrict__ out, int64_t ldo, int32_t D, float factor, bool accumulate,
+    uint32_t col_tiles, GradPlan g, const uint32_t *__restrict__ key,
+    const float *__restrict__ part, const uint32_t *__restrict__ crossing) {
+  constexpr int U = 8;
+  __shared__ float sums[kJoinWaves - 1][64 * W];
   const int lane = threadIdx.x & 63;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t items = g.crossing[0] * col_tiles;
+  const uint32_t items = crossing[0] * col_tiles;
   for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
     const uint32_t i = item / col_tiles;
     const int32_t col = (int32_t)((item - i * col_tiles) * 64 + lane) * W;
     const int n = D - col < W ? (D - col > 0 ? D - col : 0) : W;
-    const uint32_t c0 = g.crossing[1 + i];
-    const uint32_t word = g.key[(c0 + 1) * g.chunk - 1];
-    uint32_t lo = (c0 + 1) * g.chunk, hi = g.N;  // the first position past the word
-    while (lo < hi) {
+    const uint32_t c0 = crossing[1 + i];
+    const uint32_t word = key[(c0 + 1) * g.chunk - 1];
+    // the chunk in which the word ends: the last whose first key is the word
+    uint32_t lo = c0 + 1, hi = g.chunks;
+    while (hi - lo > 1) {
       const uint32_t mid = lo + (hi - lo) / 2;
-      if (g.key[mid] == word)
-        lo = mid + 1;
+      if (key[mid * g.chunk] == word)
+        lo = mid;
       else
         hi = mid;
     }
-    const uint32_t parts = (lo - 1) / g.chunk - c0 + 1;
-    const uint32_t each = (parts + 3) / 4;
-    const uint32_t from = wave * each, to = from + each < parts ? from + each : parts;
+    const uint32_t parts = lo - c0 + 1;
+    const uint32_t each = (parts + kJoinWaves - 1) / kJoinWaves;
+    const uint32_t from = wave * each < parts ? wave * each : parts;
+    const uint32_t to = from + each < parts ? from + each : parts;
     float sum[W] = {};
-    for (uint32_t k = from; k < to; ++k) {
-      float v[W];
-      const uint32_t slot = 2 * (c0 + k) + (k == 0 ? 1 : 0);
-      load_elements<F32, W>(g.part + (int64_t)slot * g.ld_part + (n ? col : 0), n ? W : 0, v);
+    for (uint32_t k = from; k < to; k += U) {
+      float v[U][W];
 #pragma unroll
-      for (int j = 0; j < W; ++j) sum[j] += v[j];
+      for (int u = 0; u < U; ++u) {
+        const uint32_t slot = 2 * (c0 + k + u) + (k + u == 0 ? 1 : 0);
+        load_elements<F32, W>(part + (int64_t)slot * g.ld_part + (n ? col : 0),
+                              n && k + u < to ? W : 0, v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < W; ++j) sum[j] += v[u][j];
     }
     if (wave > 0) {
 #pragma unroll
-      for (int j = 0; j < W; ++j) quarter[wave - 1][j * 64 + lane] = sum[j];
+      for (int j = 0; j < W; ++j) sums[wave - 1][j * 64 + lane] = sum[j];
     }
     __syncthreads();
     if (wave == 0 && n) {
 #pragma unroll
       for (int j = 0; j < W; ++j)
-        for (int q = 0; q < 3; ++q) sum[j] += quarter[q][j * 64 + lane];
+        for (int q = 0; q < kJoinWaves - 1; ++q) sum[j] += sums[q][j * 64 + lane];
       write_row<TO, W>(out, ldo, word, col, n, factor, accumulate, sum);
     }
     __syncthreads();
