@@ -83,19 +83,28 @@ struct Packed {
   typename T::store v[W];
 };
 
-// p[0 .. W) -> x; only the first `n` are read (the rest: 0) where n < W
+// p[0 .. W) as it is in memory; only the first `n` are read (the rest: 0)
+// where n < W
 template <typename T, int W>
-__device__ __forceinline__ void load_elements(const typename T::store *p, int n, float (&x)[W]) {
+__device__ __forceinline__ Packed<T, W> load_packed(const typename T::store *p, int n) {
   using R = Raw<W * (int)sizeof(typename T::store)>;
+  Packed<T, W> a;
   if (n >= W) {
     const typename R::type raw = *reinterpret_cast<const typename R::memory *>(p);
-    const auto a = __builtin_bit_cast(Packed<T, W>, raw);
-#pragma unroll
-    for (int j = 0; j < W; ++j) x[j] = T::up(a.v[j]);
+    a = __builtin_bit_cast(Packed<T, W>, raw);
   } else {
 #pragma unroll
-    for (int j = 0; j < W; ++j) x[j] = j < n ? T::up(p[j]) : 0.0f;
+    for (int j = 0; j < W; ++j) a.v[j] = j < n ? p[j] : typename T::store(0);
   }
+  return a;
+}
+
+// p[0 .. W) -> x in float
+template <typename T, int W>
+__device__ __forceinline__ void load_elements(const typename T::store *p, int n, float (&x)[W]) {
+  const Packed<T, W> a = load_packed<T, W>(p, n);
+#pragma unroll
+  for (int j = 0; j < W; ++j) x[j] = T::up(a.v[j]);
 }
 
 template <typename T, int W>

@@ -316,74 +316,106 @@ struct GradPlan {
   int64_t ld_part;
 };
 
+// The last n of a lane's W sums to its n columns of the word's row, which
+// begin at `own`.
 template <typename TO, int W>
 __device__ __forceinline__ void write_row(typename TO::store *out, int64_t ldo, uint32_t word,
-                                          int32_t col, int n, float factor, bool accumulate,
+                                          int32_t own, int n, float factor, bool accumulate,
                                           float (&sum)[W]) {
-  typename TO::store *p = out + (int64_t)word * ldo + col;
-  float old[W] = {};
-  if (accumulate) load_elements<TO, W>(p, n, old);
+  typename TO::store *p = out + (int64_t)word * ldo + own;
+  if (n == W) {
+    float old[W] = {};
+    if (accumulate) load_elements<TO, W>(p, W, old);
 #pragma unroll
-  for (int j = 0; j < W; ++j) sum[j] = accumulate ? fmaf(sum[j], factor, old[j]) : sum[j] * factor;
-  store_elements<TO, W>(p, n, sum);
+    for (int j = 0; j < W; ++j) sum[j] = accumulate ? fmaf(sum[j], factor, old[j]) : sum[j] * factor;
+    store_elements<TO, W>(p, W, sum);
+  } else {
+    p -= W - n;
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (j >= W - n)
+        p[j] = TO::down(accumulate ? fmaf(sum[j], factor, TO::up(p[j])) : sum[j] * factor);
+  }
 }
 
-// One wavefront: `chunk` sorted positions (a multiple of U), 64 W columns.  The
-// words, rows and ends of runs are the same for all lanes, so they are read and
-// compared in scalar registers; a lane's work is W conversions and additions a
-// row, and U rows are in flight together.  crossing[0] counts the chunks in
-// which a word that goes past the chunk's end begins, listed after it.
+// One wavefront: `chunk` sorted positions, 64 W columns.  It reads the words and
+// row numbers of 64 positions at a time, one to a lane; the ends of the words'
+// runs are then a mask in scalar registers, and a row's number a lane read.  U
+// rows are on their way together.  crossing[0] counts the chunks in which a word that
+// goes past the chunk's end begins, listed after it.
 template <typename TG, typename TO, int W, bool DROP>
 __global__ __launch_bounds__(256) void reduce_kernel(
     const typename TG::store *__restrict__ grad, int64_t ldg, typename TO::store *__restrict__ out,
     int64_t ldo, int32_t D, float factor, Dropout drop, bool accumulate, uint32_t col_tiles,
     GradPlan g, const uint32_t *__restrict__ key, const uint32_t *__restrict__ index,
     float *__restrict__ part, uint32_t *__restrict__ crossing) {
-  constexpr int U = 8;  // rows loaded together
+  // rows of a lane in flight: 32 registers of them
+  constexpr int U = sizeof(Packed<TG, W>) <= 8 ? 16 : 128 / (int)sizeof(Packed<TG, W>);
+  static_assert(64 % U == 0, "a batch lies within 64 positions");
   const int lane = threadIdx.x & 63;
   const uint32_t item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   const uint32_t c = item / col_tiles;
   if (c >= g.chunks) return;
   const uint32_t tile = item - c * col_tiles;
-  const int32_t col = (int32_t)(tile * 64 + lane) * W;
-  const int n = D - col < W ? (D - col > 0 ? D - col : 0) : W;
-  const typename TG::store *mine = grad + (n ? col : 0);
+  // n of the lane's columns exist; it reads, without a branch, the W columns
+  // that end where they do (in the last lanes some of the lane before)
+  const int32_t own = (int32_t)(tile * 64 + lane) * W;
+  const int n = D - own < W ? (D - own > 0 ? D - own : 0) : W;
+  const int32_t col = own < D - W ? own : D - W;
+  const bool straddles = DROP && D % W != 0 && tile == col_tiles - 1;
+  const uint32_t offset = (uint32_t)col * (uint32_t)sizeof(typename TG::store);
   const uint32_t begin = c * g.chunk;
   const uint32_t end = g.N - begin < g.chunk ? g.N : begin + g.chunk;
-  uint32_t word = key[begin];
-  bool began_here = begin == 0 || key[begin - 1] != word;
+  bool began_here = begin == 0 || key[begin - 1] != key[begin];
   float sum[W] = {};
-  for (uint32_t p = begin; p < end; p += U) {
-    float v[U][W];
-    uint32_t row[U], next[U];
+  for (uint32_t p = begin; p < end; p += 64) {
+    const uint32_t at = p + lane < end ? p + lane : end - 1;
+    const uint32_t word = key[at];
+    const uint32_t next = at + 1 < g.N ? key[at + 1] : g.V;  // the word after
+    const uint32_t row = index[at];
+    const bool live = p + lane < end && word < g.V;
+    // (tokens without a word are the last)
+    const int count = __popcll(__ballot(live));
+    const uint64_t ends = __ballot(live && (next != word || at + 1 == end));
+
+    if (count == 0) return;
+    for (int t = 0; t < count; t += U) {
+      Packed<TG, W> v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      row[u] = index[p + u < end ? p + u : end - 1];
-      next[u] = p + u + 1 < g.N ? key[p + u + 1] : g.V;  // the word after
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) load_elements<TG, W>(mine + (int64_t)row[u] * ldg, n, v[u]);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (p + u >= end) break;
-      if (word >= g.V) return;  // from here on only tokens without a word
-      uint32_t kept = 0;
-      if (DROP) kept = keep_bits((uint32_t)col >> 3, row[u], drop) >> (col & 7);
-#pragma unroll
-      for (int j = 0; j < W; ++j) sum[j] += !DROP || (kept >> j & 1) ? v[u][j] : 0.0f;
-      const bool goes_on = next[u] == word;
-      if (goes_on && p + u + 1 < end) continue;
-      if (began_here && !goes_on) {
-        if (n) write_row<TO, W>(out, ldo, word, col, n, factor, accumulate, sum);
-      } else {
-        float *slot = part + (int64_t)(2 * c + (began_here ? 1 : 0)) * g.ld_part + col;
-        if (n) store_elements<F32, W>(slot, W, sum);
-        if (began_here && tile == 0 && lane == 0) crossing[1 + atomicAdd(crossing, 1u)] = c;
+      for (int u = 0; u < U; ++u) {
+        const int64_t from = (uint32_t)__builtin_amdgcn_readlane(row, t + u);
+        uint64_t base = reinterpret_cast<uint64_t>(grad + from * ldg);
+        asm("" : "+s"(base));  // keeps the row's address in scalar registers
+        const auto *p = reinterpret_cast<const __attribute__((address_space(1))) char *>(base);
+        v[u] = load_packed<TG, W>((const typename TG::store *)(p + offset), W);
       }
-      began_here = true;
-      word = next[u];
 #pragma unroll
-      for (int j = 0; j < W; ++j) sum[j] = 0.0f;
+      for (int u = 0; u < U; ++u) {
+        if (t + u >= count) break;
+        uint32_t kept = 0;
+        if (DROP) {
+          const uint32_t r = __builtin_amdgcn_readlane(row, t + u), group = (uint32_t)col >> 3;
+          kept = keep_bits(group, r, drop);
+          if (straddles) kept |= keep_bits(group + 1, r, drop) << 8;
+          kept >>= col & 7;
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+          sum[j] += !DROP || (kept >> j & 1) ? TG::up(v[u].v[j]) : 0.0f;
+        if (!(ends >> (t + u) & 1)) continue;
+        const uint32_t w = __builtin_amdgcn_readlane(word, t + u);
+        const bool goes_on = __builtin_amdgcn_readlane(next, t + u) == w;
+        if (began_here && !goes_on) {
+          write_row<TO, W>(out, ldo, w, own, n, factor, accumulate, sum);
+        } else {
+          float *slot = part + (int64_t)(2 * c + (began_here ? 1 : 0)) * g.ld_part + col;
+          if (n) store_elements<F32, W>(slot, W, sum);
+          if (began_here && tile == 0 && lane == 0) crossing[1 + atomicAdd(crossing, 1u)] = c;
+        }
+        began_here = true;
+#pragma unroll
+        for (int j = 0; j < W; ++j) sum[j] = 0.0f;
+      }
     }
   }
 }
@@ -404,8 +436,9 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(
   const uint32_t items = crossing[0] * col_tiles;
   for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
     const uint32_t i = item / col_tiles;
-    const int32_t col = (int32_t)((item - i * col_tiles) * 64 + lane) * W;
-    const int n = D - col < W ? (D - col > 0 ? D - col : 0) : W;
+    const int32_t own = (int32_t)((item - i * col_tiles) * 64 + lane) * W;
+    const int n = D - own < W ? (D - own > 0 ? D - own : 0) : W;
+    const int32_t col = own < D - W ? own : D - W;
     const uint32_t c0 = crossing[1 + i];
     const uint32_t word = key[(c0 + 1) * g.chunk - 1];
     // the chunk in which the word ends: the last whose first key is the word
@@ -427,8 +460,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const uint32_t slot = 2 * (c0 + k + u) + (k + u == 0 ? 1 : 0);
-        load_elements<F32, W>(part + (int64_t)slot * g.ld_part + (n ? col : 0),
-                              n && k + u < to ? W : 0, v[u]);
+        load_elements<F32, W>(part + (int64_t)slot * g.ld_part + col, k + u < to ? W : 0, v[u]);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -440,11 +472,11 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(
       for (int j = 0; j < W; ++j) sums[wave - 1][j * 64 + lane] = sum[j];
     }
     __syncthreads();
-    if (wave == 0 && n) {
+    if (wave == 0) {
 #pragma unroll
       for (int j = 0; j < W; ++j)
         for (int q = 0; q < kJoinWaves - 1; ++q) sum[j] += sums[q][j * 64 + lane];
-      write_row<TO, W>(out, ldo, word, col, n, factor, accumulate, sum);
+      write_row<TO, W>(out, ldo, word, own, n, factor, accumulate, sum);
     }
     __syncthreads();
   }
