@@ -24,8 +24,31 @@ struct Dropout {
   uint32_t k0, k1;
 };
 
-// bit j of the result: whether column 8 group + j of `row` is kept
-__device__ __forceinline__ uint32_t keep_bits(uint32_t group, uint32_t row, const Dropout &d) {
+// The four words of columns 8 group .. 8 group + 7 of `row`.  Where `row` is
+// the same for a wavefront (in scalar registers) and `group` the same for
+// several rows, the compiler keeps two and a half of the ten rounds out of the
+// loop or in scalar registers: the counter's other words are uniform, and a
+// round mixes only two of the four.
+struct KeepWords {
+  uint32_t w[4];
+
+  // whether column 8 group + j is kept; j is known at compile time (an odd
+  // column's number is the word's upper half, which the whole word's comparison
+  // with q << 16 decides)
+  __device__ __forceinline__ bool kept(int j, uint32_t q) const {
+    return j & 1 ? w[j >> 1] >= q << 16 : (uint16_t)w[j >> 1] >= (uint16_t)q;
+  }
+
+  // bit j: whether column 8 group + j is kept
+  __device__ __forceinline__ uint32_t bits(uint32_t q) const {
+    uint32_t b = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) b |= (uint32_t)kept(j, q) << j;
+    return b;
+  }
+};
+
+__device__ __forceinline__ KeepWords keep_words(uint32_t group, uint32_t row, const Dropout &d) {
   uint32_t x0 = group, x1 = row, x2 = d.step, x3 = 1u, k0 = d.k0, k1 = d.k1;
 #pragma unroll
   for (int round = 0; round < 10; ++round) {
@@ -40,14 +63,7 @@ __device__ __forceinline__ uint32_t keep_bits(uint32_t group, uint32_t row, cons
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
   }
-  const uint32_t w[4] = {x0, x1, x2, x3};
-  uint32_t bits = 0;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    bits |= (uint32_t)((w[j] & 0xFFFFu) >= d.q) << (2 * j);
-    bits |= (uint32_t)((w[j] >> 16) >= d.q) << (2 * j + 1);
-  }
-  return bits;
+  return KeepWords{{x0, x1, x2, x3}};
 }
 
 }  // namespace lda

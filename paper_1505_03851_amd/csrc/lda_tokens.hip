@@ -67,14 +67,20 @@ int launch_rows(const void *x, int64_t ldx, const int32_t *word_id, void *out, i
   const int64_t rows = (int64_t)(kRowThreads >> lanes_log2) * kRowsEach;
   const int64_t tiles = (N + rows - 1) / rows * col_tiles;
   using S = typename T::store;
-  if (drop.q)
-    rows_kernel<T, GATHER, true><<<grid_of(tiles), kRowThreads, 0, s>>>(
-        (const S *)x, ldx, word_id, (S *)out, ldo, N, V, D, factor, drop, lanes_log2,
-        (uint32_t)col_tiles, tiles);
+#define LDA_ROWS(DROP, WIDE)                                                                     \
+  rows_kernel<T, GATHER, DROP, WIDE><<<grid_of(tiles), kRowThreads, 0, s>>>(                     \
+      (const S *)x, ldx, word_id, (S *)out, ldo, N, V, D, factor, drop, lanes_log2,              \
+      (uint32_t)col_tiles, tiles)
+  const bool wide = lanes_log2 >= 6;
+  if (drop.q && wide)
+    LDA_ROWS(true, true);
+  else if (drop.q)
+    LDA_ROWS(true, false);
+  else if (wide)
+    LDA_ROWS(false, true);
   else
-    rows_kernel<T, GATHER, false><<<grid_of(tiles), kRowThreads, 0, s>>>(
-        (const S *)x, ldx, word_id, (S *)out, ldo, N, V, D, factor, drop, lanes_log2,
-        (uint32_t)col_tiles, tiles);
+    LDA_ROWS(false, false);
+#undef LDA_ROWS
   return launch_status();
 }
 

@@ -392,16 +392,25 @@ __global__ __launch_bounds__(256) void reduce_kernel(
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (t + u >= count) break;
-        uint32_t kept = 0;
+        float x[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) x[j] = TG::up(v[u].v[j]);
         if (DROP) {
           const uint32_t r = __builtin_amdgcn_readlane(row, t + u), group = (uint32_t)col >> 3;
-          kept = keep_bits(group, r, drop);
-          if (straddles) kept |= keep_bits(group + 1, r, drop) << 8;
-          kept >>= col & 7;
+          const KeepWords k = keep_words(group, r, drop);
+          if (W == 8 && !straddles) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) x[j] = k.kept(j, drop.q) ? x[j] : 0.0f;
+          } else {
+            uint32_t bits = k.bits(drop.q);
+            if (straddles) bits |= keep_words(group + 1, r, drop).bits(drop.q) << 8;
+            bits >>= col & 7;
+#pragma unroll
+            for (int j = 0; j < W; ++j) x[j] = bits >> j & 1 ? x[j] : 0.0f;
+          }
         }
 #pragma unroll
-        for (int j = 0; j < W; ++j)
-          sum[j] += !DROP || (kept >> j & 1) ? TG::up(v[u].v[j]) : 0.0f;
+        for (int j = 0; j < W; ++j) sum[j] += x[j];
         if (!(ends >> (t + u) & 1)) continue;
         const uint32_t w = __builtin_amdgcn_readlane(word, t + u);
         const bool goes_on = __builtin_amdgcn_readlane(next, t + u) == w;

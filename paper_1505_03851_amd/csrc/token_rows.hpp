@@ -19,14 +19,16 @@ constexpr int kRowThreads = 256;
 constexpr int kRowsEach = 4;  // rows of one lane, loaded together
 
 // A workgroup covers (256 >> lanes_log2) * kRowsEach rows and
-// 8 << lanes_log2 columns; `col_tiles` such tiles cover a row.
-template <typename T, bool GATHER, bool DROP>
+// 8 << lanes_log2 columns; `col_tiles` such tiles cover a row.  WIDE: lanes_log2
+// is 6 or more, so a wavefront's rows are known to scalar registers.
+template <typename T, bool GATHER, bool DROP, bool WIDE>
 __global__ __launch_bounds__(kRowThreads) void rows_kernel(
     const typename T::store *__restrict__ x, int64_t ldx, const int32_t *__restrict__ word_id,
     typename T::store *out, int64_t ldo, int64_t N, int32_t V, int64_t D, float factor,
     Dropout drop, int lanes_log2, uint32_t col_tiles, int64_t tiles) {
   const int lane = (int)threadIdx.x & ((1 << lanes_log2) - 1);
-  const int slot = (int)threadIdx.x >> lanes_log2;
+  const int own_slot = (int)threadIdx.x >> lanes_log2;
+  const int slot = WIDE ? __builtin_amdgcn_readfirstlane(own_slot) : own_slot;
   const int slots = kRowThreads >> lanes_log2;
   for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const int64_t row_tile = tile / col_tiles;
@@ -51,9 +53,14 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(
     for (int r = 0; r < kRowsEach; ++r) {
       const int64_t row = first + (int64_t)r * slots;
       if (row >= N) break;
-      const uint32_t kept = DROP ? keep_bits((uint32_t)(col >> 3), (uint32_t)row, drop) : 0xFFu;
+      if (DROP) {
+        const KeepWords k = keep_words((uint32_t)(col >> 3), (uint32_t)row, drop);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[r][j] = !DROP || (kept >> j & 1) ? v[r][j] * factor : 0.0f;
+        for (int j = 0; j < 8; ++j) v[r][j] = k.kept(j, drop.q) ? v[r][j] * factor : 0.0f;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[r][j] *= factor;
+      }
       store_elements<T, 8>(out + row * ldo + col, n, v[r]);
     }
   }
