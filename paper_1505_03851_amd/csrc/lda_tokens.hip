@@ -20,6 +20,9 @@
 #include "token_grad.hpp"
 #include "logits.hpp"
 
+#ifndef LDA_MINWG
+#define LDA_MINWG 512
+#endif
 namespace lda {
 namespace {
 
@@ -216,12 +219,13 @@ int launch_grad(const void *grad, int64_t ldg, const int32_t *word_id, void *out
   return launch_status();
 }
 
-// tokens a workgroup takes of a row: the most groups that still give every
-// compute unit two workgroups
-int slice_of(int64_t B, int64_t V) {
-  int slice = 16 * kGroup;
-  while (slice > kGroup && B * ((V + slice - 1) / slice) < 512) slice /= 2;
-  return slice;
+// The groups (and wavefronts) of a workgroup: the most that still give every
+// compute unit two workgroups, since each workgroup reads its row's history.
+int group_waves(int64_t B, int64_t V) {
+  const int64_t groups = (V + kGroup - 1) / kGroup;
+  int waves = kGroupWaves;
+  while (waves > 1 && B * ((groups + waves - 1) / waves) < LDA_MINWG) waves /= 2;
+  return waves;
 }
 
 int make_rules(const lda_logit_rules *r, int64_t B, int32_t V, Rules *out) {
@@ -248,10 +252,11 @@ template <typename T>
 int launch_penalise(const void *logits, int64_t ld, void *out, int64_t ldo, int64_t B, int32_t V,
                     const Rules &r, hipStream_t s) {
   using S = typename T::store;
-  const int slice = slice_of(B, V);
-  const int64_t slices = ((int64_t)V + slice - 1) / slice, tiles = B * slices;
-  penalise_kernel<T><<<grid_of(tiles), kLogitThreads, r.history ? 4 * slice : 0, s>>>(
-      (const S *)logits, ld, (S *)out, ldo, V, r, slice, (uint32_t)slices, tiles);
+  const int waves = group_waves(B, V);
+  const int64_t slices = ((int64_t)V + waves * kGroup - 1) / (waves * kGroup), tiles = B * slices;
+  const size_t lds = r.history ? 4 * (size_t)waves * kGroup : 0;
+  penalise_kernel<T><<<grid_of(tiles), 64 * waves, lds, s>>>((const S *)logits, ld, (S *)out, ldo,
+                                                             V, r, (uint32_t)slices, tiles);
   return launch_status();
 }
 
@@ -261,20 +266,18 @@ int launch_draw(const void *logits, int64_t ld, int64_t B, int32_t V, const Rule
                 const int32_t *position, int32_t *z, float *prob, GroupSum *groups,
                 hipStream_t s) {
   using S = typename T::store;
-  const int slice = slice_of(B, V);
-  const int64_t slices = ((int64_t)V + slice - 1) / slice, tiles = B * slices;
+  const int waves = group_waves(B, V);
+  const int64_t slices = ((int64_t)V + waves * kGroup - 1) / (waves * kGroup), tiles = B * slices;
   const uint32_t per_row = (uint32_t)(((int64_t)V + kGroup - 1) / kGroup);
-  const size_t lds = r.history ? 4 * slice : 0;
-  group_kernel<T, false><<<grid_of(tiles), kLogitThreads, lds, s>>>(
-      (const S *)logits, ld, V, r, temperature, min_p, groups, per_row, slice, (uint32_t)slices,
-      tiles);
+  const size_t lds = r.history ? 4 * (size_t)waves * kGroup : 0;
+  group_kernel<T, false><<<grid_of(tiles), 64 * waves, lds, s>>>(
+      (const S *)logits, ld, V, r, temperature, min_p, groups, per_row, (uint32_t)slices, tiles);
   if (min_p)
-    group_kernel<T, true><<<grid_of(tiles), kLogitThreads, lds, s>>>(
-        (const S *)logits, ld, V, r, temperature, min_p, groups, per_row, slice, (uint32_t)slices,
-        tiles);
-  draw_kernel<T><<<grid_of(B), kLogitThreads, 0, s>>>((const S *)logits, ld, B, V, r, temperature,
-                                                      min_p, seed, position, groups, per_row, z,
-                                                      prob);
+    group_kernel<T, true><<<grid_of(tiles), 64 * waves, lds, s>>>(
+        (const S *)logits, ld, V, r, temperature, min_p, groups, per_row, (uint32_t)slices, tiles);
+  draw_kernel<T><<<grid_of(B), kDrawThreads, 0, s>>>((const S *)logits, ld, B, V, r, temperature,
+                                                     min_p, seed, position, groups, per_row, z,
+                                                     prob);
   return launch_status();
 }
 

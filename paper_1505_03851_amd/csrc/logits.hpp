@@ -26,10 +26,11 @@
 
 namespace lda {
 
-constexpr int kLogitThreads = 256;
-constexpr int kLogitWaves = kLogitThreads / 64;
 constexpr int kGroup = 1024;  // tokens of a group, the unit of a wavefront
-constexpr int kGroupSteps = kGroup / 512;
+constexpr int kSteps = kGroup / 512;
+constexpr int kGroupWaves = 8;   // groups of a workgroup, at most
+constexpr int kDrawThreads = 1024;  // of a row's last step: one for each token of a group
+constexpr int kDrawWaves = kDrawThreads / 64;
 constexpr uint32_t kSeen = 0x80000000u;
 
 struct Rules {
@@ -75,40 +76,73 @@ __device__ __forceinline__ float ruled(float x, uint32_t count, const RowRules &
   return x;
 }
 
-// The uses of the tokens [first, first + size) in row b's history, counted in
-// LDS: generated tokens in the low bits, kSeen for those of the prompt.  The
-// whole workgroup calls it; false where the row has no history.
-__device__ __forceinline__ bool count_history(const Rules &r, int64_t b, int64_t first, int size,
-                                              uint32_t *count) {
-  if (!r.history) return false;
+// A row's history, four tokens to a lane and load.
+struct History {
+  const int32_t *tokens;
+  int64_t size, prompt;  // 0 tokens where there is no history
+};
+
+__device__ __forceinline__ History row_history(const Rules &r, int64_t b) {
+  if (!r.history) return History{nullptr, 0, 0};
   int64_t n = r.lengths[b];
   n = n < r.capacity ? n : r.capacity;
-  if (n <= 0) return false;
-  const int64_t prompt = r.prompt ? r.prompt[b] : 0;
-  const int32_t *h = r.history + b * r.ld_history;
-  for (int i = threadIdx.x; i < size; i += kLogitThreads) count[i] = 0;
-  __syncthreads();
-  for (int64_t i = threadIdx.x; i < n; i += kLogitThreads) {
-    const int64_t at = (int64_t)h[i] - first;
-    if (at < 0 || at >= size) continue;
-    if (i < prompt)
+  return History{r.history + b * r.ld_history, n > 0 ? n : 0, r.prompt ? r.prompt[b] : 0};
+}
+
+__device__ __forceinline__ words4 history_load(const History &h, int64_t i) {
+  words4 t;
+  if (i + 4 <= h.size) {
+    t = *reinterpret_cast<const words4_any *>(h.tokens + i);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) t[j] = i + j < h.size ? (uint32_t)h.tokens[i + j] : 0xFFFFFFFFu;
+  }
+  return t;
+}
+
+// Adds the tokens t (of which the first is number i) that lie in [first, first +
+// size) to `count`: generated tokens in the low bits, kSeen for the prompt's.
+__device__ __forceinline__ void history_count(const History &h, int64_t i, words4 t, int64_t first,
+                                              uint32_t size, uint32_t *count) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    // (a negative token is above every vocabulary as an unsigned number)
+    const int64_t at = (int64_t)t[j] - first;
+    if ((uint64_t)at >= size) continue;
+    if (i + j < h.prompt)
       atomicOr(&count[at], kSeen);
     else
       atomicAdd(&count[at], 1u);
   }
-  __syncthreads();
-  return true;
 }
 
-// 8 logits of a row from token v on, under the rules; n of them exist
-template <typename T>
-__device__ __forceinline__ void ruled_logits(const typename T::store *row, int64_t v, int n,
-                                             const uint32_t *count, const RowRules &r,
-                                             float (&x)[8]) {
-  load_elements<T, 8>(row + v, n, x);
+// The uses of the tokens [first, first + size) in a row's history, counted in
+// LDS (which the caller has cleared and synchronised) by the whole workgroup.
+__device__ __forceinline__ void count_history(const History &h, int64_t first, uint32_t size,
+                                              uint32_t *count) {
+  const int64_t step = 4 * (int64_t)blockDim.x;
+  for (int64_t i = 4 * (int64_t)threadIdx.x; i < h.size; i += 2 * step) {
+    const words4 a = history_load(h, i), b = history_load(h, i + step);
+    history_count(h, i, a, first, size, count);
+    history_count(h, i + step, b, first, size, count);
+  }
+}
+
+// The logits of 8 neighbouring tokens from v on under the rules; n of them
+// exist.  `count`: their uses, or null.
+__device__ __forceinline__ void apply_rules(int64_t v, int n, const uint32_t *count,
+                                            const RowRules &r, float (&x)[8]) {
   if (count) {
+    uint32_t c[8], any = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = ruled(x[j], count[j], r);
+    for (int j = 0; j < 8; ++j) {
+      c[j] = count[j];
+      any |= c[j];
+    }
+    if (any) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = ruled(x[j], c[j], r);
+    }
   }
   if (r.bias) {
     float b[8];
@@ -117,30 +151,61 @@ __device__ __forceinline__ void ruled_logits(const typename T::store *row, int64
     for (int j = 0; j < 8; ++j) x[j] += b[j];
   }
   if (r.mask) {
-    const uint32_t bits = r.mask[v >> 5] >> (v & 31);
+    const uint32_t bits = n > 0 ? r.mask[v >> 5] >> (v & 31) : 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = bits >> j & 1 ? x[j] : -INFINITY;
   }
 }
 
-// A workgroup takes `slice` tokens of one row.
+// A wavefront's group of a row: its logits on their way while the workgroup
+// counts the row's history, then in float under the rules (x[s][j]: token
+// first + 512 s + 8 lane + j).  The whole workgroup calls it, wavefronts past the
+// end of the row too.
 template <typename T>
-__global__ __launch_bounds__(kLogitThreads) void penalise_kernel(
+__device__ __forceinline__ void group_logits(const typename T::store *row, int64_t first, int64_t V,
+                                             const History &h, const RowRules &r, uint32_t *lds,
+                                             float (&x)[kSteps][8], int (&n)[kSteps]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Packed<T, 8> v[kSteps];
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const int64_t left = V - first - s * 512 - lane * 8;
+    n[s] = left < 8 ? (left > 0 ? (int)left : 0) : 8;
+    v[s] = load_packed<T, 8>(row + first + s * 512 + lane * 8, n[s]);
+  }
+  if (h.size) {
+    words4 *mine = reinterpret_cast<words4 *>(lds + wave * kGroup);
+#pragma unroll
+    for (int i = 0; i < kGroup / 256; ++i) mine[i * 64 + lane] = words4{};
+    __syncthreads();
+    count_history(h, first - wave * kGroup, (blockDim.x >> 6) * kGroup, lds);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[s][j] = T::up(v[s].v[j]);
+    const int at = s * 512 + lane * 8;
+    apply_rules(first + at, n[s], h.size ? lds + wave * kGroup + at : nullptr, r, x[s]);
+  }
+}
+
+// A workgroup takes a group of one row for each of its wavefronts.
+template <typename T>
+__global__ __launch_bounds__(64 * kGroupWaves) void penalise_kernel(
     const typename T::store *logits, int64_t ld, typename T::store *out, int64_t ldo, int64_t V,
-    Rules rules, int slice, uint32_t slices, int64_t tiles) {
-  extern __shared__ uint32_t count[];
+    Rules rules, uint32_t slices, int64_t tiles) {
+  extern __shared__ uint32_t lds[];
   for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const int64_t b = tile / slices;
-    const int64_t first = (tile - b * slices) * slice;
-    const int size = V - first < slice ? (int)(V - first) : slice;
-    const RowRules r = row_rules(rules, b);
-    const bool counted = count_history(rules, b, first, slice, count);
-    for (int i = (int)threadIdx.x * 8; i < size; i += kLogitThreads * 8) {
-      float x[8];
-      const int n = size - i < 8 ? size - i : 8;
-      ruled_logits<T>(logits + b * ld, first + i, n, counted ? count + i : nullptr, r, x);
-      store_elements<T, 8>(out + b * ldo + first + i, n, x);
-    }
+    const int64_t first = (tile - b * slices) * (blockDim.x >> 6) * kGroup +
+                          (int64_t)(threadIdx.x >> 6) * kGroup;
+    float x[kSteps][8];
+    int n[kSteps];
+    group_logits<T>(logits + b * ld, first, V, row_history(rules, b), row_rules(rules, b), lds, x, n);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+      store_elements<T, 8>(out + b * ldo + first + s * 512 + (threadIdx.x & 63) * 8, n[s], x[s]);
     __syncthreads();
   }
 }
@@ -186,75 +251,55 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// A wavefront's group of a row, 8 logits of each of kGroupSteps steps per lane;
-// NaN counts as -inf.
-template <typename T>
-__device__ __forceinline__ void group_logits(const typename T::store *row, int64_t first, int64_t V,
-                                             const uint32_t *count, const RowRules &r,
-                                             float (&x)[kGroupSteps][8]) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int s = 0; s < kGroupSteps; ++s) {
-    const int i = s * 512 + lane * 8;
-    const int64_t left = V - first - i;
-    const int n = left < 8 ? (left > 0 ? (int)left : 0) : 8;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[s][j] = -INFINITY;
-    if (n > 0) ruled_logits<T>(row, first + i, n, count ? count + i : nullptr, r, x[s]);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[s][j] = j < n && x[s][j] == x[s][j] ? x[s][j] : -INFINITY;
-  }
-}
-
-// The groups' largest logits and sums of weights; a workgroup takes `slice`
-// tokens of one row, a wavefront a group at a time.  FLOOR: the groups' largest
-// are known, and the sums of the rows with a floor are made again over what is
-// above it.
+// The groups' largest logits and sums of weights; NaN counts as -inf.  FLOOR:
+// the groups' largest are known, and the sums of the rows with a floor are made
+// again over what is above it.
 template <typename T, bool FLOOR>
-__global__ __launch_bounds__(kLogitThreads) void group_kernel(
+__global__ __launch_bounds__(64 * kGroupWaves) void group_kernel(
     const typename T::store *__restrict__ logits, int64_t ld, int64_t V, Rules rules,
-    const float *temperature, const float *min_p, GroupSum *groups, uint32_t per_row, int slice,
+    const float *temperature, const float *min_p, GroupSum *groups, uint32_t per_row,
     uint32_t slices, int64_t tiles) {
-  extern __shared__ uint32_t count[];
-  const int lane = threadIdx.x & 63;
+  extern __shared__ uint32_t lds[];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const int64_t b = tile / slices;
-    const int64_t first = (tile - b * slices) * slice;
+    const uint32_t g0 = (uint32_t)(tile - b * slices) * waves, g = g0 + wave;
     const DrawRow d = draw_row(temperature, min_p, b);
     GroupSum *mine = groups + b * per_row;
     float top = -INFINITY;
     if (FLOOR) {
       if (d.greedy || d.floor == -INFINITY) continue;
-      for (uint32_t g = lane; g < per_row; g += 64) top = fmaxf(top, mine[g].top);
+      for (uint32_t i = lane; i < per_row; i += 64) top = fmaxf(top, mine[i].top);
       top = wave_max(top);
-    }
-    const RowRules r = row_rules(rules, b);
-    const bool counted = count_history(rules, b, first, slice, count);
-    for (int i = (int)(threadIdx.x >> 6) * kGroup; i < slice && first + i < V;
-         i += kLogitWaves * kGroup) {
-      const int64_t g = (first + i) / kGroup;
-      if (FLOOR && !above_floor(mine[g].top, top, d)) {
-        if (lane == 0) mine[g].sum = 0.0f;
+      bool any = false;  // a group of the workgroup's that reaches the floor
+      for (int w = 0; w < waves && g0 + w < per_row; ++w) any |= above_floor(mine[g0 + w].top, top, d);
+      if (!any) {
+        if (lane == 0 && g < per_row) mine[g].sum = 0.0f;
         continue;
       }
-      float x[kGroupSteps][8];
-      group_logits<T>(logits + b * ld, first + i, V, counted ? count + i : nullptr, r, x);
-      float m = -INFINITY, sum = 0.0f;
-#pragma unroll
-      for (int s = 0; s < kGroupSteps; ++s)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = fmaxf(m, x[s][j]);
-      m = wave_max(m);
-      if (m != -INFINITY) {
-#pragma unroll
-        for (int s = 0; s < kGroupSteps; ++s)
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (!FLOOR || above_floor(x[s][j], top, d)) sum += weight(x[s][j], m, d.inverse);
-        sum = wave_sum(sum);
-      }
-      if (lane == 0) mine[g] = GroupSum{m, sum};
     }
+    float x[kSteps][8];
+    int n[kSteps];
+    group_logits<T>(logits + b * ld, (int64_t)g * kGroup, V, row_history(rules, b),
+                    row_rules(rules, b), lds, x, n);
+    float m = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        x[s][j] = j < n[s] && x[s][j] == x[s][j] ? x[s][j] : -INFINITY;
+        m = fmaxf(m, x[s][j]);
+      }
+    m = wave_max(m);
+    if (m != -INFINITY) {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (!FLOOR || above_floor(x[s][j], top, d)) sum += weight(x[s][j], m, d.inverse);
+      sum = wave_sum(sum);
+    }
+    if (lane == 0 && g < per_row) mine[g] = GroupSum{m, sum};
     __syncthreads();
   }
 }
@@ -278,33 +323,39 @@ __device__ __forceinline__ uint64_t block_first(float value, uint32_t index, uin
   }
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = k;
   __syncthreads();
-  for (int w = 0; w < kLogitWaves; ++w) k = waves[w] < k ? waves[w] : k;
+#pragma unroll
+  for (int w = 0; w < kDrawWaves; ++w) k = waves[w] < k ? waves[w] : k;
   __syncthreads();
   return k;
 }
 
-// One workgroup per row: the group, then the token in it.
+// One workgroup per row: the group, then the token in it, one to a thread.
 template <typename T>
-__global__ __launch_bounds__(kLogitThreads) void draw_kernel(
+__global__ __launch_bounds__(kDrawThreads) void draw_kernel(
     const typename T::store *__restrict__ logits, int64_t ld, int64_t B, int64_t V, Rules rules,
     const float *temperature, const float *min_p, const int64_t *__restrict__ seed,
     const int32_t *__restrict__ position, const GroupSum *__restrict__ groups, uint32_t per_row,
     int32_t *z, float *prob) {
   __shared__ uint32_t count[kGroup];
-  __shared__ uint64_t firsts[kLogitWaves];
-  __shared__ float parts[2][kLogitWaves];
+  __shared__ uint64_t firsts[kDrawWaves];
+  __shared__ float parts[2][kDrawWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
     const DrawRow d = draw_row(temperature, min_p, b);
     const GroupSum *mine = groups + b * per_row;
     const uint64_t s = (uint64_t)seed[b];
     const uint32_t pos = (uint32_t)position[b];
+    const History h = row_history(rules, b);
+    // the first tokens of the history, on their way before the group is known
+    const words4 tokens = history_load(h, 4 * threadIdx.x);
+    count[threadIdx.x] = 0;
     float top = -INFINITY;
-    for (uint32_t g = threadIdx.x; g < per_row; g += kLogitThreads) top = fmaxf(top, mine[g].top);
+    for (uint32_t g = threadIdx.x; g < per_row; g += kDrawThreads) top = fmaxf(top, mine[g].top);
     top = wave_max(top);
     if (lane == 0) parts[0][wave] = top;
     __syncthreads();
-    for (int w = 0; w < kLogitWaves; ++w) top = fmaxf(top, parts[0][w]);
+#pragma unroll
+    for (int w = 0; w < kDrawWaves; ++w) top = fmaxf(top, parts[0][w]);
     if (top == -INFINITY) {  // nothing may be drawn
       if (threadIdx.x == 0) {
         z[b] = -1;
@@ -315,7 +366,7 @@ __global__ __launch_bounds__(kLogitThreads) void draw_kernel(
     }
     float best = INFINITY, total = 0.0f;
     uint32_t at = 0xFFFFFFFFu;
-    for (uint32_t g = threadIdx.x; g < per_row; g += kLogitThreads) {
+    for (uint32_t g = threadIdx.x; g < per_row; g += kDrawThreads) {
       const GroupSum q = mine[g];
       float v;
       if (d.greedy) {
@@ -334,39 +385,33 @@ __global__ __launch_bounds__(kLogitThreads) void draw_kernel(
     if (lane == 0) parts[1][wave] = total;
     const uint32_t group = (uint32_t)block_first(best, at, firsts);
     total = 0.0f;
-    for (int w = 0; w < kLogitWaves; ++w) total += parts[1][w];
-    const int64_t first = (int64_t)group * kGroup;
+#pragma unroll
+    for (int w = 0; w < kDrawWaves; ++w) total += parts[1][w];
+    const int64_t first = (int64_t)group * kGroup, token = first + threadIdx.x;
     const float group_top = mine[group].top;
     const RowRules r = row_rules(rules, b);
-    const bool counted = count_history(rules, b, first, kGroup, count);
-    best = INFINITY;
-    at = 0xFFFFFFFFu;
-    float mine_x = 0.0f;
-    const int i = (int)threadIdx.x * 8;
-    if (i < kGroup && first + i < V) {
-      float x[8];
-      const int n = V - first - i < 8 ? (int)(V - first - i) : 8;
-      ruled_logits<T>(logits + b * ld, first + i, n, counted ? count + i : nullptr, r, x);
-      for (int j = 0; j < n; ++j) {
-        float v;
-        if (d.greedy)
-          v = x[j] == top ? 0.0f : INFINITY;
-        else if (x[j] == x[j] && x[j] != -INFINITY && above_floor(x[j], top, d))
-          v = variate((uint32_t)(first + i + j), pos, 3u, s) / weight(x[j], group_top, d.inverse);
-        else
-          v = INFINITY;
-        if (v < best || at == 0xFFFFFFFFu) {
-          best = v;
-          at = (uint32_t)(i + j);
-          mine_x = x[j];
-        }
-      }
+    const bool there = token < V;
+    float x = there ? T::up(logits[b * ld + token]) : -INFINITY;
+    const float bias = there && r.bias ? r.bias[token] : 0.0f;
+    const uint32_t allowed = there && r.mask ? r.mask[token >> 5] : 0xFFFFFFFFu;
+    if (h.size) {
+      history_count(h, 4 * threadIdx.x, tokens, first, kGroup, count);
+      for (int64_t i = 4 * (threadIdx.x + kDrawThreads); i < h.size; i += 4 * kDrawThreads)
+        history_count(h, i, history_load(h, i), first, kGroup, count);
+      __syncthreads();
+      x = ruled(x, count[threadIdx.x], r);
     }
-    const uint32_t won = (uint32_t)block_first(best, at, firsts);
-    if (at == won) {
-      z[b] = (int32_t)(first + won);
-      const double share =
-          mine_x == top ? 1.0 : exp(((double)mine_x - (double)top) / (double)d.temperature);
+    if (r.bias) x += bias;
+    if (!(allowed >> (token & 31) & 1)) x = -INFINITY;
+    float v = INFINITY;
+    if (d.greedy)
+      v = x == top ? 0.0f : INFINITY;
+    else if (x == x && x != -INFINITY && above_floor(x, top, d))
+      v = variate((uint32_t)token, pos, 3u, s) / weight(x, group_top, d.inverse);
+    const uint32_t won = (uint32_t)block_first(v, threadIdx.x, firsts);
+    if (threadIdx.x == won) {
+      z[b] = (int32_t)token;
+      const double share = x == top ? 1.0 : exp(((double)x - (double)top) / (double)d.temperature);
       prob[b] = d.greedy ? 1.0f : (float)(share / (double)total);
     }
     __syncthreads();
