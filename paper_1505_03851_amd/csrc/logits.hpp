@@ -28,8 +28,8 @@ namespace lda {
 
 constexpr int kGroup = 1024;  // tokens of a group, the unit of a wavefront
 constexpr int kSteps = kGroup / 512;
-constexpr int kGroupWaves = 8;   // groups of a workgroup, at most
-constexpr int kDrawThreads = 1024;  // of a row's last step: one for each token of a group
+constexpr int kGroupWaves = 8;      // groups of a workgroup that applies the rules, at most
+constexpr int kDrawThreads = 1024;  // of a workgroup that draws: one for each token of a group
 constexpr int kDrawWaves = kDrawThreads / 64;
 constexpr uint32_t kSeen = 0x80000000u;
 
@@ -46,14 +46,18 @@ struct Rules {
 };
 
 struct RowRules {
-  float repetition, frequency, presence;
+  float repetition, inverse, frequency, presence;  // inverse: 1 / repetition
+  bool tame;  // repetition within 2^-30 .. 2^30
   const float *bias;
   const uint32_t *mask;
 };
 
 __device__ __forceinline__ RowRules row_rules(const Rules &r, int64_t b) {
-  return RowRules{r.repetition ? r.repetition[b] : 1.0f, r.frequency ? r.frequency[b] : 0.0f,
-                  r.presence ? r.presence[b] : 0.0f, r.bias ? r.bias + b * r.ld_bias : nullptr,
+  const float repetition = r.repetition ? r.repetition[b] : 1.0f;
+  return RowRules{repetition, 1.0f / repetition, r.frequency ? r.frequency[b] : 0.0f,
+                  r.presence ? r.presence[b] : 0.0f,
+                  repetition > 0x1p-30f && repetition < 0x1p+30f,
+                  r.bias ? r.bias + b * r.ld_bias : nullptr,
                   r.mask ? r.mask + b * r.ld_mask : nullptr};
 }
 
@@ -64,16 +68,22 @@ __device__ __forceinline__ float rounded(float x) {
   return x;
 }
 
+// x / r, rounded as the division is: with y = 1 / r rounded, q = x y and
+// q + (x - q r) y, both sums fused (an infinite q stays).  Where r is extreme
+// enough for bits to be lost on the way, the division itself.
+__device__ __forceinline__ float divided(float x, const RowRules &r) {
+  const float q = x * r.inverse, refined = fmaf(fmaf(-q, r.repetition, x), r.inverse, q);
+  return fabsf(q) < INFINITY ? refined : q;
+}
+
+// A logit with a use in the history.  EXACT: repetition within 2^-30 .. 2^30.
+template <bool EXACT>
 __device__ __forceinline__ float ruled(float x, uint32_t count, const RowRules &r) {
-  if (count) {
-    x = x > 0.0f ? x / r.repetition : rounded(x * r.repetition);
-    const uint32_t c = count & ~kSeen;
-    if (c) {
-      x -= rounded(r.frequency * (float)c);
-      x -= r.presence;
-    }
-  }
-  return x;
+  const float over = EXACT ? divided(x, r) : x / r.repetition;
+  x = x > 0.0f ? over : rounded(x * r.repetition);
+  const uint32_t c = count & ~kSeen;
+  x -= rounded(r.frequency * (float)c);
+  return x - (c ? r.presence : 0.0f);
 }
 
 // A row's history, four tokens to a lane and load.
@@ -102,14 +112,17 @@ __device__ __forceinline__ words4 history_load(const History &h, int64_t i) {
 
 // Adds the tokens t (of which the first is number i) that lie in [first, first +
 // size) to `count`: generated tokens in the low bits, kSeen for the prompt's.
-__device__ __forceinline__ void history_count(const History &h, int64_t i, words4 t, int64_t first,
+// (As an unsigned number a negative token lies past every vocabulary: where the
+// difference wraps into the range, it is to a place past the row's end.)
+__device__ __forceinline__ void history_count(const History &h, int64_t i, words4 t, uint32_t first,
                                               uint32_t size, uint32_t *count) {
+  const int64_t left = h.prompt - i;
+  const int prompt = left > 4 ? 4 : left < 0 ? 0 : (int)left;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    // (a negative token is above every vocabulary as an unsigned number)
-    const int64_t at = (int64_t)t[j] - first;
-    if ((uint64_t)at >= size) continue;
-    if (i + j < h.prompt)
+    const uint32_t at = t[j] - first;
+    if (at >= size) continue;
+    if (j < prompt)
       atomicOr(&count[at], kSeen);
     else
       atomicAdd(&count[at], 1u);
@@ -118,7 +131,7 @@ __device__ __forceinline__ void history_count(const History &h, int64_t i, words
 
 // The uses of the tokens [first, first + size) in a row's history, counted in
 // LDS (which the caller has cleared and synchronised) by the whole workgroup.
-__device__ __forceinline__ void count_history(const History &h, int64_t first, uint32_t size,
+__device__ __forceinline__ void count_history(const History &h, uint32_t first, uint32_t size,
                                               uint32_t *count) {
   const int64_t step = 4 * (int64_t)blockDim.x;
   for (int64_t i = 4 * (int64_t)threadIdx.x; i < h.size; i += 2 * step) {
@@ -128,84 +141,108 @@ __device__ __forceinline__ void count_history(const History &h, int64_t first, u
   }
 }
 
-// The logits of 8 neighbouring tokens from v on under the rules; n of them
-// exist.  `count`: their uses, or null.
-__device__ __forceinline__ void apply_rules(int64_t v, int n, const uint32_t *count,
-                                            const RowRules &r, float (&x)[8]) {
-  if (count) {
-    uint32_t c[8], any = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      c[j] = count[j];
-      any |= c[j];
-    }
-    if (any) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = ruled(x[j], c[j], r);
-    }
-  }
-  if (r.bias) {
-    float b[8];
-    load_elements<F32, 8>(r.bias + v, n, b);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] += b[j];
-  }
-  if (r.mask) {
-    const uint32_t bits = n > 0 ? r.mask[v >> 5] >> (v & 31) : 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = bits >> j & 1 ? x[j] : -INFINITY;
-  }
-}
-
-// A wavefront's group of a row: its logits on their way while the workgroup
-// counts the row's history, then in float under the rules (x[s][j]: token
-// first + 512 s + 8 lane + j).  The whole workgroup calls it, wavefronts past the
-// end of the row too.
+// A wavefront's group of a row as loaded: token first + 512 s + 8 lane + j is
+// element j of step s; n[s] of a lane's 8 exist.
 template <typename T>
-__device__ __forceinline__ void group_logits(const typename T::store *row, int64_t first, int64_t V,
-                                             const History &h, const RowRules &r, uint32_t *lds,
-                                             float (&x)[kSteps][8], int (&n)[kSteps]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Packed<T, 8> v[kSteps];
+struct Group {
+  Packed<T, 8> x[kSteps];
+  uint32_t allowed[kSteps];  // mask bits of the lane's tokens, from bit 0
+  int n[kSteps];
+};
+
+template <typename T>
+__device__ __forceinline__ void load_group(const typename T::store *row, int64_t first, int64_t V,
+                                           const RowRules &r, Group<T> &g) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
-    const int64_t left = V - first - s * 512 - lane * 8;
-    n[s] = left < 8 ? (left > 0 ? (int)left : 0) : 8;
-    v[s] = load_packed<T, 8>(row + first + s * 512 + lane * 8, n[s]);
-  }
-  if (h.size) {
-    words4 *mine = reinterpret_cast<words4 *>(lds + wave * kGroup);
-#pragma unroll
-    for (int i = 0; i < kGroup / 256; ++i) mine[i * 64 + lane] = words4{};
-    __syncthreads();
-    count_history(h, first - wave * kGroup, (blockDim.x >> 6) * kGroup, lds);
-    __syncthreads();
-  }
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[s][j] = T::up(v[s].v[j]);
-    const int at = s * 512 + lane * 8;
-    apply_rules(first + at, n[s], h.size ? lds + wave * kGroup + at : nullptr, r, x[s]);
+    const int64_t v = first + s * 512 + lane * 8, left = V - v;
+    g.n[s] = left < 8 ? (left > 0 ? (int)left : 0) : 8;
+    g.x[s] = load_packed<T, 8>(row + v, g.n[s]);
+    g.allowed[s] = r.mask && g.n[s] > 0 ? r.mask[v >> 5] >> (v & 31) : 0xFFu;
   }
 }
 
-// A workgroup takes a group of one row for each of its wavefronts.
+// The group's logits in float under the rules.  `count`: the uses of the group's
+// tokens in LDS, or null.
+template <typename T>
+__device__ __forceinline__ void rule_group(const Group<T> &g, int64_t first, const uint32_t *count,
+                                           const RowRules &r, float (&x)[kSteps][8]) {
+  const int lane = threadIdx.x & 63;
+  float bias[kSteps][8];
+  if (r.bias) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+      load_elements<F32, 8>(r.bias + first + s * 512 + lane * 8, g.n[s], bias[s]);
+  }
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[s][j] = T::up(g.x[s].v[j]);
+    if (count) {
+      uint32_t c[8], any = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        c[j] = count[s * 512 + lane * 8 + j];
+        any |= c[j];
+      }
+      if (any && r.tame) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[s][j] = c[j] ? ruled<true>(x[s][j], c[j], r) : x[s][j];
+      } else if (any) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[s][j] = c[j] ? ruled<false>(x[s][j], c[j], r) : x[s][j];
+      }
+    }
+    if (r.bias) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[s][j] += bias[s][j];
+    }
+    if (r.mask) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        // all ones where allowed; two instructions a logit
+        const uint32_t keep = (uint32_t)((int32_t)(g.allowed[s] << (31 - j)) >> 31);
+        const uint32_t bits = __builtin_bit_cast(uint32_t, x[s][j]);
+        x[s][j] = __builtin_bit_cast(float, (bits & keep) | (0xFF800000u & ~keep));
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ void clear_counts(uint32_t *count) {  // a wavefront's own group
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < kGroup / 256; ++i) reinterpret_cast<words4 *>(count)[i * 64 + lane] = words4{};
+}
+
+// A workgroup takes a group of one row for each of its wavefronts; the logits
+// are on their way while it counts the row's history.
 template <typename T>
 __global__ __launch_bounds__(64 * kGroupWaves) void penalise_kernel(
     const typename T::store *logits, int64_t ld, typename T::store *out, int64_t ldo, int64_t V,
     Rules rules, uint32_t slices, int64_t tiles) {
   extern __shared__ uint32_t lds[];
+  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  uint32_t *count = lds + wave * kGroup;
   for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const int64_t b = tile / slices;
-    const int64_t first = (tile - b * slices) * (blockDim.x >> 6) * kGroup +
-                          (int64_t)(threadIdx.x >> 6) * kGroup;
+    const int64_t b = tile / slices, start = (tile - b * slices) * waves * kGroup;
+    const int64_t first = start + wave * kGroup;
+    const RowRules r = row_rules(rules, b);
+    const History h = row_history(rules, b);
+    Group<T> g;
+    load_group<T>(logits + b * ld, first, V, r, g);
+    if (h.size) {
+      clear_counts(count);
+      __syncthreads();
+      count_history(h, (uint32_t)start, waves * kGroup, lds);
+      __syncthreads();
+    }
     float x[kSteps][8];
-    int n[kSteps];
-    group_logits<T>(logits + b * ld, first, V, row_history(rules, b), row_rules(rules, b), lds, x, n);
+    rule_group<T>(g, first, h.size ? count : nullptr, r, x);
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
-      store_elements<T, 8>(out + b * ldo + first + s * 512 + (threadIdx.x & 63) * 8, n[s], x[s]);
+      store_elements<T, 8>(out + b * ldo + first + s * 512 + (threadIdx.x & 63) * 8, g.n[s], x[s]);
     __syncthreads();
   }
 }
@@ -216,9 +253,9 @@ struct GroupSum {
 
 struct DrawRow {
   float temperature;
-  float inverse;  // 1 / temperature
-  float floor;    // log(min_p); -inf: none
-  bool greedy;    // the row takes its largest logit
+  float scale;  // log2(e) / temperature
+  float floor;  // log2(min_p); -inf: none
+  bool greedy;  // the row takes its largest logit
 };
 
 __device__ __forceinline__ DrawRow draw_row(const float *temperature, const float *min_p,
@@ -227,81 +264,65 @@ __device__ __forceinline__ DrawRow draw_row(const float *temperature, const floa
   // an infinite temperature would make -inf * 0 of the logits that may not be drawn
   const float t = fminf(given, 1e30f);
   const float p = min_p ? min_p[b] : 0.0f;
-  return DrawRow{t, 1.0f / t, p > 0.0f ? logf(fminf(p, 1.0f)) : -INFINITY, !(given > 0.0f)};
+  return DrawRow{t, fminf(1.44269504f / t, 3e38f),
+                 p > 0.0f ? log2f(fminf(p, 1.0f)) : -INFINITY, !(given > 0.0f)};
 }
 
 // exp((x - top) / temperature), 1 at the top itself whatever it is
-__device__ __forceinline__ float weight(float x, float top, float inverse) {
-  return x == top ? 1.0f : expf((x - top) * inverse);
+__device__ __forceinline__ float weight(float x, float top, const DrawRow &d) {
+  return x == top ? 1.0f : __builtin_amdgcn_exp2f((x - top) * d.scale);
 }
 
 __device__ __forceinline__ bool above_floor(float x, float top, const DrawRow &d) {
-  return x == top || (x - top) * d.inverse >= d.floor;
+  return x == top || (x - top) * d.scale >= d.floor;
+}
+
+// Reductions over a wavefront by data-parallel moves (rows of 16 lanes, then
+// across rows), which take a quarter of the time of exchanges through LDS; the
+// result is in every lane.
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t other, uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)other, (int)x, CONTROL, ROWS, 0xF, false);
+}
+
+template <typename F>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t x, uint32_t identity, F f) {
+  x = f(x, moved<0x111, 0xF>(identity, x));  // from 1, 2, 4 and 8 lanes below in the row
+  x = f(x, moved<0x112, 0xF>(identity, x));
+  x = f(x, moved<0x114, 0xF>(identity, x));
+  x = f(x, moved<0x118, 0xF>(identity, x));
+  x = f(x, moved<0x142, 0xA>(identity, x));  // a row's last lane to the next row
+  x = f(x, moved<0x143, 0xC>(identity, x));  // lane 31 to the upper half
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+  const auto f = [](uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
+  };
+  return __builtin_bit_cast(float, wave_reduce(__builtin_bit_cast(uint32_t, v), 0xFF800000u, f));
 }
 
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+  const auto f = [](uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b));
+  };
+  return __builtin_bit_cast(float, wave_reduce(__builtin_bit_cast(uint32_t, v), 0u, f));
 }
 
-// The groups' largest logits and sums of weights; NaN counts as -inf.  FLOOR:
-// the groups' largest are known, and the sums of the rows with a floor are made
-// again over what is above it.
-template <typename T, bool FLOOR>
-__global__ __launch_bounds__(64 * kGroupWaves) void group_kernel(
-    const typename T::store *__restrict__ logits, int64_t ld, int64_t V, Rules rules,
-    const float *temperature, const float *min_p, GroupSum *groups, uint32_t per_row,
-    uint32_t slices, int64_t tiles) {
-  extern __shared__ uint32_t lds[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const int64_t b = tile / slices;
-    const uint32_t g0 = (uint32_t)(tile - b * slices) * waves, g = g0 + wave;
-    const DrawRow d = draw_row(temperature, min_p, b);
-    GroupSum *mine = groups + b * per_row;
-    float top = -INFINITY;
-    if (FLOOR) {
-      if (d.greedy || d.floor == -INFINITY) continue;
-      for (uint32_t i = lane; i < per_row; i += 64) top = fmaxf(top, mine[i].top);
-      top = wave_max(top);
-      bool any = false;  // a group of the workgroup's that reaches the floor
-      for (int w = 0; w < waves && g0 + w < per_row; ++w) any |= above_floor(mine[g0 + w].top, top, d);
-      if (!any) {
-        if (lane == 0 && g < per_row) mine[g].sum = 0.0f;
-        continue;
-      }
-    }
-    float x[kSteps][8];
-    int n[kSteps];
-    group_logits<T>(logits + b * ld, (int64_t)g * kGroup, V, row_history(rules, b),
-                    row_rules(rules, b), lds, x, n);
-    float m = -INFINITY, sum = 0.0f;
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        x[s][j] = j < n[s] && x[s][j] == x[s][j] ? x[s][j] : -INFINITY;
-        m = fmaxf(m, x[s][j]);
-      }
-    m = wave_max(m);
-    if (m != -INFINITY) {
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (!FLOOR || above_floor(x[s][j], top, d)) sum += weight(x[s][j], m, d.inverse);
-      sum = wave_sum(sum);
-    }
-    if (lane == 0 && g < per_row) mine[g] = GroupSum{m, sum};
-    __syncthreads();
-  }
+__device__ __forceinline__ uint32_t wave_min(uint32_t v) {
+  return wave_reduce(v, 0xFFFFFFFFu, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+}
+
+// The smallest value of a wavefront (not negative, not NaN: their bits are in
+// their order) and the lowest index that has it.
+struct First {
+  uint32_t value, index;
+};
+
+__device__ __forceinline__ First wave_first(First mine) {
+  const uint32_t v = wave_min(mine.value);
+  return First{v, wave_min(mine.value == v ? mine.index : 0xFFFFFFFFu)};
 }
 
 // -log(1 - u), u = (y + 1/2) / 2^32 with y the first word of the counter
@@ -313,93 +334,159 @@ __device__ __forceinline__ float variate(uint32_t i, uint32_t position, uint32_t
   return -log1pf(-u);
 }
 
-// smallest (value, index) of the workgroup; values are not negative and not NaN
-__device__ __forceinline__ uint64_t block_first(float value, uint32_t index, uint64_t *waves) {
-  uint64_t k = (uint64_t)__builtin_bit_cast(uint32_t, value) << 32 | index;
+// The largest logit of a wavefront's group (NaN, and what does not exist: -inf)
+// and the sum of its weights to that, over what lies above the floor under
+// `row_top` where FLOOR.
+template <bool FLOOR>
+__device__ __forceinline__ GroupSum group_sum(float (&x)[kSteps][8], const int (&n)[kSteps],
+                                              bool full, float row_top, const DrawRow &d) {
+  float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-  for (int d = 32; d; d >>= 1) {
-    const uint64_t o = __shfl_xor((unsigned long long)k, d);
-    k = o < k ? o : k;
+  for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (!full) x[s][j] = j < n[s] ? x[s][j] : -INFINITY;
+      x[s][j] = fmaxf(x[s][j], -INFINITY);  // (the maximum of NaN and a number is the number)
+      top = fmaxf(top, x[s][j]);
+    }
+  top = wave_max(top);
+  if (top == -INFINITY || (d.greedy && !FLOOR)) return GroupSum{top, 0.0f};
+  if (FLOOR) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        x[s][j] = above_floor(x[s][j], row_top, d) ? x[s][j] : -INFINITY;
   }
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = k;
-  __syncthreads();
+  if (top == INFINITY) {  // shared by the logits of +inf
 #pragma unroll
-  for (int w = 0; w < kDrawWaves; ++w) k = waves[w] < k ? waves[w] : k;
-  __syncthreads();
-  return k;
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += x[s][j] == top ? 1.0f : 0.0f;
+  } else {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += __builtin_amdgcn_exp2f((x[s][j] - top) * d.scale);
+  }
+  return GroupSum{top, wave_sum(sum)};
 }
 
-// One workgroup per row: the group, then the token in it, one to a thread.
+// The groups' largest logits and sums of weights, a group to a wavefront.
+// FLOOR: the groups' largest are known, and the sums of the rows with a floor
+// are made again over what is above it.
+template <typename T, bool FLOOR>
+__global__ __launch_bounds__(64 * kGroupWaves) void group_kernel(
+    const typename T::store *__restrict__ logits, int64_t ld, int64_t V, Rules rules,
+    const float *temperature, const float *min_p, GroupSum *groups, uint32_t per_row,
+    uint32_t slices, int64_t tiles) {
+  extern __shared__ uint32_t lds[];
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t *count = lds + wave * kGroup;
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int64_t b = tile / slices;
+    const uint32_t g0 = (uint32_t)(tile - b * slices) * waves, g = g0 + wave;
+    const DrawRow d = draw_row(temperature, min_p, b);
+    GroupSum *mine = groups + b * per_row;
+    float top = -INFINITY;
+    if (FLOOR) {
+      if (d.greedy || d.floor == -INFINITY) continue;
+      for (uint32_t i = lane; i < per_row; i += 64) top = fmaxf(top, mine[i].top);
+      top = wave_max(top);
+      // whether a group of the workgroup's reaches the floor
+      const bool reaches =
+          lane < waves && g0 + lane < per_row && above_floor(mine[g0 + lane].top, top, d);
+      if (!__ballot(reaches)) {
+        if (lane == 0 && g < per_row) mine[g].sum = 0.0f;
+        continue;
+      }
+    }
+    const int64_t first = (int64_t)g * kGroup;
+    const RowRules r = row_rules(rules, b);
+    const History h = row_history(rules, b);
+    Group<T> q;
+    load_group<T>(logits + b * ld, first, V, r, q);
+    if (h.size) {
+      clear_counts(count);
+      __syncthreads();
+      count_history(h, g0 * kGroup, waves * kGroup, lds);
+      __syncthreads();
+    }
+    float x[kSteps][8];
+    rule_group<T>(q, first, h.size ? count : nullptr, r, x);
+    const GroupSum sum = group_sum<FLOOR>(x, q.n, first + kGroup <= V, top, d);
+    if (lane == 0 && g < per_row) mine[g] = sum;
+    __syncthreads();
+  }
+}
+
+// One workgroup per row: the groups' race (by every wavefront for itself), then
+// the race of the group's tokens, one to a thread.
 template <typename T>
 __global__ __launch_bounds__(kDrawThreads) void draw_kernel(
     const typename T::store *__restrict__ logits, int64_t ld, int64_t B, int64_t V, Rules rules,
-    const float *temperature, const float *min_p, const int64_t *__restrict__ seed,
-    const int32_t *__restrict__ position, const GroupSum *__restrict__ groups, uint32_t per_row,
-    int32_t *z, float *prob) {
+    const float *__restrict__ temperature, const float *__restrict__ min_p,
+    const int64_t *__restrict__ seed, const int32_t *__restrict__ position,
+    const GroupSum *__restrict__ groups, uint32_t per_row, int32_t *__restrict__ z,
+    float *__restrict__ prob) {
   __shared__ uint32_t count[kGroup];
-  __shared__ uint64_t firsts[kDrawWaves];
-  __shared__ float parts[2][kDrawWaves];
+  __shared__ First firsts[kDrawWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
     const DrawRow d = draw_row(temperature, min_p, b);
     const GroupSum *mine = groups + b * per_row;
     const uint64_t s = (uint64_t)seed[b];
     const uint32_t pos = (uint32_t)position[b];
+    const RowRules r = row_rules(rules, b);
     const History h = row_history(rules, b);
     // the first tokens of the history, on their way before the group is known
     const words4 tokens = history_load(h, 4 * threadIdx.x);
     count[threadIdx.x] = 0;
     float top = -INFINITY;
-    for (uint32_t g = threadIdx.x; g < per_row; g += kDrawThreads) top = fmaxf(top, mine[g].top);
+    for (uint32_t g = lane; g < per_row; g += 64) top = fmaxf(top, mine[g].top);
     top = wave_max(top);
-    if (lane == 0) parts[0][wave] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kDrawWaves; ++w) top = fmaxf(top, parts[0][w]);
     if (top == -INFINITY) {  // nothing may be drawn
       if (threadIdx.x == 0) {
         z[b] = -1;
         prob[b] = 0.0f;
       }
-      __syncthreads();
       continue;
     }
-    float best = INFINITY, total = 0.0f;
-    uint32_t at = 0xFFFFFFFFu;
-    for (uint32_t g = threadIdx.x; g < per_row; g += kDrawThreads) {
+    First best{0x7F800000u, 0xFFFFFFFFu};
+    float total = 0.0f;
+    for (uint32_t g = lane; g < per_row; g += 64) {
       const GroupSum q = mine[g];
       float v;
       if (d.greedy) {
         v = q.top == top ? 0.0f : INFINITY;
       } else {
-        const float w = q.top == -INFINITY ? 0.0f : weight(q.top, top, d.inverse) * q.sum;
+        const float w = q.top == -INFINITY ? 0.0f : weight(q.top, top, d) * q.sum;
         total += w;
         v = variate(g, pos, 2u, s) / w;
       }
-      if (v < best || at == 0xFFFFFFFFu) {
-        best = v;
-        at = g;
-      }
+      const uint32_t bits = __builtin_bit_cast(uint32_t, v);
+      if (bits < best.value || best.index == 0xFFFFFFFFu) best = First{bits, g};
     }
     total = wave_sum(total);
-    if (lane == 0) parts[1][wave] = total;
-    const uint32_t group = (uint32_t)block_first(best, at, firsts);
-    total = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kDrawWaves; ++w) total += parts[1][w];
-    const int64_t first = (int64_t)group * kGroup, token = first + threadIdx.x;
+    const uint32_t group = wave_first(best).index;
+    const uint32_t first = group * kGroup;
+    const int64_t token = (int64_t)first + threadIdx.x;
     const float group_top = mine[group].top;
-    const RowRules r = row_rules(rules, b);
     const bool there = token < V;
     float x = there ? T::up(logits[b * ld + token]) : -INFINITY;
     const float bias = there && r.bias ? r.bias[token] : 0.0f;
     const uint32_t allowed = there && r.mask ? r.mask[token >> 5] : 0xFFFFFFFFu;
+    // a token's own variate, on its way with its logit
+    const float own = d.greedy ? 0.0f : variate((uint32_t)token, pos, 3u, s);
     if (h.size) {
+      __syncthreads();
       history_count(h, 4 * threadIdx.x, tokens, first, kGroup, count);
       for (int64_t i = 4 * (threadIdx.x + kDrawThreads); i < h.size; i += 4 * kDrawThreads)
         history_count(h, i, history_load(h, i), first, kGroup, count);
       __syncthreads();
-      x = ruled(x, count[threadIdx.x], r);
+      const uint32_t c = count[threadIdx.x];
+      if (c) x = r.tame ? ruled<true>(x, c, r) : ruled<false>(x, c, r);
     }
     if (r.bias) x += bias;
     if (!(allowed >> (token & 31) & 1)) x = -INFINITY;
@@ -407,12 +494,20 @@ __global__ __launch_bounds__(kDrawThreads) void draw_kernel(
     if (d.greedy)
       v = x == top ? 0.0f : INFINITY;
     else if (x == x && x != -INFINITY && above_floor(x, top, d))
-      v = variate((uint32_t)token, pos, 3u, s) / weight(x, group_top, d.inverse);
-    const uint32_t won = (uint32_t)block_first(v, threadIdx.x, firsts);
-    if (threadIdx.x == won) {
+      v = own / weight(x, group_top, d);
+    const First of_wave = wave_first(First{__builtin_bit_cast(uint32_t, v), threadIdx.x});
+    if (lane == 0) firsts[wave] = of_wave;
+    __syncthreads();
+    const First won = wave_first(lane < kDrawWaves ? firsts[lane] : First{0xFFFFFFFFu, 0xFFFFFFFFu});
+    if (threadIdx.x == won.index) {
       z[b] = (int32_t)token;
-      const double share = x == top ? 1.0 : exp(((double)x - (double)top) / (double)d.temperature);
-      prob[b] = d.greedy ? 1.0f : (float)(share / (double)total);
+      // the exponent in 64 bits: in 32 its rounding would be the largest error
+      const double y = ((double)x - (double)top) / (double)d.temperature * 1.4426950408889634;
+      const double whole = rint(y);
+      const float share =
+          x == top ? 1.0f
+                   : ldexpf(__builtin_amdgcn_exp2f((float)(y - whole)), (int)fmax(whole, -1000.0));
+      prob[b] = d.greedy ? 1.0f : share / total;
     }
     __syncthreads();
   }
