@@ -28,7 +28,7 @@ namespace lda {
 
 constexpr int kGroup = 1024;  // tokens of a group, the unit of a wavefront
 constexpr int kSteps = kGroup / 512;
-constexpr int kGroupWaves = 8;      // groups of a workgroup that applies the rules, at most
+constexpr int kGroupWaves = 8;      // groups of a workgroup, at most
 constexpr int kDrawThreads = 1024;  // of a workgroup that draws: one for each token of a group
 constexpr int kDrawWaves = kDrawThreads / 64;
 constexpr uint32_t kSeen = 0x80000000u;
@@ -42,22 +42,18 @@ struct Rules {
   int64_t ld_bias;
   const uint32_t *mask;  // [B][ld_mask] or null; ld_mask 0: one row
   int64_t ld_mask;
-  int64_t capacity;  // history's columns
+  int32_t capacity;  // history's columns
 };
 
 struct RowRules {
-  float repetition, inverse, frequency, presence;  // inverse: 1 / repetition
-  bool tame;  // repetition within 2^-30 .. 2^30
+  float repetition, frequency, presence;
   const float *bias;
   const uint32_t *mask;
 };
 
 __device__ __forceinline__ RowRules row_rules(const Rules &r, int64_t b) {
-  const float repetition = r.repetition ? r.repetition[b] : 1.0f;
-  return RowRules{repetition, 1.0f / repetition, r.frequency ? r.frequency[b] : 0.0f,
-                  r.presence ? r.presence[b] : 0.0f,
-                  repetition > 0x1p-30f && repetition < 0x1p+30f,
-                  r.bias ? r.bias + b * r.ld_bias : nullptr,
+  return RowRules{r.repetition ? r.repetition[b] : 1.0f, r.frequency ? r.frequency[b] : 0.0f,
+                  r.presence ? r.presence[b] : 0.0f, r.bias ? r.bias + b * r.ld_bias : nullptr,
                   r.mask ? r.mask + b * r.ld_mask : nullptr};
 }
 
@@ -68,44 +64,41 @@ __device__ __forceinline__ float rounded(float x) {
   return x;
 }
 
-// x / r, rounded as the division is: with y = 1 / r rounded, q = x y and
-// q + (x - q r) y, both sums fused (an infinite q stays).  Where r is extreme
-// enough for bits to be lost on the way, the division itself.
-__device__ __forceinline__ float divided(float x, const RowRules &r) {
-  const float q = x * r.inverse, refined = fmaf(fmaf(-q, r.repetition, x), r.inverse, q);
-  return fabsf(q) < INFINITY ? refined : q;
-}
-
-// A logit with a use in the history.  EXACT: repetition within 2^-30 .. 2^30.
-template <bool EXACT>
 __device__ __forceinline__ float ruled(float x, uint32_t count, const RowRules &r) {
-  const float over = EXACT ? divided(x, r) : x / r.repetition;
-  x = x > 0.0f ? over : rounded(x * r.repetition);
+  x = x > 0.0f ? x / r.repetition : rounded(x * r.repetition);
   const uint32_t c = count & ~kSeen;
   x -= rounded(r.frequency * (float)c);
   return x - (c ? r.presence : 0.0f);
 }
 
-// A row's history, four tokens to a lane and load.
+// Where the count of a group's token lies: a lane's two blocks of four tokens
+// are 256 words apart, so that 64 lanes read 16 bytes each from neighbouring
+// banks.
+__device__ __forceinline__ uint32_t count_slot(uint32_t at) {
+  return (at & ~511u) | (at & 4) << 6 | (at >> 1 & 252) | (at & 3);
+}
+
+// A row's history; the first `prompt` of its tokens are not generated.
 struct History {
   const int32_t *tokens;
-  int64_t size, prompt;  // 0 tokens where there is no history
+  int32_t size, prompt;  // 0 tokens where there is no history
 };
 
 __device__ __forceinline__ History row_history(const Rules &r, int64_t b) {
   if (!r.history) return History{nullptr, 0, 0};
-  int64_t n = r.lengths[b];
-  n = n < r.capacity ? n : r.capacity;
+  const int32_t n = r.lengths[b] < r.capacity ? r.lengths[b] : r.capacity;
   return History{r.history + b * r.ld_history, n > 0 ? n : 0, r.prompt ? r.prompt[b] : 0};
 }
 
-__device__ __forceinline__ words4 history_load(const History &h, int64_t i) {
+// Four tokens from number i on; those past the end are -1.
+__device__ __forceinline__ words4 history_load(const History &h, uint32_t i) {
   words4 t;
-  if (i + 4 <= h.size) {
+  if (i + 4 <= (uint32_t)h.size) {
     t = *reinterpret_cast<const words4_any *>(h.tokens + i);
   } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) t[j] = i + j < h.size ? (uint32_t)h.tokens[i + j] : 0xFFFFFFFFu;
+    for (uint32_t j = 0; j < 4; ++j)
+      t[j] = i + j < (uint32_t)h.size ? (uint32_t)h.tokens[i + j] : 0xFFFFFFFFu;
   }
   return t;
 }
@@ -114,18 +107,17 @@ __device__ __forceinline__ words4 history_load(const History &h, int64_t i) {
 // size) to `count`: generated tokens in the low bits, kSeen for the prompt's.
 // (As an unsigned number a negative token lies past every vocabulary: where the
 // difference wraps into the range, it is to a place past the row's end.)
-__device__ __forceinline__ void history_count(const History &h, int64_t i, words4 t, uint32_t first,
-                                              uint32_t size, uint32_t *count) {
-  const int64_t left = h.prompt - i;
-  const int prompt = left > 4 ? 4 : left < 0 ? 0 : (int)left;
+__device__ __forceinline__ void history_count(const History &h, uint32_t i, words4 t,
+                                              uint32_t first, uint32_t size, uint32_t *count) {
+  const int32_t prompt = h.prompt - (int32_t)i;  // (i is below 2^31)
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const uint32_t at = t[j] - first;
     if (at >= size) continue;
     if (j < prompt)
-      atomicOr(&count[at], kSeen);
+      atomicOr(&count[count_slot(at)], kSeen);
     else
-      atomicAdd(&count[at], 1u);
+      atomicAdd(&count[count_slot(at)], 1u);
   }
 }
 
@@ -133,8 +125,8 @@ __device__ __forceinline__ void history_count(const History &h, int64_t i, words
 // LDS (which the caller has cleared and synchronised) by the whole workgroup.
 __device__ __forceinline__ void count_history(const History &h, uint32_t first, uint32_t size,
                                               uint32_t *count) {
-  const int64_t step = 4 * (int64_t)blockDim.x;
-  for (int64_t i = 4 * (int64_t)threadIdx.x; i < h.size; i += 2 * step) {
+  const uint32_t step = 4 * blockDim.x;
+  for (uint32_t i = 4 * threadIdx.x; i < (uint32_t)h.size; i += 2 * step) {
     const words4 a = history_load(h, i), b = history_load(h, i + step);
     history_count(h, i, a, first, size, count);
     history_count(h, i + step, b, first, size, count);
@@ -153,50 +145,52 @@ struct Group {
 template <typename T>
 __device__ __forceinline__ void load_group(const typename T::store *row, int64_t first, int64_t V,
                                            const RowRules &r, Group<T> &g) {
-  const int lane = threadIdx.x & 63;
+  // (row and first are the same for the wavefront: 32-bit offsets from there)
+  const int64_t rest = V - first;
+  const int32_t left = rest < 0 ? 0 : rest < kGroup ? (int32_t)rest : kGroup;
+  const typename T::store *x = row + first;
+  const uint32_t *mask = r.mask + (first >> 5);
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
-    const int64_t v = first + s * 512 + lane * 8, left = V - v;
-    g.n[s] = left < 8 ? (left > 0 ? (int)left : 0) : 8;
-    g.x[s] = load_packed<T, 8>(row + v, g.n[s]);
-    g.allowed[s] = r.mask && g.n[s] > 0 ? r.mask[v >> 5] >> (v & 31) : 0xFFu;
+    const uint32_t at = s * 512 + (threadIdx.x & 63) * 8;
+    const int32_t n = left - (int32_t)at;
+    g.n[s] = n < 0 ? 0 : n < 8 ? n : 8;
+    g.x[s] = load_packed<T, 8>(x + at, g.n[s]);
+    g.allowed[s] = r.mask && g.n[s] > 0 ? mask[at >> 5] >> (at & 31) : 0xFFu;
   }
 }
 
 // The group's logits in float under the rules.  `count`: the uses of the group's
 // tokens in LDS, or null.
 template <typename T>
-__device__ __forceinline__ void rule_group(const Group<T> &g, int64_t first, const uint32_t *count,
-                                           const RowRules &r, float (&x)[kSteps][8]) {
+__device__ __forceinline__ void rule_group(const Group<T> &g, int64_t first, const uint32_t *count, const RowRules &r,
+                                           float (&x)[kSteps][8]) {
   const int lane = threadIdx.x & 63;
-  float bias[kSteps][8];
-  if (r.bias) {
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-      load_elements<F32, 8>(r.bias + first + s * 512 + lane * 8, g.n[s], bias[s]);
-  }
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
+    float bias[8];
+    if (r.bias) load_elements<F32, 8>(r.bias + first + (uint32_t)(s * 512 + lane * 8), g.n[s], bias);
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[s][j] = T::up(g.x[s].v[j]);
     if (count) {
+      const words4 *mine = reinterpret_cast<const words4 *>(count + s * 512) + lane;
+      const words4 low = mine[0], high = mine[64];
       uint32_t c[8], any = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        c[j] = count[s * 512 + lane * 8 + j];
+        c[j] = j < 4 ? low[j & 3] : high[j & 3];
         any |= c[j];
       }
-      if (any && r.tame) {
+      if (any) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[s][j] = c[j] ? ruled<true>(x[s][j], c[j], r) : x[s][j];
-      } else if (any) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[s][j] = c[j] ? ruled<false>(x[s][j], c[j], r) : x[s][j];
+        for (int j = 0; j < 8; ++j) {
+          if (c[j]) x[s][j] = ruled(x[s][j], c[j], r);
+        }
       }
     }
     if (r.bias) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[s][j] += bias[s][j];
+      for (int j = 0; j < 8; ++j) x[s][j] += bias[j];
     }
     if (r.mask) {
 #pragma unroll
@@ -210,10 +204,11 @@ __device__ __forceinline__ void rule_group(const Group<T> &g, int64_t first, con
   }
 }
 
-__device__ __forceinline__ void clear_counts(uint32_t *count) {  // a wavefront's own group
+// a wavefront's own group
+__device__ __forceinline__ void clear_counts(uint32_t *count) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int i = 0; i < kGroup / 256; ++i) reinterpret_cast<words4 *>(count)[i * 64 + lane] = words4{};
+  for (int i = 0; i < 2 * kSteps; ++i) reinterpret_cast<words4 *>(count)[i * 64 + lane] = words4{};
 }
 
 // A workgroup takes a group of one row for each of its wavefronts; the logits
@@ -223,7 +218,7 @@ __global__ __launch_bounds__(64 * kGroupWaves) void penalise_kernel(
     const typename T::store *logits, int64_t ld, typename T::store *out, int64_t ldo, int64_t V,
     Rules rules, uint32_t slices, int64_t tiles) {
   extern __shared__ uint32_t lds[];
-  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   uint32_t *count = lds + wave * kGroup;
   for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const int64_t b = tile / slices, start = (tile - b * slices) * waves * kGroup;
@@ -242,7 +237,8 @@ __global__ __launch_bounds__(64 * kGroupWaves) void penalise_kernel(
     rule_group<T>(g, first, h.size ? count : nullptr, r, x);
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
-      store_elements<T, 8>(out + b * ldo + first + s * 512 + (threadIdx.x & 63) * 8, g.n[s], x[s]);
+      store_elements<T, 8>(out + b * ldo + first + (uint32_t)(s * 512 + (threadIdx.x & 63) * 8),
+                           g.n[s], x[s]);
     __syncthreads();
   }
 }
@@ -440,8 +436,8 @@ __global__ __launch_bounds__(kDrawThreads) void draw_kernel(
     const uint32_t pos = (uint32_t)position[b];
     const RowRules r = row_rules(rules, b);
     const History h = row_history(rules, b);
-    // the first tokens of the history, on their way before the group is known
-    const words4 tokens = history_load(h, 4 * threadIdx.x);
+    // the first of the history's tokens, on their way before the group is known
+    const words4 ahead = history_load(h, 4 * threadIdx.x);
     count[threadIdx.x] = 0;
     float top = -INFINITY;
     for (uint32_t g = lane; g < per_row; g += 64) top = fmaxf(top, mine[g].top);
@@ -481,12 +477,12 @@ __global__ __launch_bounds__(kDrawThreads) void draw_kernel(
     const float own = d.greedy ? 0.0f : variate((uint32_t)token, pos, 3u, s);
     if (h.size) {
       __syncthreads();
-      history_count(h, 4 * threadIdx.x, tokens, first, kGroup, count);
-      for (int64_t i = 4 * (threadIdx.x + kDrawThreads); i < h.size; i += 4 * kDrawThreads)
+      history_count(h, 4 * threadIdx.x, ahead, first, kGroup, count);
+      for (uint32_t i = 4 * (threadIdx.x + kDrawThreads); i < (uint32_t)h.size; i += 4 * kDrawThreads)
         history_count(h, i, history_load(h, i), first, kGroup, count);
       __syncthreads();
-      const uint32_t c = count[threadIdx.x];
-      if (c) x = r.tame ? ruled<true>(x, c, r) : ruled<false>(x, c, r);
+      const uint32_t c = count[count_slot(threadIdx.x)];
+      if (c) x = ruled(x, c, r);
     }
     if (r.bias) x += bias;
     if (!(allowed >> (token & 31) & 1)) x = -INFINITY;
