@@ -8,17 +8,19 @@ call allocates belong to the stream it runs on.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
+import functools
 
 import torch
 
 from . import _lib
-from ._lib import _handle, _require
+from ._lib import _require
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # LDA_F32, LDA_BF16, LDA_F16
-_I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
+_I32, _I64, _F32, _U8 = torch.int32, torch.int64, torch.float32, torch.uint8
 _U64, _U32 = 2 ** 64 - 1, 2 ** 32 - 1
+_Tensor = torch.Tensor
+_current_device = _lib._current_device or torch.cuda.current_device
 
 
 class LogitRules(ctypes.Structure):
@@ -51,37 +53,74 @@ def bind(lib: ctypes.CDLL) -> None:
     lib.lda_draw_logits_workspace_bytes.restype = SZ
 
 
-def _ld(t: torch.Tensor) -> int:
-    """Elements from row to row (the width where there is one row or none)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+# The checks below read each attribute once and in the order in which a call whose
+# arguments are all as they should be passes soonest: a small call takes as long
+# on the host as on the GPU.  What fails goes on to the checks that say why.
 
 
-def _rows(t, name: str, dev=None, dtype=None, shape=None, out: bool = False) -> None:
-    """A matrix whose rows are contiguous, of a supported type, on ``dev``."""
-    if not isinstance(t, torch.Tensor):
+def _entry(fn):
+    """``fn`` in the context of its first tensor's device, and of the stream the
+    call is given: what it allocates and launches belongs to that stream."""
+    @functools.wraps(fn)
+    def call(first, *args, stream=None, **kw):
+        if type(first) is _Tensor and stream is None:
+            dev = first.get_device()
+            if dev >= 0 and dev == _current_device():
+                return fn(first, *args, **kw)
+        if not isinstance(first, _Tensor):
+            raise TypeError("the first argument must be a torch.Tensor")
+        if not first.is_cuda:
+            raise ValueError("the first argument must be on the GPU")
+        with torch.cuda.stream(stream) if stream is not None else torch.cuda.device(first.device):
+            return fn(first, *args, **kw)
+    return call
+
+
+def _run(name: str, dev: int, *args) -> None:
+    """One call of the library on the current stream of device ``dev``."""
+    raw = _lib._raw_stream
+    handle = raw(dev) if raw is not None else torch.cuda.current_stream(dev).cuda_stream
+    st = getattr(_lib._lib or _lib.load(), name)(*args, handle)
+    if st != 0:
+        _lib._check(st)
+
+
+def _rows(t, name: str, dev: int, dtype=None, shape=None, out: bool = False) -> tuple[int, int, int]:
+    """(rows, width, elements from row to row) of a matrix whose rows are
+    contiguous, of type ``dtype`` (None: a supported one), on device ``dev``."""
+    if isinstance(t, _Tensor) and t.dim() == 2 and t.get_device() == dev and (
+            t.dtype is dtype or (dtype is None and t.dtype in DTYPES)):
+        n, width = t.shape
+        apart, one = t.stride()
+        if n <= 1:
+            apart = width
+        if ((one == 1 or width <= 1) and (shape is None or shape == (n, width))
+                and (not out or apart >= width)):
+            return n, width, apart
+    if not isinstance(t, _Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be on the GPU")
-    if dev is not None and t.device != dev:
+    if t.get_device() != dev:
         raise ValueError("all tensors must be on one device")
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if dtype is None and t.dtype not in DTYPES:
-        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    if t.dtype != dtype if dtype is not None else t.dtype not in DTYPES:
+        raise TypeError(f"{name} must be {dtype or 'float32, bfloat16 or float16'}, got {t.dtype}")
     if t.dim() != 2:
         raise ValueError(f"{name} must have 2 dimensions")
     if shape is not None and tuple(t.shape) != shape:
         raise ValueError(f"{name} must have the shape {shape}, got {tuple(t.shape)}")
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must have contiguous rows")
-    if out and t.shape[0] > 1 and t.stride(0) < t.shape[1]:
-        raise ValueError(f"{name}'s rows overlap")
+    raise ValueError(f"{name}'s rows overlap")
 
 
-def _vector(t, name: str, dtype, n: int, dev) -> None:
-    _require(t, name, dtype, 1)
-    if t.shape[0] != n or t.device != dev:
+def _vector(t, name: str, dtype, n: int, dev: int) -> int:
+    """The address of a dense vector of ``n`` entries on device ``dev``."""
+    if not (isinstance(t, _Tensor) and t.dtype is dtype and t.dim() == 1 and t.numel() == n
+            and t.get_device() == dev and t.is_contiguous()):
+        _require(t, name, dtype, 1)
         raise ValueError(f"{name} must hold {n} entries on the tensors' device")
+    return t.data_ptr()
 
 
 def _probability(p) -> float:
@@ -91,198 +130,176 @@ def _probability(p) -> float:
     return p
 
 
-def _on(dev, stream):
-    """The context in which a call allocates and launches: its device, and the
-    stream it was given (so that what it allocates belongs to that stream)."""
-    if stream is not None:
-        return torch.cuda.stream(stream)
-    if dev.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(dev)
-
-
-def _run(name: str, dev, stream, *args) -> None:
-    st = getattr(_lib.load(), name)(*args, _handle(stream, dev.index))
-    if st != 0:
-        _lib._check(st)
-
-
+@_entry
 def embed(table, word_id, scale: float = 1.0, p: float = 0.0, seed: int = 0, step: int = 0,
-          out=None, stream=None) -> torch.Tensor:
+          out=None) -> torch.Tensor:
     """out[n] = table[word_id[n]] * scale, dropped out with probability ``p``
     (lda_embed).  table [V][D] float32, bfloat16 or float16; word_id int32 [N];
-    out [N][D] of the table's type.  A word outside [0, V) gives a row of zeros."""
-    _rows(table, "table")
-    dev = table.device
-    _require(word_id, "word_id", _I32, 1)
-    if word_id.device != dev:
-        raise ValueError("all tensors must be on one device")
-    (V, D), N = table.shape, word_id.shape[0]
-    p = _probability(p)
-    with _on(dev, stream):
-        if out is None:
-            out = torch.empty((N, D), dtype=table.dtype, device=dev)
-        else:
-            _rows(out, "out", dev, table.dtype, (N, D), out=True)
-        _run("lda_embed", dev, stream, table.data_ptr(), _ld(table), word_id.data_ptr(),
-             out.data_ptr(), _ld(out), N, V, D, DTYPES[table.dtype], float(scale), p,
-             int(seed) & _U64, int(step) & _U32)
+    out [N][D] of the table's type.  A word outside [0, V) gives a row of zeros.
+    ``stream``: where it runs (None: the current stream)."""
+    dev = table.get_device()
+    V, D, ld = _rows(table, "table", dev)
+    N = word_id.numel() if isinstance(word_id, _Tensor) else -1
+    ids = _vector(word_id, "word_id", _I32, N, dev)
+    dtype = table.dtype
+    if out is None:
+        out, ldo = table.new_empty((N, D)), D
+    else:
+        ldo = _rows(out, "out", dev, dtype, (N, D), True)[2]
+    _run("lda_embed", dev, table.data_ptr(), ld, ids, out.data_ptr(), ldo, N, V, D, DTYPES[dtype],
+         scale, _probability(p), int(seed) & _U64, int(step) & _U32)
     return out
 
 
+@functools.lru_cache(maxsize=256)
 def embed_grad_workspace_bytes(N: int, V: int, D: int) -> int:
     """Bytes of device workspace ``embed_grad`` needs (0: none, or unsupported)."""
     return int(_lib.load().lda_embed_grad_workspace_bytes(int(N), int(V), int(D)))
 
 
+@_entry
 def embed_grad(grad, word_id, V: int, scale: float = 1.0, p: float = 0.0, seed: int = 0,
-               step: int = 0, out=None, accumulate: bool = False, dtype=None, workspace=None,
-               stream=None) -> torch.Tensor:
+               step: int = 0, out=None, accumulate: bool = False, dtype=None,
+               workspace=None) -> torch.Tensor:
     """The gradient of ``embed``'s table, [V][D]: the sum over each word's
     tokens of ``grad`` [N][D] (lda_embed_grad), for the same scale, p, seed and
     step.  ``out`` (or a new tensor of type ``dtype``): the gradient's type or
     float32; with ``accumulate`` the sums are added to it and rows without
     tokens are not touched.  The result does not depend on the order in which
     the GPU works.  ``workspace``: a uint8 tensor of at least
-    ``embed_grad_workspace_bytes(N, V, D)`` bytes, or None to allocate one."""
-    _rows(grad, "grad")
-    dev = grad.device
-    _require(word_id, "word_id", _I32, 1)
-    N, D = grad.shape
-    V = int(V)
-    if word_id.shape[0] != N:
-        raise ValueError("grad and word_id lengths differ")
-    if word_id.device != dev:
-        raise ValueError("all tensors must be on one device")
-    p = _probability(p)
-    if accumulate and out is None:
-        raise ValueError("accumulate needs out")
-    with _on(dev, stream):
-        if out is None:
-            dtype = grad.dtype if dtype is None else dtype
-            if dtype not in (_F32, grad.dtype):
-                raise TypeError("dtype must be float32 or the gradient's")
-            out = torch.empty((V, D), dtype=dtype, device=dev)
-        else:
-            _rows(out, "out", dev, None, (V, D), out=True)
-            if out.dtype not in (_F32, grad.dtype) or dtype not in (None, out.dtype):
-                raise TypeError("out must be float32 or the gradient's type, and dtype its own")
-        need = embed_grad_workspace_bytes(N, V, D)
-        if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        else:
-            _require(workspace, "workspace", torch.uint8, 1)
-            if workspace.device != dev:
-                raise ValueError("workspace must be on the tensors' device")
-        _run("lda_embed_grad", dev, stream, grad.data_ptr(), _ld(grad), word_id.data_ptr(),
-             out.data_ptr(), _ld(out), N, V, D, DTYPES[grad.dtype], DTYPES[out.dtype],
-             float(scale), p, int(seed) & _U64, int(step) & _U32, int(bool(accumulate)),
-             workspace.data_ptr(), workspace.numel())
+    ``embed_grad_workspace_bytes(N, V, D)`` bytes, or None to allocate one.
+    ``stream``: where it runs (None: the current stream)."""
+    dev = grad.get_device()
+    N, D, ld = _rows(grad, "grad", dev)
+    ids = _vector(word_id, "word_id", _I32, N, dev)
+    V, own = int(V), grad.dtype
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        if dtype is not None and dtype not in (_F32, own):
+            raise TypeError("dtype must be float32 or the gradient's")
+        out, ldo = grad.new_empty((V, D), dtype=dtype or own), D
+    else:
+        ldo = _rows(out, "out", dev, None, (V, D), True)[2]
+        if out.dtype not in (_F32, own) or dtype not in (None, out.dtype):
+            raise TypeError("out must be float32 or the gradient's type, and dtype its own")
+    if workspace is None:
+        workspace = grad.new_empty(embed_grad_workspace_bytes(N, V, D), dtype=_U8)
+    else:
+        _require(workspace, "workspace", _U8, 1)
+        if workspace.get_device() != dev:
+            raise ValueError("workspace must be on the tensors' device")
+    _run("lda_embed_grad", dev, grad.data_ptr(), ld, ids, out.data_ptr(), ldo, N, V, D, DTYPES[own],
+         DTYPES[out.dtype], scale, _probability(p), int(seed) & _U64, int(step) & _U32,
+         1 if accumulate else 0, workspace.data_ptr(), workspace.numel())
     return out
 
 
-def dropout(x, p: float, seed: int, step: int = 0, out=None, stream=None) -> torch.Tensor:
+def _as_rows(t, name: str):
+    """A contiguous tensor as the matrix of its last dimension's rows (a vector:
+    one row); a matrix as it is."""
+    if t.dim() == 2:
+        return t
+    if t.dim() == 0:
+        raise ValueError(f"{name} must have at least 1 dimension")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.view(-1, t.shape[-1]) if t.numel() else t.reshape(0, 1)
+
+
+@_entry
+def dropout(x, p: float, seed: int, step: int = 0, out=None) -> torch.Tensor:
     """``x`` with each element 0 with probability ``p`` and otherwise divided by
     the probability of keeping it (lda_dropout); given the gradient of that,
     the same call gives the gradient of ``x``.  x: a contiguous tensor of any
     shape (rows: its last dimension; a vector is one row), or a matrix of
-    contiguous rows.  ``out`` may be ``x``."""
-    if not isinstance(x, torch.Tensor):
-        raise TypeError("x must be a torch.Tensor")
-    if x.dim() == 0:
-        raise ValueError("x must have at least 1 dimension")
+    contiguous rows.  ``out`` may be ``x``.  ``stream``: where it runs (None: the
+    current stream)."""
+    dev = x.get_device()
+    a = _as_rows(x, "x")
+    rows, cols, ld = _rows(a, "x", dev)
     p = _probability(p)
-    if x.dim() != 2 and not x.is_contiguous():
-        raise ValueError("x must be contiguous")
-    a = x if x.dim() == 2 else x.view(-1, x.shape[-1]) if x.numel() else x.reshape(0, 1)
-    _rows(a, "x")
-    dev = x.device
-    with _on(dev, stream):
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        elif not isinstance(out, torch.Tensor) or out.shape != x.shape:
+    if out is None:
+        out = x.new_empty(x.shape)
+        ldo = cols
+    else:
+        if not isinstance(out, _Tensor) or out.shape != x.shape:
             raise ValueError("out must be a tensor of x's shape")
-        elif out.dim() != 2 and not out.is_contiguous():
-            raise ValueError("out must be contiguous")
-        b = out if out.dim() == 2 else out.view(a.shape)
-        _rows(b, "out", dev, x.dtype, tuple(a.shape), out=True)
-        if x.numel():
-            _run("lda_dropout", dev, stream, a.data_ptr(), _ld(a), b.data_ptr(), _ld(b),
-                 a.shape[0], a.shape[1], DTYPES[x.dtype], p, int(seed) & _U64, int(step) & _U32)
+        ldo = _rows(_as_rows(out, "out"), "out", dev, x.dtype, (rows, cols), True)[2]
+    if rows and cols:
+        _run("lda_dropout", dev, x.data_ptr(), ld, out.data_ptr(), ldo, rows, cols, DTYPES[x.dtype],
+             p, int(seed) & _U64, int(step) & _U32)
     return out
 
 
-def _rules(logits, history, lengths, prompt, repetition, frequency, presence, bias, mask):
+def _rules(dev, B, V, history, lengths, prompt, repetition, frequency, presence, bias, mask):
     """The rules as the library takes them, or None where there are none."""
-    B, V = logits.shape
-    dev = logits.device
-    r = LogitRules()
+    past = (None, 0, 0, None, None, None, None, None)
     if history is not None:
-        _rows(history, "history", dev, _I32)
-        if history.shape[0] != B:
+        n, capacity, apart = _rows(history, "history", dev, _I32)
+        if n != B:
             raise ValueError("history must have a row for each row of logits")
         if lengths is None:
             raise ValueError("history needs lengths")
-        if B > 1 and history.stride(0) < history.shape[1]:
+        if apart < capacity:
             raise ValueError("history's rows overlap")
-        r.history, r.ld_history, r.capacity = history.data_ptr(), _ld(history), history.shape[1]
-        _vector(lengths, "lengths", _I32, B, dev)
-        r.lengths = lengths.data_ptr()
-        for t, name, dtype in ((prompt, "prompt", _I32), (repetition, "repetition", _F32),
-                               (frequency, "frequency", _F32), (presence, "presence", _F32)):
-            if t is not None:
-                _vector(t, name, dtype, B, dev)
-                setattr(r, name, t.data_ptr())
+        past = (history.data_ptr(), apart, capacity, _vector(lengths, "lengths", _I32, B, dev),
+                None if prompt is None else _vector(prompt, "prompt", _I32, B, dev),
+                None if repetition is None else _vector(repetition, "repetition", _F32, B, dev),
+                None if frequency is None else _vector(frequency, "frequency", _F32, B, dev),
+                None if presence is None else _vector(presence, "presence", _F32, B, dev))
     elif not (lengths is prompt is repetition is frequency is presence is None):
         raise ValueError("lengths, prompt and penalties need history")
-    for t, name, dtype, width in ((bias, "bias", _F32, V), (mask, "mask", _I32, (V + 31) // 32)):
-        if t is None:
-            continue
-        if isinstance(t, torch.Tensor) and t.dim() == 1:  # one row for all
-            _vector(t, name, dtype, width, dev)
-            ld = 0
-        else:
-            _rows(t, name, dev, dtype, (B, width))
-            ld = _ld(t)
-            if 0 < ld < width:
-                raise ValueError(f"{name}'s rows overlap")
-        setattr(r, name, t.data_ptr())
-        setattr(r, "ld_" + name, ld)
-    if history is None and bias is None and mask is None:
+    elif bias is None and mask is None:
         return None
-    return ctypes.byref(r)
+    return ctypes.byref(LogitRules(*past, *_row_or_rows(bias, "bias", _F32, B, V, dev),
+                                   *_row_or_rows(mask, "mask", _I32, B, (V + 31) // 32, dev)))
 
 
+def _row_or_rows(t, name, dtype, B, width, dev):
+    """(address, elements from row to row), 0 where one row serves all."""
+    if t is None:
+        return None, 0
+    if isinstance(t, _Tensor) and t.dim() == 1:
+        return _vector(t, name, dtype, width, dev), 0
+    apart = _rows(t, name, dev, dtype, (B, width))[2]
+    if 0 < apart < width:
+        raise ValueError(f"{name}'s rows overlap")
+    return t.data_ptr(), apart
+
+
+@_entry
 def penalise_logits(logits, history=None, lengths=None, prompt=None, repetition=None,
-                    frequency=None, presence=None, bias=None, mask=None, out=None,
-                    stream=None) -> torch.Tensor:
+                    frequency=None, presence=None, bias=None, mask=None,
+                    out=None) -> torch.Tensor:
     """logits [B][V] under the rules (lda_penalise_logits): ``history`` int32
     [B][capacity] with ``lengths`` int32 [B], the first ``prompt`` [B] of them
     not generated; ``repetition``, ``frequency``, ``presence`` float32 [B];
     ``bias`` float32 [V] or [B][V]; ``mask`` int32 [V / 32] or [B][V / 32]
     (rounded up), bit 0 where a token is not allowed.  ``out`` may be
-    ``logits``."""
-    _rows(logits, "logits")
-    rules = _rules(logits, history, lengths, prompt, repetition, frequency, presence, bias, mask)
-    (B, V), dev = logits.shape, logits.device
-    with _on(dev, stream):
-        if out is None:
-            out = torch.empty((B, V), dtype=logits.dtype, device=dev)
-        else:
-            _rows(out, "out", dev, logits.dtype, (B, V), out=True)
-        _run("lda_penalise_logits", dev, stream, logits.data_ptr(), _ld(logits), out.data_ptr(),
-             _ld(out), B, V, DTYPES[logits.dtype], rules)
+    ``logits``.  ``stream``: where it runs (None: the current stream)."""
+    dev = logits.get_device()
+    B, V, ld = _rows(logits, "logits", dev)
+    rules = _rules(dev, B, V, history, lengths, prompt, repetition, frequency, presence, bias, mask)
+    if out is None:
+        out, ldo = logits.new_empty((B, V)), V
+    else:
+        ldo = _rows(out, "out", dev, logits.dtype, (B, V), True)[2]
+    _run("lda_penalise_logits", dev, logits.data_ptr(), ld, out.data_ptr(), ldo, B, V,
+         DTYPES[logits.dtype], rules)
     return out
 
 
+@functools.lru_cache(maxsize=256)
 def draw_logits_workspace_bytes(B: int, V: int) -> int:
     """Bytes of device workspace ``draw_logits`` needs (0: none, or unsupported)."""
     return int(_lib.load().lda_draw_logits_workspace_bytes(int(B), int(V)))
 
 
+@_entry
 def draw_logits(logits, seed, position, temperature=None, min_p=None, history=None, lengths=None,
                 prompt=None, repetition=None, frequency=None, presence=None, bias=None, mask=None,
-                out=None, workspace=None, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+                out=None, workspace=None) -> tuple[torch.Tensor, torch.Tensor]:
     """(z int32 [B], prob float32 [B]): one token of each row of ``logits``
     [B][V] under ``penalise_logits``' rules, and the probability with which it
     was drawn (lda_draw_logits).  ``seed`` int64 [B] and ``position`` int32 [B]
@@ -290,32 +307,28 @@ def draw_logits(logits, seed, position, temperature=None, min_p=None, history=No
     float32 [B]: where it is not above 0 the row takes its largest logit.
     ``min_p`` float32 [B]: tokens below that share of the likeliest token's
     probability are not drawn.  A row with nothing to draw gives z = -1 and
-    prob = 0.  ``out``: (z, prob) to overwrite."""
-    _rows(logits, "logits")
-    rules = _rules(logits, history, lengths, prompt, repetition, frequency, presence, bias, mask)
-    (B, V), dev = logits.shape, logits.device
-    _vector(seed, "seed", _I64, B, dev)
-    _vector(position, "position", _I32, B, dev)
-    for t, name in ((temperature, "temperature"), (min_p, "min_p")):
-        if t is not None:
-            _vector(t, name, _F32, B, dev)
-    with _on(dev, stream):
-        if out is None:
-            z = torch.empty(B, dtype=_I32, device=dev)
-            prob = torch.empty(B, dtype=_F32, device=dev)
-        else:
-            z, prob = out
-            _vector(z, "out[0]", _I32, B, dev)
-            _vector(prob, "out[1]", _F32, B, dev)
-        need = draw_logits_workspace_bytes(B, V)
-        if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        else:
-            _require(workspace, "workspace", torch.uint8, 1)
-            if workspace.device != dev:
-                raise ValueError("workspace must be on the tensors' device")
-        _run("lda_draw_logits", dev, stream, logits.data_ptr(), _ld(logits), B, V,
-             DTYPES[logits.dtype], rules, None if temperature is None else temperature.data_ptr(),
-             None if min_p is None else min_p.data_ptr(), seed.data_ptr(), position.data_ptr(),
-             z.data_ptr(), prob.data_ptr(), workspace.data_ptr(), workspace.numel())
+    prob = 0.  ``out``: (z, prob) to overwrite.  ``workspace``: a uint8 tensor of
+    at least ``draw_logits_workspace_bytes(B, V)`` bytes, or None to allocate
+    one.  ``stream``: where it runs (None: the current stream)."""
+    dev = logits.get_device()
+    B, V, ld = _rows(logits, "logits", dev)
+    rules = _rules(dev, B, V, history, lengths, prompt, repetition, frequency, presence, bias, mask)
+    seeds = _vector(seed, "seed", _I64, B, dev)
+    places = _vector(position, "position", _I32, B, dev)
+    heat = None if temperature is None else _vector(temperature, "temperature", _F32, B, dev)
+    floor = None if min_p is None else _vector(min_p, "min_p", _F32, B, dev)
+    if out is None:
+        z, prob = logits.new_empty(B, dtype=_I32), logits.new_empty(B, dtype=_F32)
+        to = z.data_ptr(), prob.data_ptr()
+    else:
+        z, prob = out
+        to = _vector(z, "out[0]", _I32, B, dev), _vector(prob, "out[1]", _F32, B, dev)
+    if workspace is None:
+        workspace = logits.new_empty(draw_logits_workspace_bytes(B, V), dtype=_U8)
+    else:
+        _require(workspace, "workspace", _U8, 1)
+        if workspace.get_device() != dev:
+            raise ValueError("workspace must be on the tensors' device")
+    _run("lda_draw_logits", dev, logits.data_ptr(), ld, B, V, DTYPES[logits.dtype], rules, heat,
+         floor, seeds, places, *to, workspace.data_ptr(), workspace.numel())
     return z, prob
