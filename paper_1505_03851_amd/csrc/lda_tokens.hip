@@ -92,7 +92,7 @@ struct GradLayout {
   uint32_t col_tiles;      // tiles of 64 width columns
   uint32_t chunk, chunks;  // sorted positions of a wavefront
   int64_t ld_part;
-  size_t key[2], index[2], hist, total, crossing, part, bytes;
+  size_t tokens[2], hist, total, crossing, part, bytes;
 };
 
 GradLayout grad_layout(int64_t N, int32_t V, int32_t D) {
@@ -118,10 +118,7 @@ GradLayout grad_layout(int64_t N, int32_t V, int32_t D) {
     at += (b + 255) & ~(size_t)255;
     return o;
   };
-  for (int i = 0; i < 2; ++i) {
-    L.key[i] = take(4 * (size_t)N);
-    L.index[i] = take(4 * (size_t)N);
-  }
+  for (int i = 0; i < 2; ++i) L.tokens[i] = take(sizeof(Token) * (size_t)N);
   L.hist = take(4 * (size_t)L.sort_chunks << L.bits);
   L.total = take(4 * (size_t)kSortMaxBins);
   L.crossing = take(4 * ((size_t)L.chunks + 1));
@@ -133,7 +130,7 @@ GradLayout grad_layout(int64_t N, int32_t V, int32_t D) {
 template <typename TG, typename TO, int W>
 void launch_reduce(const void *grad, int64_t ldg, void *out, int64_t ldo, int32_t D, float factor,
                    const Dropout &drop, bool accumulate, const GradLayout &L, const GradPlan &g,
-                   const uint32_t *key, const uint32_t *index, char *w, hipStream_t s) {
+                   const Token *token, char *w, hipStream_t s) {
   using SG = typename TG::store;
   using SO = typename TO::store;
   float *part = (float *)(w + L.part);
@@ -142,14 +139,14 @@ void launch_reduce(const void *grad, int64_t ldg, void *out, int64_t ldo, int32_
   if (drop.q)
     reduce_kernel<TG, TO, W, true><<<grid, 256, 0, s>>>((const SG *)grad, ldg, (SO *)out, ldo, D,
                                                         factor, drop, accumulate, L.col_tiles, g,
-                                                        key, index, part, crossing);
+                                                        token, part, crossing);
   else
     reduce_kernel<TG, TO, W, false><<<grid, 256, 0, s>>>((const SG *)grad, ldg, (SO *)out, ldo, D,
                                                          factor, drop, accumulate, L.col_tiles, g,
-                                                         key, index, part, crossing);
+                                                         token, part, crossing);
   if (L.chunks > 1)
     join_kernel<TO, W><<<512, kJoinWaves * 64, 0, s>>>((SO *)out, ldo, D, factor, accumulate,
-                                                       L.col_tiles, g, key, part, crossing);
+                                                       L.col_tiles, g, token, part, crossing);
 }
 
 template <typename TG, typename TO>
@@ -175,37 +172,33 @@ int launch_grad(const void *grad, int64_t ldg, const int32_t *word_id, void *out
   char *w = (char *)workspace;
   uint32_t *hist = (uint32_t *)(w + L.hist), *total = (uint32_t *)(w + L.total);
   uint32_t *crossing = (uint32_t *)(w + L.crossing);
-  const uint32_t *key = nullptr, *index = nullptr;
+  const Token *token = nullptr;
   if (chunks == 1) {
-    uint32_t *key_out = (uint32_t *)(w + L.key[0]), *index_out = (uint32_t *)(w + L.index[0]);
+    Token *out_tokens = (Token *)(w + L.tokens[0]);
     sort_chunk_kernel<<<1 + extra, kSortThreads, 0, s>>>(word_id, (int32_t)N, V, L.passes, L.bits,
-                                                         key_out, index_out, crossing, clear);
-    key = key_out;
-    index = index_out;
+                                                         out_tokens, crossing, clear);
+    token = out_tokens;
   }
   for (int pass = 0; chunks > 1 && pass < L.passes; ++pass) {
-    uint32_t *key_out = (uint32_t *)(w + L.key[pass & 1]);
-    uint32_t *index_out = (uint32_t *)(w + L.index[pass & 1]);
+    Token *out_tokens = (Token *)(w + L.tokens[pass & 1]);
     const int shift = pass * L.bits;
     clear.part = 2 * pass;
     sort_hist_kernel<<<chunks + extra, kSortThreads, 0, s>>>(
-        word_id, key, N, V, shift, L.bits, hist, pass == 0 ? crossing : nullptr, clear);
+        word_id, token, N, V, shift, L.bits, hist, pass == 0 ? crossing : nullptr, clear);
     // from 17 chunks on a launch of its own sums the chunks before each
     const bool scan = chunks > 16;
     if (scan)
       sort_scan_kernel<<<((1u << L.bits) + 63) / 64, kSortThreads, 0, s>>>(hist, total, chunks,
                                                                            1 << L.bits);
     clear.part = 2 * pass + 1;
-    sort_scatter_kernel<<<chunks + extra, kSortThreads, 0, s>>>(
-        word_id, key, index, N, V, shift, L.bits, hist, scan ? total : nullptr, key_out, index_out,
-        clear);
-    key = key_out;
-    index = index_out;
+    sort_scatter_kernel<<<chunks + extra, kSortThreads, 0, s>>>(word_id, token, N, V, shift, L.bits,
+                                                                hist, scan ? total : nullptr,
+                                                                out_tokens, clear);
+    token = out_tokens;
   }
   const GradPlan g{(uint32_t)N, (uint32_t)V, L.chunk, L.chunks, L.ld_part};
 #define LDA_REDUCE(W)                                                                           \
-  launch_reduce<TG, TO, W>(grad, ldg, out, ldo, D, factor, drop, accumulate, L, g, key, index,  \
-                           w, s)
+  launch_reduce<TG, TO, W>(grad, ldg, out, ldo, D, factor, drop, accumulate, L, g, token, w, s)
   switch (L.width) {
     case 8: LDA_REDUCE(8); break;
     case 4: LDA_REDUCE(4); break;

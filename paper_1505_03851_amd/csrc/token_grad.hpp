@@ -55,17 +55,23 @@ __device__ __forceinline__ void clear_share(const ClearShare &c) {
   }
 }
 
-// a token's key: its word, or V (sorted last, given no gradient) outside [0, V)
-__device__ __forceinline__ uint32_t sort_key(const int32_t *word_id, const uint32_t *key,
-                                             int64_t i, int32_t V) {
-  if (key) return key[i];
+// A token to be sorted, kept and moved as one value of 8 bytes: its word, or V
+// (sorted last, given no gradient) outside [0, V), and its number.
+struct alignas(8) Token {
+  uint32_t word, number;
+};
+
+// token i as the pass before left it, or (the first pass) from word_id
+__device__ __forceinline__ Token load_token(const int32_t *word_id, const Token *sorted, int64_t i,
+                                            int32_t V) {
+  if (sorted) return sorted[i];
   const int32_t w = word_id[i];
-  return (uint32_t)w < (uint32_t)V ? (uint32_t)w : (uint32_t)V;
+  return Token{(uint32_t)w < (uint32_t)V ? (uint32_t)w : (uint32_t)V, (uint32_t)i};
 }
 
 // hist[chunk][digit]: the tokens of each chunk with each digit
 __global__ __launch_bounds__(kSortThreads) void sort_hist_kernel(
-    const int32_t *__restrict__ word_id, const uint32_t *__restrict__ key, int64_t N, int32_t V,
+    const int32_t *__restrict__ word_id, const Token *__restrict__ sorted, int64_t N, int32_t V,
     int shift, int bits, uint32_t *__restrict__ hist, uint32_t *crossing, ClearShare clear) {
   __shared__ uint32_t count[kSortMaxBins];
   if (blockIdx.x >= clear.blocks) {
@@ -79,7 +85,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_hist_kernel(
 #pragma unroll
   for (int r = 0; r < kSortEach; ++r) {
     const int64_t i = first + r * kSortThreads + threadIdx.x;
-    k[r] = i < N ? sort_key(word_id, key, i, V) : 0;
+    k[r] = i < N ? load_token(word_id, sorted, i, V).word : 0;
   }
   for (int b = threadIdx.x; b < bins; b += kSortThreads) count[b] = 0;
   __syncthreads();
@@ -158,7 +164,7 @@ struct SortLds {
 // chunk): rank[r] is the number of tokens of the same digit before the token in
 // its wavefront, and count[wave][digit] becomes the number in the wavefronts
 // before it.  Returns thread b's tokens of digit b in the whole chunk.
-__device__ __forceinline__ uint32_t rank_chunk(SortLds &s, const uint32_t (&k)[kSortEach], int n,
+__device__ __forceinline__ uint32_t rank_chunk(SortLds &s, const Token (&k)[kSortEach], int n,
                                                int first, int shift, int bits,
                                                uint32_t (&rank)[kSortEach]) {
   const int bins = 1 << bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -168,7 +174,7 @@ __device__ __forceinline__ uint32_t rank_chunk(SortLds &s, const uint32_t (&k)[k
 #pragma unroll
   for (int r = 0; r < kSortEach; ++r) {
     const bool there = first + 64 * r < n;
-    const uint32_t digit = k[r] >> shift & (bins - 1);
+    const uint32_t digit = k[r].word >> shift & (bins - 1);
     uint64_t same = __ballot(there);
     for (int b = 0; b < bits; ++b) {
       const uint64_t set = __ballot(digit >> b & 1);
@@ -201,10 +207,9 @@ __device__ __forceinline__ uint32_t rank_chunk(SortLds &s, const uint32_t (&k)[k
 // The tokens of one chunk to their places by one digit: the chunk's base for
 // the digit, the wavefront's and the token's rank in it.
 __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(
-    const int32_t *__restrict__ word_id, const uint32_t *__restrict__ key,
-    const uint32_t *__restrict__ index, int64_t N, int32_t V, int shift, int bits,
-    const uint32_t *__restrict__ hist, const uint32_t *__restrict__ total,
-    uint32_t *__restrict__ key_out, uint32_t *__restrict__ index_out, ClearShare clear) {
+    const int32_t *__restrict__ word_id, const Token *__restrict__ sorted, int64_t N, int32_t V,
+    int shift, int bits, const uint32_t *__restrict__ hist, const uint32_t *__restrict__ total,
+    Token *__restrict__ out, ClearShare clear) {
   __shared__ SortLds s;
   if (blockIdx.x >= clear.blocks) {
     clear_share(clear);
@@ -214,12 +219,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(
   const int64_t start = (int64_t)blockIdx.x * kSortChunk;
   const int n = N - start < kSortChunk ? (int)(N - start) : kSortChunk;
   const int first = wave * 64 * kSortEach + (threadIdx.x & 63);
-  uint32_t k[kSortEach], from[kSortEach], rank[kSortEach];
+  Token k[kSortEach];
+  uint32_t rank[kSortEach];
 #pragma unroll
   for (int r = 0; r < kSortEach; ++r) {
     const int i = first + 64 * r;
-    k[r] = i < n ? sort_key(word_id, key, start + i, V) : 0;
-    from[r] = i < n && index ? index[start + i] : (uint32_t)(start + i);
+    k[r] = i < n ? load_token(word_id, sorted, start + i, V) : Token{0, 0};
   }
   // this digit's tokens of all chunks (to place the digit) and of earlier
   // chunks: from sort_scan_kernel, or (few chunks) summed here
@@ -242,21 +247,17 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(
 #pragma unroll
   for (int r = 0; r < kSortEach; ++r) {
     if (first + 64 * r >= n) break;
-    const uint32_t digit = k[r] >> shift & (bins - 1);
-    const uint32_t at = s.base[digit] + s.count[wave][digit] + rank[r];
-    key_out[at] = k[r];
-    index_out[at] = from[r];
+    const uint32_t digit = k[r].word >> shift & (bins - 1);
+    out[s.base[digit] + s.count[wave][digit] + rank[r]] = k[r];
   }
 }
 
 // One chunk: every pass in one workgroup, through LDS.
 __global__ __launch_bounds__(kSortThreads) void sort_chunk_kernel(
     const int32_t *__restrict__ word_id, int32_t N, int32_t V, int passes, int bits,
-    uint32_t *__restrict__ key_out, uint32_t *__restrict__ index_out, uint32_t *crossing,
-    ClearShare clear) {
+    Token *__restrict__ out, uint32_t *crossing, ClearShare clear) {
   __shared__ SortLds s;
-  __shared__ uint32_t keys[kSortChunk];
-  __shared__ uint16_t indices[kSortChunk];
+  __shared__ Token tokens[kSortChunk];
   if (blockIdx.x >= clear.blocks) {
     clear_share(clear);
     return;
@@ -264,12 +265,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_chunk_kernel(
   if (threadIdx.x == 0) *crossing = 0;
   const int wave = threadIdx.x >> 6;
   const int first = wave * 64 * kSortEach + (threadIdx.x & 63);
-  uint32_t k[kSortEach], from[kSortEach], rank[kSortEach];
+  Token k[kSortEach];
+  uint32_t rank[kSortEach];
 #pragma unroll
   for (int r = 0; r < kSortEach; ++r) {
     const int i = first + 64 * r;
-    k[r] = i < N ? sort_key(word_id, nullptr, i, V) : 0;
-    from[r] = (uint32_t)i;
+    k[r] = i < N ? load_token(word_id, nullptr, i, V) : Token{0, 0};
   }
   for (int pass = 0; pass < passes; ++pass) {
     const int shift = pass * bits;
@@ -278,27 +279,18 @@ __global__ __launch_bounds__(kSortThreads) void sort_chunk_kernel(
     if ((int)threadIdx.x < 1 << bits) s.base[threadIdx.x] = place;
     __syncthreads();
     const bool last = pass + 1 == passes;
+    Token *to = last ? out : tokens;
 #pragma unroll
     for (int r = 0; r < kSortEach; ++r) {
       if (first + 64 * r >= N) break;
-      const uint32_t digit = k[r] >> shift & ((1 << bits) - 1);
-      const uint32_t at = s.base[digit] + s.count[wave][digit] + rank[r];
-      if (last) {
-        key_out[at] = k[r];
-        index_out[at] = from[r];
-      } else {
-        keys[at] = k[r];
-        indices[at] = (uint16_t)from[r];
-      }
+      const uint32_t digit = k[r].word >> shift & ((1 << bits) - 1);
+      to[s.base[digit] + s.count[wave][digit] + rank[r]] = k[r];
     }
     __syncthreads();
     if (last) break;
 #pragma unroll
-    for (int r = 0; r < kSortEach; ++r) {
-      const int i = first + 64 * r;
-      k[r] = i < N ? keys[i] : 0;
-      from[r] = i < N ? indices[i] : 0;
-    }
+    for (int r = 0; r < kSortEach; ++r)
+      if (first + 64 * r < N) k[r] = tokens[first + 64 * r];
     __syncthreads();
   }
 }
@@ -347,8 +339,8 @@ template <typename TG, typename TO, int W, bool DROP>
 __global__ __launch_bounds__(256) void reduce_kernel(
     const typename TG::store *__restrict__ grad, int64_t ldg, typename TO::store *__restrict__ out,
     int64_t ldo, int32_t D, float factor, Dropout drop, bool accumulate, uint32_t col_tiles,
-    GradPlan g, const uint32_t *__restrict__ key, const uint32_t *__restrict__ index,
-    float *__restrict__ part, uint32_t *__restrict__ crossing) {
+    GradPlan g, const Token *__restrict__ token, float *__restrict__ part,
+    uint32_t *__restrict__ crossing) {
   // rows of a lane in flight: 32 registers of them
   constexpr int U = sizeof(Packed<TG, W>) <= 8 ? 16 : 128 / (int)sizeof(Packed<TG, W>);
   static_assert(64 % U == 0, "a batch lies within 64 positions");
@@ -366,13 +358,13 @@ __global__ __launch_bounds__(256) void reduce_kernel(
   const uint32_t offset = (uint32_t)col * (uint32_t)sizeof(typename TG::store);
   const uint32_t begin = c * g.chunk;
   const uint32_t end = g.N - begin < g.chunk ? g.N : begin + g.chunk;
-  bool began_here = begin == 0 || key[begin - 1] != key[begin];
+  bool began_here = begin == 0 || token[begin - 1].word != token[begin].word;
   float sum[W] = {};
   for (uint32_t p = begin; p < end; p += 64) {
     const uint32_t at = p + lane < end ? p + lane : end - 1;
-    const uint32_t word = key[at];
-    const uint32_t next = at + 1 < g.N ? key[at + 1] : g.V;  // the word after
-    const uint32_t row = index[at];
+    const Token own_token = token[at];
+    const uint32_t word = own_token.word, row = own_token.number;
+    const uint32_t next = at + 1 < g.N ? token[at + 1].word : g.V;  // the word after
     const bool live = p + lane < end && word < g.V;
     // (tokens without a word are the last)
     const int count = __popcll(__ballot(live));
@@ -436,7 +428,7 @@ constexpr int kJoinWaves = 8;
 template <typename TO, int W>
 __global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(
     typename TO::store *__restrict__ out, int64_t ldo, int32_t D, float factor, bool accumulate,
-    uint32_t col_tiles, GradPlan g, const uint32_t *__restrict__ key,
+    uint32_t col_tiles, GradPlan g, const Token *__restrict__ token,
     const float *__restrict__ part, const uint32_t *__restrict__ crossing) {
   constexpr int U = 8;
   __shared__ float sums[kJoinWaves - 1][64 * W];
@@ -449,15 +441,15 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(
     const int n = D - own < W ? (D - own > 0 ? D - own : 0) : W;
     const int32_t col = own < D - W ? own : D - W;
     const uint32_t c0 = crossing[1 + i];
-    const uint32_t word = key[(c0 + 1) * g.chunk - 1];
-    // the chunk in which the word ends: the last whose first key is the word
+    const uint32_t word = token[(c0 + 1) * g.chunk - 1].word;
+    // the chunk in which the word ends: the last whose first token is one of it,
+    // sought 64 at a time
     uint32_t lo = c0 + 1, hi = g.chunks;
     while (hi - lo > 1) {
-      const uint32_t mid = lo + (hi - lo) / 2;
-      if (key[mid * g.chunk] == word)
-        lo = mid;
-      else
-        hi = mid;
+      const uint32_t step = (hi - lo + 62) / 64, probe = lo + (lane + 1) * step;
+      const uint64_t yes = __ballot(probe < hi && token[probe * g.chunk].word == word);
+      lo += __popcll(yes) * step;
+      hi = hi - lo > step ? lo + step : hi;
     }
     const uint32_t parts = lo - c0 + 1;
     const uint32_t each = (parts + kJoinWaves - 1) / kJoinWaves;
