@@ -121,15 +121,32 @@ __device__ __forceinline__ void history_count(const History &h, uint32_t i, word
   }
 }
 
+// The first of a row's history, two loads of a lane, which can be on their way
+// while other things are.
+struct Tokens {
+  words4 t[2];
+};
+
+__device__ __forceinline__ Tokens load_tokens(const History &h) {
+  const uint32_t i = 4 * threadIdx.x;
+  return Tokens{{history_load(h, i), history_load(h, i + 4 * blockDim.x)}};
+}
+
 // The uses of the tokens [first, first + size) in a row's history, counted in
-// LDS (which the caller has cleared and synchronised) by the whole workgroup.
-__device__ __forceinline__ void count_history(const History &h, uint32_t first, uint32_t size,
-                                              uint32_t *count) {
+// LDS (which the caller has cleared and synchronised) by the whole workgroup;
+// `ahead`: load_tokens of it.
+__device__ __forceinline__ void count_history(const History &h, Tokens ahead, uint32_t first,
+                                              uint32_t size, uint32_t *count) {
   const uint32_t step = 4 * blockDim.x;
-  for (uint32_t i = 4 * threadIdx.x; i < (uint32_t)h.size; i += 2 * step) {
-    const words4 a = history_load(h, i), b = history_load(h, i + step);
-    history_count(h, i, a, first, size, count);
-    history_count(h, i + step, b, first, size, count);
+  for (uint32_t i = 4 * threadIdx.x, start = 0; start < (uint32_t)h.size;
+       i += 2 * step, start += 2 * step) {
+    // the next two loads on their way while these are counted
+    Tokens next;
+    const bool more = start + 2 * step < (uint32_t)h.size;
+    if (more) next = Tokens{{history_load(h, i + 2 * step), history_load(h, i + 3 * step)}};
+    history_count(h, i, ahead.t[0], first, size, count);
+    history_count(h, i + step, ahead.t[1], first, size, count);
+    if (more) ahead = next;
   }
 }
 
@@ -225,12 +242,13 @@ __global__ __launch_bounds__(64 * kGroupWaves) void penalise_kernel(
     const int64_t first = start + wave * kGroup;
     const RowRules r = row_rules(rules, b);
     const History h = row_history(rules, b);
+    const Tokens ahead = load_tokens(h);
     Group<T> g;
     load_group<T>(logits + b * ld, first, V, r, g);
     if (h.size) {
       clear_counts(count);
       __syncthreads();
-      count_history(h, (uint32_t)start, waves * kGroup, lds);
+      count_history(h, ahead, (uint32_t)start, waves * kGroup, lds);
       __syncthreads();
     }
     float x[kSteps][8];
@@ -386,8 +404,14 @@ __global__ __launch_bounds__(64 * kGroupWaves) void group_kernel(
     const DrawRow d = draw_row(temperature, min_p, b);
     GroupSum *mine = groups + b * per_row;
     float top = -INFINITY;
+    if (FLOOR && (d.greedy || d.floor == -INFINITY)) continue;
+    const int64_t first = (int64_t)g * kGroup;
+    const RowRules r = row_rules(rules, b);
+    const History h = row_history(rules, b);
+    const Tokens ahead = load_tokens(h);
+    Group<T> q;
+    load_group<T>(logits + b * ld, first, V, r, q);
     if (FLOOR) {
-      if (d.greedy || d.floor == -INFINITY) continue;
       for (uint32_t i = lane; i < per_row; i += 64) top = fmaxf(top, mine[i].top);
       top = wave_max(top);
       // whether a group of the workgroup's reaches the floor
@@ -398,15 +422,10 @@ __global__ __launch_bounds__(64 * kGroupWaves) void group_kernel(
         continue;
       }
     }
-    const int64_t first = (int64_t)g * kGroup;
-    const RowRules r = row_rules(rules, b);
-    const History h = row_history(rules, b);
-    Group<T> q;
-    load_group<T>(logits + b * ld, first, V, r, q);
     if (h.size) {
       clear_counts(count);
       __syncthreads();
-      count_history(h, g0 * kGroup, waves * kGroup, lds);
+      count_history(h, ahead, g0 * kGroup, waves * kGroup, lds);
       __syncthreads();
     }
     float x[kSteps][8];
@@ -437,7 +456,7 @@ __global__ __launch_bounds__(kDrawThreads) void draw_kernel(
     const RowRules r = row_rules(rules, b);
     const History h = row_history(rules, b);
     // the first of the history's tokens, on their way before the group is known
-    const words4 ahead = history_load(h, 4 * threadIdx.x);
+    const Tokens ahead = load_tokens(h);
     count[threadIdx.x] = 0;
     float top = -INFINITY;
     for (uint32_t g = lane; g < per_row; g += 64) top = fmaxf(top, mine[g].top);
@@ -477,9 +496,7 @@ __global__ __launch_bounds__(kDrawThreads) void draw_kernel(
     const float own = d.greedy ? 0.0f : variate((uint32_t)token, pos, 3u, s);
     if (h.size) {
       __syncthreads();
-      history_count(h, 4 * threadIdx.x, ahead, first, kGroup, count);
-      for (uint32_t i = 4 * (threadIdx.x + kDrawThreads); i < (uint32_t)h.size; i += 4 * kDrawThreads)
-        history_count(h, i, history_load(h, i), first, kGroup, count);
+      count_history(h, ahead, first, kGroup, count);
       __syncthreads();
       const uint32_t c = count[count_slot(threadIdx.x)];
       if (c) x = ruled(x, c, r);
