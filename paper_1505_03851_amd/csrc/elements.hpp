@@ -84,13 +84,16 @@ struct Packed {
 };
 
 // p[0 .. W) as it is in memory; only the first `n` are read (the rest: 0)
-// where n < W
-template <typename T, int W>
+// where n < W.  STREAM: what is read or written passes the caches by (it is
+// larger than they are and touched once), so that it does not put out what they
+// hold, nor wait for what they have to write back.
+template <typename T, int W, bool STREAM = false>
 __device__ __forceinline__ Packed<T, W> load_packed(const typename T::store *p, int n) {
   using R = Raw<W * (int)sizeof(typename T::store)>;
   Packed<T, W> a;
   if (n >= W) {
-    const typename R::type raw = *reinterpret_cast<const typename R::memory *>(p);
+    const auto *memory = reinterpret_cast<const typename R::memory *>(p);
+    const typename R::type raw = STREAM ? __builtin_nontemporal_load(memory) : *memory;
     a = __builtin_bit_cast(Packed<T, W>, raw);
   } else {
 #pragma unroll
@@ -100,21 +103,25 @@ __device__ __forceinline__ Packed<T, W> load_packed(const typename T::store *p, 
 }
 
 // p[0 .. W) -> x in float
-template <typename T, int W>
+template <typename T, int W, bool STREAM = false>
 __device__ __forceinline__ void load_elements(const typename T::store *p, int n, float (&x)[W]) {
-  const Packed<T, W> a = load_packed<T, W>(p, n);
+  const Packed<T, W> a = load_packed<T, W, STREAM>(p, n);
 #pragma unroll
   for (int j = 0; j < W; ++j) x[j] = T::up(a.v[j]);
 }
 
-template <typename T, int W>
+template <typename T, int W, bool STREAM = false>
 __device__ __forceinline__ void store_elements(typename T::store *p, int n, const float (&x)[W]) {
   using R = Raw<W * (int)sizeof(typename T::store)>;
   if (n >= W) {
     Packed<T, W> a;
 #pragma unroll
     for (int j = 0; j < W; ++j) a.v[j] = T::down(x[j]);
-    *reinterpret_cast<typename R::memory *>(p) = __builtin_bit_cast(typename R::type, a);
+    auto *memory = reinterpret_cast<typename R::memory *>(p);
+    if (STREAM)
+      __builtin_nontemporal_store(__builtin_bit_cast(typename R::type, a), memory);
+    else
+      *memory = __builtin_bit_cast(typename R::type, a);
   } else {
 #pragma unroll
     for (int j = 0; j < W; ++j)

@@ -136,14 +136,26 @@ void launch_reduce(const void *grad, int64_t ldg, void *out, int64_t ldo, int32_
   float *part = (float *)(w + L.part);
   uint32_t *crossing = (uint32_t *)(w + L.crossing);
   const unsigned grid = (unsigned)(((uint64_t)L.chunks * L.col_tiles + 3) / 4);
-  if (drop.q)
-    reduce_kernel<TG, TO, W, true><<<grid, 256, 0, s>>>((const SG *)grad, ldg, (SO *)out, ldo, D,
-                                                        factor, drop, accumulate, L.col_tiles, g,
-                                                        token, part, crossing);
+  // A gradient that the 256 MB behind the L2s cannot hold anyway passes them by:
+  // 1M tokens of 256 bfloat16 170 us against 185, 32,768 of 2,048 136 against 139;
+  // a smaller one may still be there from the launch that made it (131,072 of 256:
+  // 72.4 against 70.7).  In float a lane's 32 bytes are two accesses to one line
+  // (16,384 of 2,048: 131 against 129).
+  constexpr bool kMayStream = sizeof(SG) == 2;
+  const bool stream = kMayStream && (int64_t)g.N * D * (int64_t)sizeof(SG) >= (int64_t)128 << 20;
+#define LDA_SUM(DROP, STREAM)                                                                    \
+  reduce_kernel<TG, TO, W, DROP, STREAM><<<grid, 256, 0, s>>>(                                   \
+      (const SG *)grad, ldg, (SO *)out, ldo, D, factor, drop, accumulate, L.col_tiles, g, token, \
+      part, crossing)
+  if (drop.q && stream)
+    LDA_SUM(true, kMayStream);
+  else if (drop.q)
+    LDA_SUM(true, false);
+  else if (stream)
+    LDA_SUM(false, kMayStream);
   else
-    reduce_kernel<TG, TO, W, false><<<grid, 256, 0, s>>>((const SG *)grad, ldg, (SO *)out, ldo, D,
-                                                         factor, drop, accumulate, L.col_tiles, g,
-                                                         token, part, crossing);
+    LDA_SUM(false, false);
+#undef LDA_SUM
   if (L.chunks > 1)
     join_kernel<TO, W><<<512, kJoinWaves * 64, 0, s>>>((SO *)out, ldo, D, factor, accumulate,
                                                        L.col_tiles, g, token, part, crossing);

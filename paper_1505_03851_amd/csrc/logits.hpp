@@ -255,7 +255,7 @@ __global__ __launch_bounds__(64 * kGroupWaves) void penalise_kernel(
     rule_group<T>(g, first, h.size ? count : nullptr, r, x);
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
-      store_elements<T, 8>(out + b * ldo + first + (uint32_t)(s * 512 + (threadIdx.x & 63) * 8),
+      store_elements<T, 8, true>(out + b * ldo + first + (uint32_t)(s * 512 + (threadIdx.x & 63) * 8),
                            g.n[s], x[s]);
     __syncthreads();
   }

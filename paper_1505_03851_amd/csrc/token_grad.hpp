@@ -48,7 +48,7 @@ __device__ __forceinline__ void clear_share(const ClearShare &c) {
     const int64_t at = (i - row * units) << 4;
     char *p = c.out + row * c.ld + at;
     if (c.width - at >= 16) {
-      *reinterpret_cast<words4_any *>(p) = zero;
+      __builtin_nontemporal_store(zero, reinterpret_cast<words4_any *>(p));
     } else {
       for (int64_t j = 0; j < c.width - at; j += 2) *reinterpret_cast<half_any *>(p + j) = 0;
     }
@@ -335,7 +335,7 @@ __device__ __forceinline__ void write_row(typename TO::store *out, int64_t ldo, 
 // runs are then a mask in scalar registers, and a row's number a lane read.  U
 // rows are on their way together.  crossing[0] counts the chunks in which a word that
 // goes past the chunk's end begins, listed after it.
-template <typename TG, typename TO, int W, bool DROP>
+template <typename TG, typename TO, int W, bool DROP, bool STREAM>
 __global__ __launch_bounds__(256) void reduce_kernel(
     const typename TG::store *__restrict__ grad, int64_t ldg, typename TO::store *__restrict__ out,
     int64_t ldo, int32_t D, float factor, Dropout drop, bool accumulate, uint32_t col_tiles,
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(256) void reduce_kernel(
         uint64_t base = reinterpret_cast<uint64_t>(grad + from * ldg);
         asm("" : "+s"(base));  // keeps the row's address in scalar registers
         const auto *p = reinterpret_cast<const __attribute__((address_space(1))) char *>(base);
-        v[u] = load_packed<TG, W>((const typename TG::store *)(p + offset), W);
+        v[u] = load_packed<TG, W, STREAM>((const typename TG::store *)(p + offset), W);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
