@@ -71,6 +71,8 @@ def _entry(fn):
             raise TypeError("the first argument must be a torch.Tensor")
         if not first.is_cuda:
             raise ValueError("the first argument must be on the GPU")
+        if stream is not None and stream.device != first.device:
+            raise ValueError("stream must be on the tensors' device")
         with torch.cuda.stream(stream) if stream is not None else torch.cuda.device(first.device):
             return fn(first, *args, **kw)
     return call

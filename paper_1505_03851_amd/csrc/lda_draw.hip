@@ -881,9 +881,9 @@ extern "C" const char *lda_status_string(int status) {
       return "unsupported size (K > LDA_MAX_K, N > LDA_MAX_N, a table larger than the entry "
              "point takes, or a K or N the entry point does not take)";
     case LDA_ERR_HIP: return "HIP runtime error";
-    case LDA_ERR_ALIGN: return "a pointer is not aligned (4 bytes; 8 for offsets and workspaces)";
+    case LDA_ERR_ALIGN: return "a pointer is not aligned (its element; 8 bytes for offsets and workspaces)";
     case LDA_ERR_WORKSPACE:
-      return "routing workspace too small, or the route does not belong to these tokens";
+      return "workspace too small, or the route does not belong to these tokens";
     case LDA_ERR_VALUE:
       return "a value out of range (an element type, a probability or a row stride)";
     default: return "unknown status";

@@ -23,7 +23,7 @@ constexpr int kRowsEach = 4;  // rows of one lane, loaded together
 // is 6 or more, so a wavefront's rows are known to scalar registers.
 template <typename T, bool GATHER, bool DROP, bool WIDE>
 __global__ __launch_bounds__(kRowThreads) void rows_kernel(
-    const typename T::store *__restrict__ x, int64_t ldx, const int32_t *__restrict__ word_id,
+    const typename T::store *x, int64_t ldx, const int32_t *__restrict__ word_id,
     typename T::store *out, int64_t ldo, int64_t N, int32_t V, int64_t D, float factor,
     Dropout drop, int lanes_log2, uint32_t col_tiles, int64_t tiles) {
   // What passes the caches by (16,384 rows of 4,096 bfloat16 looked up: 35 us

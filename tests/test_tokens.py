@@ -126,6 +126,8 @@ def test_logits_refusals(lib, st, fn):
         assert fn(lib, rules=_rules(**{name: A + 2})) == st["ALIGN"], name
     assert fn(lib, rules=_rules(history=A, capacity=4, ld_history=4)) == st["NULL"]  # no lengths
     assert fn(lib, rules=_rules(history=A, lengths=A, capacity=-1)) == st["SHAPE"]
+    assert fn(lib, rules=_rules(history=A, lengths=A, capacity=2 ** 30 + 1,
+                                ld_history=2 ** 31)) == st["UNSUPPORTED"]
     for kw in (dict(history=A, lengths=A, capacity=5, ld_history=4), dict(bias=A, ld_bias=39),
                dict(mask=A, ld_mask=1), dict(bias=A, ld_bias=-40)):
         assert fn(lib, rules=_rules(**kw)) == st["VALUE"], kw

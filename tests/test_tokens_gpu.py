@@ -181,7 +181,9 @@ def _ids(kind, N, V, g):
     ("none", 50, 6, 100, 0.0), ("zipf", 4096, 1000, 100, 0.0), ("zipf", 4097, 1023, 33, 0.1),
     ("zipf", 5000, 1024, 129, 0.0), ("holes", 9001, 70_000, 20, 0.0), ("one", 20_000, 2, 17, 0.0),
     ("zipf", 20_000, 50_000, 260, 0.1), ("holes", 70_001, 300, 64, 0.0),
-    ("uniform", 90_000, 2_000_000, 2, 0.0), ("zipf", 3000, 100, 1000, 0.3)])
+    ("uniform", 90_000, 2_000_000, 2, 0.0), ("zipf", 3000, 100, 1000, 0.3),
+    ("zipf", 500, 60, 1003, 0.3), ("one", 70, 2, 131, 0.5), ("uniform", 100, 3_000_000, 5, 0.0),
+    ("zipf", 300, 20, 2055, 0.2)])
 def test_embed_grad(dtype, out, kind, N, V, D, p):
     lda = _lda()
     g = np.random.default_rng(N + V + D)
@@ -203,6 +205,31 @@ def test_embed_grad(dtype, out, kind, N, V, D, p):
     both = lda.embed_grad(*args, out=_gpu(old, out), accumulate=True)
     _close(_np(both), want + old, slack + EPS * np.abs(old) * 2, out, "accumulate")
     assert np.array_equal(_np(both)[tokens == 0], old[tokens == 0])
+
+
+@pytest.mark.parametrize("dtype,D,p", [("bfloat16", 1003, 0.1), ("float16", 96, 0.0)])
+def test_embed_grad_past_the_caches(dtype, D, p):
+    """A gradient of more than 128 MB (read past the caches), against a sum in 64
+    bits on the GPU."""
+    import torch
+    lda = _lda()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(D)
+    N, V = (140 << 20) // (2 * D), 5000
+    ids = (torch.rand(N, device="cuda", generator=g) ** 4 * (V + 2)).int() - 1
+    grad = torch.randn(N, D, device="cuda", generator=g).to(_torch_type(dtype))
+    got = lda.embed_grad(grad, ids, V, 0.5, p, 21, 4)
+    assert torch.equal(got, lda.embed_grad(grad, ids, V, 0.5, p, 21, 4))
+    x = grad.double()
+    if p:
+        x *= _gpu(ref.keep_factor(N, D, p, 21, 4))
+    x *= 0.5
+    row = torch.where((ids >= 0) & (ids < V), ids, V)
+    want = torch.zeros(V + 1, D, dtype=torch.float64, device="cuda").index_add_(0, row, x)[:V]
+    size = torch.zeros(V + 1, D, dtype=torch.float64, device="cuda").index_add_(0, row, x.abs_())[:V]
+    tokens = torch.bincount(row, minlength=V + 1)[:V, None].double()
+    slack = (tokens + 2) * EPS * size
+    _close(_np(got), _np(want), _np(slack), dtype, (dtype, D))
 
 
 def test_embed_grad_of_no_tokens():
@@ -606,7 +633,7 @@ def test_refusals_on_the_gpu():
         lambda: lda.draw_logits(x, i, i), lambda: lda.draw_logits(x, s, s),
         lambda: lda.draw_logits(x, s[:2], i), lambda: lda.draw_logits(x, s, i, f[:3]),
         lambda: lda.draw_logits(x, s, i, min_p=f.half()), lambda: lda.draw_logits(x, s, i, out=(s, f)),
-        lambda: lda.draw_logits(x, s, i, workspace=f),
+        lambda: lda.draw_logits(x, s, i, workspace=f), lambda: lda.draw_logits(x, s, i, out=(i, x)),
     ]
     for k, call in enumerate(bad):
         with pytest.raises((TypeError, ValueError)):
