@@ -16,6 +16,7 @@
 
 #include "elements.hpp"
 #include "keep_bits.hpp"
+#include "wave_ops.hpp"
 
 namespace lda {
 
@@ -138,12 +139,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scan_kernel(uint32_t *hist,
 // Exclusive sum of one value per thread over the workgroup, by thread index.
 __device__ __forceinline__ uint32_t block_exclusive_sum(uint32_t v, uint32_t *wave_sums) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t s = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t o = __shfl_up(s, d);
-    if (lane >= d) s += o;
-  }
+  const uint32_t s = wave_inclusive_sum(v);
   if (lane == 63) wave_sums[wave] = s;
   __syncthreads();
   uint32_t before = 0;
@@ -159,33 +155,54 @@ struct SortLds {
   uint32_t wave_sums[kSortWaves];
 };
 
-// Ranks by one digit of a chunk's tokens, of which a wavefront holds 64
-// kSortEach neighbours, 64 to a round (token `first + 64 r` of the `n` in the
-// chunk): rank[r] is the number of tokens of the same digit before the token in
-// its wavefront, and count[wave][digit] becomes the number in the wavefronts
-// before it.  Returns thread b's tokens of digit b in the whole chunk.
+// A chunk's `n` tokens among the workgroup's threads: a wavefront holds 64
+// rounds(n) neighbours, 64 to a round; token 64 r + the place of its first in the
+// chunk is the lane's of round r.
+__device__ __forceinline__ int rounds_of(int n) { return (n + kSortThreads - 1) / kSortThreads; }
+
+__device__ __forceinline__ int first_of(int rounds) {
+  return (int)(threadIdx.x >> 6) * 64 * rounds + (int)(threadIdx.x & 63);
+}
+
+// Ranks by one digit of a chunk's tokens: rank[r] is the number of tokens of the
+// same digit before the token in its wavefront, and count[wave][digit] becomes
+// the number in the wavefronts before it.  Returns thread b's tokens of digit b in
+// the whole chunk.
 __device__ __forceinline__ uint32_t rank_chunk(SortLds &s, const Token (&k)[kSortEach], int n,
-                                               int first, int shift, int bits,
+                                               int rounds, int shift, int bits,
                                                uint32_t (&rank)[kSortEach]) {
   const int bins = 1 << bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int first = first_of(rounds);
   for (int b = lane; b < bins; b += 64) s.count[wave][b] = 0;
+  // the lanes of a round with the lane's digit, a ballot for each bit
+  uint64_t same[kSortEach];
+#pragma unroll
+  for (int r = 0; r < kSortEach; ++r) {
+    if (r >= rounds) break;
+    const uint32_t digit = k[r].word >> shift;
+    const uint64_t there = __ballot(first + 64 * r < n);
+    uint32_t low = (uint32_t)there, high = (uint32_t)(there >> 32);
+    for (int b = 0; b < bits; ++b) {
+      const uint32_t set = (uint32_t)((int32_t)(digit << (31 - b)) >> 31);  // all ones: bit b is 1
+      const uint64_t with = __ballot(set != 0);
+      low &= ~((uint32_t)with ^ set);
+      high &= ~((uint32_t)(with >> 32) ^ set);
+    }
+    same[r] = (uint64_t)high << 32 | low;
+  }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
   for (int r = 0; r < kSortEach; ++r) {
-    const bool there = first + 64 * r < n;
+    if (r >= rounds) break;
     const uint32_t digit = k[r].word >> shift & (bins - 1);
-    uint64_t same = __ballot(there);
-    for (int b = 0; b < bits; ++b) {
-      const uint64_t set = __ballot(digit >> b & 1);
-      same &= digit >> b & 1 ? set : ~set;
-    }
-    const uint64_t below = same & ((1ull << lane) - 1);
+    const uint64_t below = same[r] & ((1ull << lane) - 1);
     const uint32_t prior = s.count[wave][digit];
     rank[r] = prior + __popcll(below);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    if (there && below == 0) s.count[wave][digit] = (uint16_t)(prior + __popcll(same));
+    if (first + 64 * r < n && below == 0)
+      s.count[wave][digit] = (uint16_t)(prior + __popcll(same[r]));
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
@@ -218,13 +235,13 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(
   const int bins = 1 << bits, wave = threadIdx.x >> 6;
   const int64_t start = (int64_t)blockIdx.x * kSortChunk;
   const int n = N - start < kSortChunk ? (int)(N - start) : kSortChunk;
-  const int first = wave * 64 * kSortEach + (threadIdx.x & 63);
+  const int rounds = rounds_of(n), first = first_of(rounds);
   Token k[kSortEach];
   uint32_t rank[kSortEach];
 #pragma unroll
   for (int r = 0; r < kSortEach; ++r) {
     const int i = first + 64 * r;
-    k[r] = i < n ? load_token(word_id, sorted, start + i, V) : Token{0, 0};
+    k[r] = r < rounds && i < n ? load_token(word_id, sorted, start + i, V) : Token{0, 0};
   }
   // this digit's tokens of all chunks (to place the digit) and of earlier
   // chunks: from sort_scan_kernel, or (few chunks) summed here
@@ -240,13 +257,13 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(
       before += c < blockIdx.x ? h : 0;
     }
   }
-  rank_chunk(s, k, n, first, shift, bits, rank);
+  rank_chunk(s, k, n, rounds, shift, bits, rank);
   const uint32_t place = block_exclusive_sum(all, s.wave_sums);
   if ((int)threadIdx.x < bins) s.base[threadIdx.x] = place + before;
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < kSortEach; ++r) {
-    if (first + 64 * r >= n) break;
+    if (r >= rounds || first + 64 * r >= n) break;
     const uint32_t digit = k[r].word >> shift & (bins - 1);
     out[s.base[digit] + s.count[wave][digit] + rank[r]] = k[r];
   }
@@ -264,17 +281,17 @@ __global__ __launch_bounds__(kSortThreads) void sort_chunk_kernel(
   }
   if (threadIdx.x == 0) *crossing = 0;
   const int wave = threadIdx.x >> 6;
-  const int first = wave * 64 * kSortEach + (threadIdx.x & 63);
+  const int rounds = rounds_of(N), first = first_of(rounds);
   Token k[kSortEach];
   uint32_t rank[kSortEach];
 #pragma unroll
   for (int r = 0; r < kSortEach; ++r) {
     const int i = first + 64 * r;
-    k[r] = i < N ? load_token(word_id, nullptr, i, V) : Token{0, 0};
+    k[r] = r < rounds && i < N ? load_token(word_id, nullptr, i, V) : Token{0, 0};
   }
   for (int pass = 0; pass < passes; ++pass) {
     const int shift = pass * bits;
-    const uint32_t all = rank_chunk(s, k, N, first, shift, bits, rank);
+    const uint32_t all = rank_chunk(s, k, N, rounds, shift, bits, rank);
     const uint32_t place = block_exclusive_sum(all, s.wave_sums);
     if ((int)threadIdx.x < 1 << bits) s.base[threadIdx.x] = place;
     __syncthreads();
@@ -282,7 +299,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_chunk_kernel(
     Token *to = last ? out : tokens;
 #pragma unroll
     for (int r = 0; r < kSortEach; ++r) {
-      if (first + 64 * r >= N) break;
+      if (r >= rounds || first + 64 * r >= N) break;
       const uint32_t digit = k[r].word >> shift & ((1 << bits) - 1);
       to[s.base[digit] + s.count[wave][digit] + rank[r]] = k[r];
     }
@@ -290,7 +307,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_chunk_kernel(
     if (last) break;
 #pragma unroll
     for (int r = 0; r < kSortEach; ++r)
-      if (first + 64 * r < N) k[r] = tokens[first + 64 * r];
+      if (r < rounds && first + 64 * r < N) k[r] = tokens[first + 64 * r];
     __syncthreads();
   }
 }
