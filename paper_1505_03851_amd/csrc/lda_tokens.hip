@@ -104,12 +104,14 @@ GradLayout grad_layout(int64_t N, int32_t V, int32_t D) {
   L.sort_chunks = (N + kSortChunk - 1) / kSortChunk;
   L.width = D > 256 ? 8 : D > 128 ? 4 : D > 64 ? 2 : 1;
   L.col_tiles = (uint32_t)((D + 64 * L.width - 1) / (64 * L.width));
-  // Up to 4,096 wavefronts (4 per SIMD), then longer runs, which leave fewer
-  // parts to join: 32,768 tokens of 2,048 columns 156 us against 166 with 8,192
-  // wavefronts and 160 with 2,048, 1M tokens of 256 columns 198 us against 213
-  // and 363.
+  // A wavefront's time grows with its run, and that of joining a frequent word's
+  // parts with the number of runs, so the run grows with the root of N: 32 chunk^2
+  // holds it.  Measured against half and twice the run: 1,000 tokens 13.6 us
+  // (twice 15.4), 8,000 of 512 columns 32.6 (34.4, 36.5), 32,000 41.9 (47.8),
+  // 32,768 of 2,048 136 (140, 142), 131,072 of 512 74.8 (83.8, 77.4), 1M of 256
+  // 168 (176, 179).
   L.chunk = 8;
-  while (L.chunk < 512 && (N / L.chunk) * L.col_tiles > 4096) L.chunk *= 2;
+  while (L.chunk < 512 && (int64_t)32 * L.chunk * L.chunk < N) L.chunk *= 2;
   L.chunks = (uint32_t)((N + L.chunk - 1) / L.chunk);
   L.ld_part = ((int64_t)D + 7) & ~(int64_t)7;
   size_t at = 0;
