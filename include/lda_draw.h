@@ -516,8 +516,8 @@ int lda_embed(const void *table, int64_t ld_table, const int32_t *word_id, void 
  * all tokens (ld_grad = 0: the gradient of a broadcast).  `workspace`: device
  * memory, 8-byte aligned, of at least lda_embed_grad_workspace_bytes(N, V, D)
  * bytes (LDA_ERR_WORKSPACE), free to use again once the call's kernels are
- * done; not needed if N = 0.  N above LDA_COUNT_MAX_N is LDA_ERR_UNSUPPORTED
- * (and 0 workspace bytes).
+ * done; NULL will do where that is 0 (N up to 128).  N above LDA_COUNT_MAX_N is
+ * LDA_ERR_UNSUPPORTED (and 0 workspace bytes).
  */
 size_t lda_embed_grad_workspace_bytes(int64_t N, int32_t V, int32_t D);
 int lda_embed_grad(const void *grad, int64_t ld_grad, const int32_t *word_id, void *out,

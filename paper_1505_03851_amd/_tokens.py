@@ -185,15 +185,17 @@ def embed_grad(grad, word_id, V: int, scale: float = 1.0, p: float = 0.0, seed: 
         ldo = _rows(out, "out", dev, None, (V, D), True)[2]
         if out.dtype not in (_F32, own) or dtype not in (None, out.dtype):
             raise TypeError("out must be float32 or the gradient's type, and dtype its own")
-    if workspace is None:
-        workspace = grad.new_empty(embed_grad_workspace_bytes(N, V, D), dtype=_U8)
-    else:
+    need = embed_grad_workspace_bytes(N, V, D)
+    if workspace is not None:
         _require(workspace, "workspace", _U8, 1)
         if workspace.get_device() != dev:
             raise ValueError("workspace must be on the tensors' device")
+        need = workspace.numel()
+    elif need:
+        workspace = grad.new_empty(need, dtype=_U8)
     _run("lda_embed_grad", dev, grad.data_ptr(), ld, ids, out.data_ptr(), ldo, N, V, D, DTYPES[own],
          DTYPES[out.dtype], scale, _probability(p), int(seed) & _U64, int(step) & _U32,
-         1 if accumulate else 0, workspace.data_ptr(), workspace.numel())
+         1 if accumulate else 0, None if workspace is None else workspace.data_ptr(), need)
     return out
 
 

@@ -163,12 +163,48 @@ void launch_reduce(const void *grad, int64_t ldg, void *out, int64_t ldo, int32_
                                                        L.col_tiles, g, token, part, crossing);
 }
 
+// N of 1 to kFewTokens: one launch, no workspace (64 tokens of 512 columns: 5 us
+// against 11 with the sort).
+template <typename TG, typename TO, int W>
+void launch_few(const void *grad, int64_t ldg, const int32_t *word_id, void *out, int64_t ldo,
+                int64_t N, int32_t V, int32_t D, float factor, const Dropout &drop,
+                bool accumulate, uint32_t col_tiles, hipStream_t s) {
+  using SG = typename TG::store;
+  using SO = typename TO::store;
+  const unsigned clear_blocks =
+      accumulate ? 0u : grid_of(((int64_t)V + 4 * kFewRows - 1) / (4 * kFewRows));
+  const unsigned grid = clear_blocks + (unsigned)((N * col_tiles + 3) / 4);
+  if (drop.q)
+    few_kernel<TG, TO, W, true><<<grid, 256, 0, s>>>((const SG *)grad, ldg, word_id, (int32_t)N,
+                                                     (SO *)out, ldo, V, D, factor, drop, accumulate,
+                                                     col_tiles, clear_blocks);
+  else
+    few_kernel<TG, TO, W, false><<<grid, 256, 0, s>>>((const SG *)grad, ldg, word_id, (int32_t)N,
+                                                      (SO *)out, ldo, V, D, factor, drop,
+                                                      accumulate, col_tiles, clear_blocks);
+}
+
 template <typename TG, typename TO>
 int launch_grad(const void *grad, int64_t ldg, const int32_t *word_id, void *out, int64_t ldo,
                 int64_t N, int32_t V, int32_t D, double scale, double p, uint64_t seed,
                 uint32_t step, bool accumulate, void *workspace, hipStream_t s) {
   const int64_t size = (int64_t)sizeof(typename TO::store);
   const GradLayout L = grad_layout(N, V, D);
+  float factor;
+  const Dropout drop = make_dropout(p, seed, step, scale, &factor);
+  if (N > 0 && N <= kFewTokens) {
+#define LDA_FEW(W)                                                                               \
+  launch_few<TG, TO, W>(grad, ldg, word_id, out, ldo, N, V, D, factor, drop, accumulate,         \
+                        L.col_tiles, s)
+    switch (L.width) {
+      case 8: LDA_FEW(8); break;
+      case 4: LDA_FEW(4); break;
+      case 2: LDA_FEW(2); break;
+      default: LDA_FEW(1);
+    }
+#undef LDA_FEW
+    return launch_status();
+  }
   const unsigned chunks = (unsigned)L.sort_chunks;
   // each launch of the sort sets its share of the rows to zero
   const bool dense = ldo == D;
@@ -181,8 +217,6 @@ int launch_grad(const void *grad, int64_t ldg, const int32_t *word_id, void *out
     if (extra) clear_kernel<<<extra, kSortThreads, 0, s>>>(clear);
     return launch_status();
   }
-  float factor;
-  const Dropout drop = make_dropout(p, seed, step, scale, &factor);
   char *w = (char *)workspace;
   uint32_t *hist = (uint32_t *)(w + L.hist), *total = (uint32_t *)(w + L.total);
   uint32_t *crossing = (uint32_t *)(w + L.crossing);
@@ -342,7 +376,7 @@ extern "C" int lda_dropout(const void *x, int64_t ld_x, void *out, int64_t ld_ou
 }
 
 extern "C" size_t lda_embed_grad_workspace_bytes(int64_t N, int32_t V, int32_t D) {
-  if (N <= 0 || V <= 0 || D <= 0 || N > LDA_COUNT_MAX_N) return 0;
+  if (N <= kFewTokens || V <= 0 || D <= 0 || N > LDA_COUNT_MAX_N) return 0;
   return grad_layout(N, V, D).bytes;
 }
 
@@ -357,11 +391,12 @@ extern "C" int lda_embed_grad(const void *grad, int64_t ld_grad, const int32_t *
   if (!size || !out_size || !probability(p) || ld_grad < 0 || ld_out < D) return LDA_ERR_VALUE;
   if (out_dtype != LDA_F32 && out_dtype != grad_dtype) return LDA_ERR_UNSUPPORTED;
   if (!out) return LDA_ERR_NULL;
-  if (N > 0 && (!grad || !word_id || !workspace)) return LDA_ERR_NULL;
+  const size_t need = lda_embed_grad_workspace_bytes(N, V, D);
+  if ((N > 0 && (!grad || !word_id)) || (need > 0 && !workspace)) return LDA_ERR_NULL;
   if (!aligned(out, out_size) || !aligned(grad, size) || !aligned(word_id, 4) ||
       !aligned(workspace, 8))
     return LDA_ERR_ALIGN;
-  if (workspace_bytes < lda_embed_grad_workspace_bytes(N, V, D)) return LDA_ERR_WORKSPACE;
+  if (workspace_bytes < need) return LDA_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
 #define LDA_GRAD(TG, TO)                                                                       \
   launch_grad<TG, TO>(grad, ld_grad, word_id, out, ld_out, N, V, D, scale, p, seed, step,      \

@@ -38,21 +38,25 @@ struct ClearShare {
   uint32_t blocks;  // workgroups that sort
 };
 
+// 16 bytes from p on, or n if there are fewer, to zero (past the caches, which a
+// gradient's table is larger than)
+__device__ __forceinline__ void clear_bytes(char *p, int64_t n) {
+  if (n >= 16) {
+    __builtin_nontemporal_store(words4{}, reinterpret_cast<words4_any *>(p));
+  } else {
+    for (int64_t j = 0; j < n; j += 2) *reinterpret_cast<half_any *>(p + j) = 0;
+  }
+}
+
 __device__ __forceinline__ void clear_share(const ClearShare &c) {
   const int64_t units = (c.width + 15) >> 4, all = units * c.rows;
   const int64_t end = all * (c.part + 1) / c.parts;
-  const words4 zero = {};
   for (int64_t i = all * c.part / c.parts + (int64_t)(blockIdx.x - c.blocks) * kSortThreads +
                    threadIdx.x;
        i < end; i += (int64_t)(gridDim.x - c.blocks) * kSortThreads) {
     const int64_t row = c.rows == 1 ? 0 : i / units;
     const int64_t at = (i - row * units) << 4;
-    char *p = c.out + row * c.ld + at;
-    if (c.width - at >= 16) {
-      __builtin_nontemporal_store(zero, reinterpret_cast<words4_any *>(p));
-    } else {
-      for (int64_t j = 0; j < c.width - at; j += 2) *reinterpret_cast<half_any *>(p + j) = 0;
-    }
+    clear_bytes(c.out + row * c.ld + at, c.width - at);
   }
 }
 
@@ -347,6 +351,56 @@ __device__ __forceinline__ void write_row(typename TO::store *out, int64_t ldo, 
   }
 }
 
+// What dropout kept of a row's W columns from `col` on, added to `sum`.
+// `straddles`: some lane's columns lie in two of the mask's groups of eight.
+template <typename TG, int W, bool DROP>
+__device__ __forceinline__ void add_row(const Packed<TG, W> &v, uint32_t row, int32_t col,
+                                        bool straddles, const Dropout &drop, float (&sum)[W]) {
+  float x[W];
+#pragma unroll
+  for (int j = 0; j < W; ++j) x[j] = TG::up(v.v[j]);
+  if (DROP) {
+    const uint32_t group = (uint32_t)col >> 3;
+    const KeepWords k = keep_words(group, row, drop);
+    if (W == 8 && !straddles) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) x[j] = k.kept(j, drop.q) ? x[j] : 0.0f;
+    } else {
+      uint32_t bits = k.bits(drop.q);
+      if (straddles) bits |= keep_words(group + 1, row, drop).bits(drop.q) << 8;
+      bits >>= col & 7;
+#pragma unroll
+      for (int j = 0; j < W; ++j) x[j] = bits >> j & 1 ? x[j] : 0.0f;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < W; ++j) sum[j] += x[j];
+}
+
+// W columns of a row, `offset` bytes into it; the row's address stays in scalar
+// registers.
+template <typename TG, int W, bool STREAM>
+__device__ __forceinline__ Packed<TG, W> load_row(const typename TG::store *grad, int64_t ldg,
+                                                  uint32_t row, uint32_t offset) {
+  uint64_t base = reinterpret_cast<uint64_t>(grad + (int64_t)row * ldg);
+  asm("" : "+s"(base));
+  const auto *p = reinterpret_cast<const __attribute__((address_space(1))) char *>(base);
+  return load_packed<TG, W, STREAM>((const typename TG::store *)(p + offset), W);
+}
+
+// A lane's columns: n of the W from `own` on exist; it reads, without a branch,
+// the W columns from `col` on, which end where they do (in the last lanes some are
+// the lane's before).
+template <int W>
+struct Columns {
+  int32_t own, n, col;
+  __device__ __forceinline__ Columns(uint32_t tile, int32_t D) {
+    own = (int32_t)(tile * 64 + (threadIdx.x & 63)) * W;
+    n = D - own < W ? (D - own > 0 ? D - own : 0) : W;
+    col = own < D - W ? own : D - W;
+  }
+};
+
 // One wavefront: `chunk` sorted positions, 64 W columns.  It reads the words and
 // row numbers of 64 positions at a time, one to a lane; the ends of the words'
 // runs are then a mask in scalar registers, and a row's number a lane read.  U
@@ -366,11 +420,8 @@ __global__ __launch_bounds__(256) void reduce_kernel(
   const uint32_t c = item / col_tiles;
   if (c >= g.chunks) return;
   const uint32_t tile = item - c * col_tiles;
-  // n of the lane's columns exist; it reads, without a branch, the W columns
-  // that end where they do (in the last lanes some of the lane before)
-  const int32_t own = (int32_t)(tile * 64 + lane) * W;
-  const int n = D - own < W ? (D - own > 0 ? D - own : 0) : W;
-  const int32_t col = own < D - W ? own : D - W;
+  const Columns<W> columns(tile, D);
+  const int32_t own = columns.own, n = columns.n, col = columns.col;
   const bool straddles = DROP && D % W != 0 && tile == col_tiles - 1;
   const uint32_t offset = (uint32_t)col * (uint32_t)sizeof(typename TG::store);
   const uint32_t begin = c * g.chunk;
@@ -392,34 +443,14 @@ __global__ __launch_bounds__(256) void reduce_kernel(
       Packed<TG, W> v[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int64_t from = (uint32_t)__builtin_amdgcn_readlane(row, t + u);
-        uint64_t base = reinterpret_cast<uint64_t>(grad + from * ldg);
-        asm("" : "+s"(base));  // keeps the row's address in scalar registers
-        const auto *p = reinterpret_cast<const __attribute__((address_space(1))) char *>(base);
-        v[u] = load_packed<TG, W, STREAM>((const typename TG::store *)(p + offset), W);
+        v[u] = load_row<TG, W, STREAM>(grad, ldg, (uint32_t)__builtin_amdgcn_readlane(row, t + u),
+                                       offset);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (t + u >= count) break;
-        float x[W];
-#pragma unroll
-        for (int j = 0; j < W; ++j) x[j] = TG::up(v[u].v[j]);
-        if (DROP) {
-          const uint32_t r = __builtin_amdgcn_readlane(row, t + u), group = (uint32_t)col >> 3;
-          const KeepWords k = keep_words(group, r, drop);
-          if (W == 8 && !straddles) {
-#pragma unroll
-            for (int j = 0; j < W; ++j) x[j] = k.kept(j, drop.q) ? x[j] : 0.0f;
-          } else {
-            uint32_t bits = k.bits(drop.q);
-            if (straddles) bits |= keep_words(group + 1, r, drop).bits(drop.q) << 8;
-            bits >>= col & 7;
-#pragma unroll
-            for (int j = 0; j < W; ++j) x[j] = bits >> j & 1 ? x[j] : 0.0f;
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < W; ++j) sum[j] += x[j];
+        add_row<TG, W, DROP>(v[u], (uint32_t)__builtin_amdgcn_readlane(row, t + u), col, straddles,
+                             drop, sum);
         if (!(ends >> (t + u) & 1)) continue;
         const uint32_t w = __builtin_amdgcn_readlane(word, t + u);
         const bool goes_on = __builtin_amdgcn_readlane(next, t + u) == w;
@@ -454,9 +485,8 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(
   const uint32_t items = crossing[0] * col_tiles;
   for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
     const uint32_t i = item / col_tiles;
-    const int32_t own = (int32_t)((item - i * col_tiles) * 64 + lane) * W;
-    const int n = D - own < W ? (D - own > 0 ? D - own : 0) : W;
-    const int32_t col = own < D - W ? own : D - W;
+    const Columns<W> columns(item - i * col_tiles, D);
+    const int32_t own = columns.own, n = columns.n, col = columns.col;
     const uint32_t c0 = crossing[1 + i];
     const uint32_t word = token[(c0 + 1) * g.chunk - 1].word;
     // the chunk in which the word ends: the last whose first token is one of it,
@@ -498,6 +528,74 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(
     }
     __syncthreads();
   }
+}
+
+// A few tokens, without a sort: each wavefront has one token and a tile of
+// columns, finds the tokens of the same word by comparing all of them (two to a
+// lane), and, if its own is the first of them, adds them up.  The workgroups
+// before those clear the rows without tokens, kFewRows to a wavefront.
+constexpr int kFewTokens = 128;
+constexpr int kFewRows = 16;
+
+template <typename TG, typename TO, int W, bool DROP>
+__global__ __launch_bounds__(256) void few_kernel(
+    const typename TG::store *__restrict__ grad, int64_t ldg, const int32_t *__restrict__ word_id,
+    int32_t N, typename TO::store *__restrict__ out, int64_t ldo, int32_t V, int32_t D, float factor,
+    Dropout drop, bool accumulate, uint32_t col_tiles, uint32_t clear_blocks) {
+  constexpr int U = 8;
+  const int lane = threadIdx.x & 63;
+  const int32_t low = lane < N ? word_id[lane] : -1;
+  const int32_t high = lane + 64 < N ? word_id[lane + 64] : -1;
+  if (blockIdx.x < clear_blocks) {
+    const int64_t width = (int64_t)D * (int64_t)sizeof(typename TO::store);
+    const uint32_t unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    for (int64_t first = (int64_t)unit * kFewRows; first < V;
+         first += (int64_t)clear_blocks * 4 * kFewRows) {
+      for (int64_t row = first; row < first + kFewRows && row < V; ++row) {
+        if (__ballot(low == row) | __ballot(high == row)) continue;
+        char *p = reinterpret_cast<char *>(out + row * ldo);
+        for (int64_t at = lane * 16; at < width; at += 1024) clear_bytes(p + at, width - at);
+      }
+    }
+    return;
+  }
+  const uint32_t item =
+      __builtin_amdgcn_readfirstlane((blockIdx.x - clear_blocks) * 4 + (threadIdx.x >> 6));
+  const uint32_t t = item / col_tiles, tile = item - t * col_tiles;
+  if (t >= (uint32_t)N) return;
+  const int32_t word = t < 64 ? __builtin_amdgcn_readlane(low, t)
+                              : __builtin_amdgcn_readlane(high, t - 64);
+  if ((uint32_t)word >= (uint32_t)V) return;
+  uint64_t a = __ballot(low == word), b = __ballot(high == word);
+  if ((a ? (uint32_t)__builtin_ctzll(a) : 64 + (uint32_t)__builtin_ctzll(b)) != t) return;
+  const Columns<W> columns(tile, D);
+  const bool straddles = DROP && D % W != 0 && tile == col_tiles - 1;
+  const uint32_t offset = (uint32_t)columns.col * (uint32_t)sizeof(typename TG::store);
+  float sum[W] = {};
+  while (a | b) {
+    Packed<TG, W> v[U];
+    uint32_t row[U];
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (a | b) {
+        row[u] = a ? (uint32_t)__builtin_ctzll(a) : 64 + (uint32_t)__builtin_ctzll(b);
+        if (a)
+          a &= a - 1;
+        else
+          b &= b - 1;
+        n = u + 1;
+      } else {
+        row[u] = t;
+      }
+      v[u] = load_row<TG, W, false>(grad, ldg, row[u], offset);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u < n) add_row<TG, W, DROP>(v[u], row[u], columns.col, straddles, drop, sum);
+    }
+  }
+  write_row<TO, W>(out, ldo, (uint32_t)word, columns.own, columns.n, factor, accumulate, sum);
 }
 
 }  // namespace lda

@@ -61,25 +61,28 @@ def test_embed_grad_refusals(lib, st):
     assert grad(lib, gt=F16, ot=BF16) == st["UNSUPPORTED"]
     for kw in (dict(gt=7), dict(ot=-1), dict(p=1.5), dict(ldg=-16), dict(ldo=8)):
         assert grad(lib, **kw) == st["VALUE"], kw
-    for key in ("g", "ids", "out", "ws"):
+    for key in ("g", "ids", "out"):
         assert grad(lib, **{key: None}) == st["NULL"], key
+    assert grad(lib, N=1000, ws=None) == st["NULL"]
     for key in ("g", "ids", "out"):
         assert grad(lib, **{key: A + 2}) == st["ALIGN"], key
     assert grad(lib, ws=A + 4) == st["ALIGN"]
     assert grad(lib, N=0, out=None) == st["NULL"]  # out is cleared
-    need = lib.lda_embed_grad_workspace_bytes(10, 5, 16)
-    assert need > 0 and grad(lib, size=need - 1) == st["WORKSPACE"]
+    need = lib.lda_embed_grad_workspace_bytes(1000, 5, 16)
+    assert need > 0 and grad(lib, N=1000, size=need - 1) == st["WORKSPACE"]
 
 
 def test_embed_grad_workspace(lib):
     f = lib.lda_embed_grad_workspace_bytes
     for bad in ((0, 5, 16), (-1, 5, 16), (10, 0, 16), (10, 5, 0), (2 ** 31, 5, 16)):
         assert f(*bad) == 0, bad
+    for N in (1, 7, 128):  # a few tokens need none
+        assert f(N, 50_000, 64) == 0
     last = 0
-    for N in (1, 7, 4096, 4097, 70_000, 1 << 20, 2 ** 31 - 1):
+    for N in (129, 1000, 4096, 4097, 70_000, 1 << 20, 2 ** 31 - 1):
         assert f(N, 50_000, 64) >= max(last, 16 * N)
         last = f(N, 50_000, 64)
-    assert f(10, 2 ** 31 - 1, 8) > 0
+    assert f(1000, 2 ** 31 - 1, 8) > 0
 
 
 def test_dropout_refusals(lib, st):

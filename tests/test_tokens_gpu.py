@@ -183,7 +183,9 @@ def _ids(kind, N, V, g):
     ("zipf", 20_000, 50_000, 260, 0.1), ("holes", 70_001, 300, 64, 0.0),
     ("uniform", 90_000, 2_000_000, 2, 0.0), ("zipf", 3000, 100, 1000, 0.3),
     ("zipf", 500, 60, 1003, 0.3), ("one", 70, 2, 131, 0.5), ("uniform", 100, 3_000_000, 5, 0.0),
-    ("zipf", 300, 20, 2055, 0.2)])
+    ("zipf", 300, 20, 2055, 0.2), ("one", 64, 40, 65, 0.0), ("one", 128, 3, 700, 0.2),
+    ("holes", 128, 100, 33, 0.0), ("zipf", 129, 50, 260, 0.1), ("uniform", 65, 5000, 1003, 0.3),
+    ("none", 128, 17, 9, 0.0)])
 def test_embed_grad(dtype, out, kind, N, V, D, p):
     lda = _lda()
     g = np.random.default_rng(N + V + D)
@@ -640,7 +642,8 @@ def test_refusals_on_the_gpu():
             call()
             print("not refused:", k)
     small = torch.empty(8, dtype=torch.uint8, device="cuda")
-    for call in (lambda: lda.embed_grad(x, i, 9, workspace=small),
+    many = torch.zeros(200, dtype=torch.int32, device="cuda")
+    for call in (lambda: lda.embed_grad(x[:1].expand(200, 40), many, 9, workspace=small),
                  lambda: lda.draw_logits(x, s, i, workspace=small)):
         with pytest.raises(lda.LdaError) as e:
             call()
