@@ -114,7 +114,6 @@ def draw(x, temperature, min_p, seed, position):
     if top == -np.inf:
         return -1, 0.0, np.inf
     if not temperature > 0:
-        order = np.sort(x)
         return int(np.argmax(x)), 1.0, np.inf
     if np.isposinf(top):
         w = (x == top).astype(np.float64)

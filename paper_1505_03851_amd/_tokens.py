@@ -61,20 +61,23 @@ def bind(lib: ctypes.CDLL) -> None:
 def _entry(fn):
     """``fn`` in the context of its first tensor's device, and of the stream the
     call is given: what it allocates and launches belongs to that stream."""
+    name = fn.__code__.co_varnames[0]
+
     @functools.wraps(fn)
-    def call(first, *args, stream=None, **kw):
+    def call(*args, stream=None, **kw):
+        first = args[0] if args else kw.get(name)
         if type(first) is _Tensor and stream is None:
             dev = first.get_device()
             if dev >= 0 and dev == _current_device():
-                return fn(first, *args, **kw)
+                return fn(*args, **kw)
         if not isinstance(first, _Tensor):
-            raise TypeError("the first argument must be a torch.Tensor")
+            raise TypeError(f"{name} must be a torch.Tensor")
         if not first.is_cuda:
-            raise ValueError("the first argument must be on the GPU")
+            raise ValueError(f"{name} must be on the GPU")
         if stream is not None and stream.device != first.device:
             raise ValueError("stream must be on the tensors' device")
         with torch.cuda.stream(stream) if stream is not None else torch.cuda.device(first.device):
-            return fn(first, *args, **kw)
+            return fn(*args, **kw)
     return call
 
 

@@ -651,6 +651,20 @@ def test_refusals_on_the_gpu():
     torch.cuda.synchronize()
 
 
+def test_arguments_by_name():
+    import torch
+    lda = _lda()
+    x = torch.randn(200, 40, device="cuda")
+    i = torch.arange(200, dtype=torch.int32, device="cuda") % 9
+    assert torch.equal(lda.embed(word_id=i, table=x), x[i.long()])
+    assert torch.equal(lda.embed_grad(V=9, word_id=i, grad=x), lda.embed_grad(x, i, 9))
+    assert torch.equal(lda.dropout(p=0.5, seed=3, x=x), lda.dropout(x, 0.5, 3))
+    assert torch.equal(lda.penalise_logits(logits=x), x)
+    z, p = lda.draw_logits(position=i, seed=i.long(), logits=x)
+    z2, p2 = lda.draw_logits(x, i.long(), i)
+    assert torch.equal(z, z2) and torch.equal(p, p2)
+
+
 def test_past_32_bits():
     """Tables, gradients and logits of more than 2^32 elements: the last rows."""
     import torch
@@ -665,6 +679,11 @@ def test_past_32_bits():
     out = lda.embed_grad(got, ids, V, out=table)  # overwrites the table
     assert torch.equal(out[-1].float(), (torch.arange(D, device="cuda") % 128).float())
     assert not out[1:-1].any() and not out[0].any()
+    many = torch.full((300,), V - 1, dtype=torch.int32, device="cuda")  # through the sort
+    many[::2] = 7
+    lda.embed_grad(got[:1].expand(300, D), many, V, out=out)
+    assert torch.equal(out[-1], ((torch.arange(D, device="cuda") % 128) * 75.0).bfloat16())
+    assert torch.equal(out[7], out[-1]) and not out[8:-1].any() and not out[:7].any()
     del table, out
     torch.cuda.empty_cache()
     y = torch.ones(V, D, dtype=torch.float16, device="cuda")
