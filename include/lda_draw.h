@@ -589,7 +589,8 @@ int lda_penalise_logits(const void *logits, int64_t ld_logits, void *out, int64_
  * of the group's weights), its token the one of that group with the smallest
  * E(v, 3) / w_v, the lowest among equals: an exact draw by the weights.
  * `workspace`: device memory, 8-byte aligned, at least
- * lda_draw_logits_workspace_bytes(B, V) bytes (LDA_ERR_WORKSPACE).
+ * lda_draw_logits_workspace_bytes(B, V) bytes (LDA_ERR_WORKSPACE); NULL will do
+ * where that is 0 (V up to 32,768).
  */
 size_t lda_draw_logits_workspace_bytes(int64_t B, int32_t V);
 int lda_draw_logits(const void *logits, int64_t ld_logits, int64_t B, int32_t V, int32_t dtype,

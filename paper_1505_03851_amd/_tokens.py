@@ -330,12 +330,14 @@ def draw_logits(logits, seed, position, temperature=None, min_p=None, history=No
     else:
         z, prob = out
         to = _vector(z, "out[0]", _I32, B, dev), _vector(prob, "out[1]", _F32, B, dev)
-    if workspace is None:
-        workspace = logits.new_empty(draw_logits_workspace_bytes(B, V), dtype=_U8)
-    else:
+    need = draw_logits_workspace_bytes(B, V)
+    if workspace is not None:
         _require(workspace, "workspace", _U8, 1)
         if workspace.get_device() != dev:
             raise ValueError("workspace must be on the tensors' device")
+        need = workspace.numel()
+    elif need:
+        workspace = logits.new_empty(need, dtype=_U8)
     _run("lda_draw_logits", dev, logits.data_ptr(), ld, B, V, DTYPES[logits.dtype], rules, heat,
-         floor, seeds, places, *to, workspace.data_ptr(), workspace.numel())
+         floor, seeds, places, *to, None if workspace is None else workspace.data_ptr(), need)
     return z, prob

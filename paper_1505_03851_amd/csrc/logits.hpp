@@ -34,7 +34,8 @@
 // move; 17 us with no rules, 23 without the history); 64 draws from 100,000 with
 // a history of up to 8,192, bias, masks, temperatures and floors 36 us (17 the
 // sums, 12 the sums above the floors, 9 the races); 256 plain draws from 49,999
-// floats 18.5 us (13 and 7); one draw from 32,768 10 us on the GPU, 18 a call.
+// floats 18.5 us (13 and 7); one draw from 32,768, in one launch, 11.5 us on the
+// GPU and 14 a call.
 #pragma once
 
 #include "elements.hpp"
@@ -48,6 +49,7 @@ constexpr int kSteps = kGroup / 512;
 constexpr int kGroupWaves = 8;      // groups of a workgroup, at most
 constexpr int kDrawThreads = 1024;  // of a workgroup that draws: one for each token of a group
 constexpr int kDrawWaves = kDrawThreads / 64;
+constexpr int kShortGroups = 2 * kDrawWaves;  // of a row that one launch draws from
 constexpr uint32_t kSeen = 0x80000000u;
 
 struct Rules {
@@ -416,6 +418,27 @@ __global__ __launch_bounds__(64 * kGroupWaves) void group_kernel(
   }
 }
 
+// The last step of a workgroup that has a token to each thread: the one with the
+// smallest key `v` is drawn, and its share of `total` its probability.
+__device__ __forceinline__ void choose_token(float v, float x, float top, float total,
+                                             uint32_t token, const DrawRow &d, First *firsts,
+                                             int32_t *z, float *prob) {
+  const int lane = threadIdx.x & 63;
+  const First of_wave = wave_first(First{__builtin_bit_cast(uint32_t, v), threadIdx.x});
+  if (lane == 0) firsts[threadIdx.x >> 6] = of_wave;
+  __syncthreads();
+  const First won = wave_first(lane < kDrawWaves ? firsts[lane] : First{0xFFFFFFFFu, 0xFFFFFFFFu});
+  if (threadIdx.x != won.index) return;
+  *z = (int32_t)token;
+  // the exponent in 64 bits: in 32 its rounding would be the largest error
+  const double y = ((double)x - (double)top) / (double)d.temperature * 1.4426950408889634;
+  const double whole = rint(y);
+  const float share =
+      x == top ? 1.0f
+               : ldexpf(__builtin_amdgcn_exp2f((float)(y - whole)), (int)fmax(whole, -1000.0));
+  *prob = d.greedy ? 1.0f : share / total;
+}
+
 // One workgroup per row: the groups' race (by every wavefront for itself), then
 // the race of the group's tokens, one to a thread.
 template <typename T>
@@ -427,7 +450,7 @@ __global__ __launch_bounds__(kDrawThreads) void draw_kernel(
     float *__restrict__ prob) {
   __shared__ uint32_t count[kGroup];
   __shared__ First firsts[kDrawWaves];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
   for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
     const DrawRow d = draw_row(temperature, min_p, b);
     const GroupSum *mine = groups + b * per_row;
@@ -488,20 +511,104 @@ __global__ __launch_bounds__(kDrawThreads) void draw_kernel(
       v = x == top ? 0.0f : INFINITY;
     else if (x == x && x != -INFINITY && above_floor(x, top, d))
       v = own / weight(x, group_top, d);
-    const First of_wave = wave_first(First{__builtin_bit_cast(uint32_t, v), threadIdx.x});
-    if (lane == 0) firsts[wave] = of_wave;
+    choose_token(v, x, top, total, (uint32_t)token, d, firsts, z + b, prob + b);
     __syncthreads();
-    const First won = wave_first(lane < kDrawWaves ? firsts[lane] : First{0xFFFFFFFFu, 0xFFFFFFFFu});
-    if (threadIdx.x == won.index) {
-      z[b] = (int32_t)token;
-      // the exponent in 64 bits: in 32 its rounding would be the largest error
-      const double y = ((double)x - (double)top) / (double)d.temperature * 1.4426950408889634;
-      const double whole = rint(y);
-      const float share =
-          x == top ? 1.0f
-                   : ldexpf(__builtin_amdgcn_exp2f((float)(y - whole)), (int)fmax(whole, -1000.0));
-      prob[b] = d.greedy ? 1.0f : share / total;
+  }
+}
+
+// A short row (up to R kDrawWaves groups) in one workgroup and one launch: R groups
+// to a wavefront, whose logits under the rules stay in registers for the floor's
+// second sums and for the race of the tokens.
+template <typename T, int R>
+__global__ __launch_bounds__(kDrawThreads) void short_draw_kernel(
+    const typename T::store *__restrict__ logits, int64_t ld, int64_t B, int64_t V, Rules rules,
+    const float *__restrict__ temperature, const float *__restrict__ min_p,
+    const int64_t *__restrict__ seed, const int32_t *__restrict__ position, int32_t *__restrict__ z,
+    float *__restrict__ prob) {
+  constexpr int kGroups = R * kDrawWaves;
+  static_assert(kGroups <= 64, "a group to a lane");
+  extern __shared__ uint32_t lds[];  // the counts of all groups, where there is a history
+  __shared__ GroupSum sums[kGroups];
+  __shared__ float again[kGroups], winners[kGroup];
+  __shared__ First firsts[kDrawWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
+    const RowRules r = row_rules(rules, b);
+    const History h = row_history(rules, b);
+    const Tokens ahead = load_tokens(h);
+    Group<T> q[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      load_group<T>(logits + b * ld, (int64_t)(i * kDrawWaves + wave) * kGroup, V, r, q[i]);
+    const DrawRow d = draw_row(temperature, min_p, b);
+    const uint64_t s = (uint64_t)seed[b];
+    const uint32_t pos = (uint32_t)position[b];
+    if (h.size) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) clear_counts(lds + (i * kDrawWaves + wave) * kGroup);
+      __syncthreads();
+      count_history(h, ahead, 0, kGroups * kGroup, lds);
+      __syncthreads();
     }
+    float x[R][kSteps][8];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int g = i * kDrawWaves + wave;
+      const int64_t first = (int64_t)g * kGroup;
+      rule_group<T>(q[i], first, h.size ? lds + g * kGroup : nullptr, r, x[i]);
+      const GroupSum sum = group_sum<false>(x[i], q[i].n, first + kGroup <= V, 0.0f, d);
+      if (lane == 0) sums[g] = sum;
+    }
+    // a lane's group, whose variate does not wait for its sum
+    const float own = lane < kGroups ? variate(lane, pos, 2u, s) : 0.0f;
+    __syncthreads();
+    GroupSum mine = lane < kGroups ? sums[lane] : GroupSum{-INFINITY, 0.0f};
+    const float top = wave_max(mine.top);
+    if (top == -INFINITY) {  // nothing may be drawn
+      if (threadIdx.x == 0) {
+        z[b] = -1;
+        prob[b] = 0.0f;
+      }
+      __syncthreads();
+      continue;
+    }
+    if (!d.greedy && d.floor != -INFINITY) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int g = i * kDrawWaves + wave;
+        float sum = 0.0f;
+        if (above_floor(sums[g].top, top, d))
+          sum = group_sum<true>(x[i], q[i].n, true, top, d).sum;
+        if (lane == 0) again[g] = sum;
+      }
+      __syncthreads();
+      mine.sum = lane < kGroups ? again[lane] : 0.0f;
+    }
+    const float w = mine.top == -INFINITY || d.greedy ? 0.0f : weight(mine.top, top, d) * mine.sum;
+    const float total = wave_sum(w);
+    const float key = d.greedy ? (mine.top == top ? 0.0f : INFINITY) : own / w;
+    const uint32_t group =
+        wave_first(First{lane < kGroups ? __builtin_bit_cast(uint32_t, key) : 0xFFFFFFFFu,
+                         (uint32_t)lane}).index;
+    const uint32_t token = group * kGroup + threadIdx.x;
+    const float token_own = d.greedy ? 0.0f : variate(token, pos, 3u, s);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if ((uint32_t)(i * kDrawWaves + wave) != group) continue;
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) winners[k * 512 + lane * 8 + j] = x[i][k][j];
+    }
+    const float group_top = sums[group].top;
+    __syncthreads();
+    const float mine_x = winners[threadIdx.x];
+    float v = INFINITY;
+    if (d.greedy)
+      v = mine_x == top ? 0.0f : INFINITY;
+    else if (mine_x != -INFINITY && above_floor(mine_x, top, d))
+      v = token_own / weight(mine_x, group_top, d);
+    choose_token(v, mine_x, top, total, token, d, firsts, z + b, prob + b);
     __syncthreads();
   }
 }

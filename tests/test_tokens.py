@@ -139,15 +139,17 @@ def test_logits_refusals(lib, st, fn):
 def test_logits_own_refusals(lib, st):
     assert penalise(lib, ldo=39) == st["VALUE"]
     assert penalise(lib, out=None) == st["NULL"]
-    for key in ("seed", "pos", "z", "prob", "ws"):
+    for key in ("seed", "pos", "z", "prob"):
         assert draw(lib, **{key: None}) == st["NULL"], key
+    assert draw(lib, V=40_000, ld=40_000, ws=None) == st["NULL"]
     for key in ("t", "m", "pos", "z", "prob"):
         assert draw(lib, **{key: A + 2}) == st["ALIGN"], key
     for key in ("seed", "ws"):
         assert draw(lib, **{key: A + 4}) == st["ALIGN"], key
-    need = lib.lda_draw_logits_workspace_bytes(3, 40)
-    assert need == 24 and draw(lib, size=need - 1) == st["WORKSPACE"]
-    assert lib.lda_draw_logits_workspace_bytes(2, 1025) == 32
+    need = lib.lda_draw_logits_workspace_bytes(3, 40_000)
+    assert need == 960 and draw(lib, V=40_000, ld=40_000, size=need - 1) == st["WORKSPACE"]
+    assert lib.lda_draw_logits_workspace_bytes(2, 32_769) == 528
+    assert lib.lda_draw_logits_workspace_bytes(2, 32_768) == 0  # short rows need none
     for bad in ((0, 5), (3, 0), (2 ** 31, 5)):
         assert lib.lda_draw_logits_workspace_bytes(*bad) == 0
 

@@ -328,7 +328,7 @@ def _gpu_rules(rules):
     return out
 
 
-SHAPES = [(1, 1, 0), (1, 7, 3), (3, 31, 1), (7, 300, 40), (6, 1023, 100), (2, 1024, 0), (8, 1025, 17),
+SHAPES = [(1, 1, 0), (3, 16_384, 50), (5, 16_385, 2000), (6, 32_768, 9000), (2, 32_769, 10), (1, 7, 3), (3, 31, 1), (7, 300, 40), (6, 1023, 100), (2, 1024, 0), (8, 1025, 17),
           (5, 2500, 700), (9, 8193, 300), (300, 1500, 20), (4, 33_001, 5000), (7, 50_000, 64)]
 
 
@@ -414,7 +414,8 @@ def test_draw(dtype, B, V, cap):
         _check_draw(_case(B, V, cap, s, dtype=dtype), dtype, t, m, seed, position, "rules")
 
 
-def test_draw_special_rows():
+@pytest.mark.parametrize("wide", [0, 20_000, 40_000])
+def test_draw_special_rows(wide):
     """Greedy ties take the lowest token; NaN is never drawn; +inf shares the
     draw; nothing to draw gives -1; extreme temperatures and floors."""
     V = 2500
@@ -445,6 +446,7 @@ def test_draw_special_rows():
     row({2: 1.0, 3: 1.0, 4: 0.9}, m=1.0, fill=0.0)          # only the likeliest
     row({2: 1.0, 3: 1.0, 4: 0.9}, m=7.0, fill=0.0)
     row({2: 60.0}, m=1e-30, fill=0.0)
+    rows = [np.concatenate([x, np.full(wide, -np.inf)]) for x in rows]
     n = 40
     x = np.repeat(np.array(rows), n, 0)
     t, m = np.repeat(temps, n), np.repeat(floors, n)
@@ -644,7 +646,8 @@ def test_refusals_on_the_gpu():
     small = torch.empty(8, dtype=torch.uint8, device="cuda")
     many = torch.zeros(200, dtype=torch.int32, device="cuda")
     for call in (lambda: lda.embed_grad(x[:1].expand(200, 40), many, 9, workspace=small),
-                 lambda: lda.draw_logits(x, s, i, workspace=small)):
+                 lambda: lda.draw_logits(x[:, :1].expand(4, 40).repeat(1, 1000), s, i,
+                                         workspace=small)):
         with pytest.raises(lda.LdaError) as e:
             call()
         assert e.value.status == lda.STATUS["LDA_ERR_WORKSPACE"]
