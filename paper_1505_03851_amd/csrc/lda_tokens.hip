@@ -25,6 +25,8 @@ namespace {
 
 // A launch holds fewer than 2^32 work-items; kernels stride over the rest.
 constexpr int64_t kMaxBlocks = 1 << 20;
+// 16-byte units of a table (64 MB) from which clearing it bounds a call.
+constexpr int64_t kClearApart = (64 << 20) / 16;
 
 unsigned grid_of(int64_t tiles) {
   return (unsigned)(tiles < 1 ? 1 : tiles < kMaxBlocks ? tiles : kMaxBlocks);
@@ -168,20 +170,23 @@ void launch_reduce(const void *grad, int64_t ldg, void *out, int64_t ldo, int32_
 template <typename TG, typename TO, int W>
 void launch_few(const void *grad, int64_t ldg, const int32_t *word_id, void *out, int64_t ldo,
                 int64_t N, int32_t V, int32_t D, float factor, const Dropout &drop,
-                bool accumulate, uint32_t col_tiles, hipStream_t s) {
+                bool accumulate, bool clear, uint32_t col_tiles, hipStream_t s) {
   using SG = typename TG::store;
   using SO = typename TO::store;
-  const unsigned clear_blocks =
-      accumulate ? 0u : grid_of(((int64_t)V + 4 * kFewRows - 1) / (4 * kFewRows));
+  // about 4 KB of rows to a wavefront, so that the workgroups, which start in their
+  // order, write one stretch after another
+  const int64_t width = (int64_t)sizeof(SO) * D;
+  const int32_t rows = width >= 4096 ? 1 : width < 256 ? 16 : (int32_t)(4096 / width);
+  const unsigned clear_blocks = clear ? grid_of(((int64_t)V + 4 * rows - 1) / (4 * rows)) : 0u;
   const unsigned grid = clear_blocks + (unsigned)((N * col_tiles + 3) / 4);
   if (drop.q)
     few_kernel<TG, TO, W, true><<<grid, 256, 0, s>>>((const SG *)grad, ldg, word_id, (int32_t)N,
                                                      (SO *)out, ldo, V, D, factor, drop, accumulate,
-                                                     col_tiles, clear_blocks);
+                                                     col_tiles, clear_blocks, rows);
   else
     few_kernel<TG, TO, W, false><<<grid, 256, 0, s>>>((const SG *)grad, ldg, word_id, (int32_t)N,
                                                       (SO *)out, ldo, V, D, factor, drop,
-                                                      accumulate, col_tiles, clear_blocks);
+                                                      accumulate, col_tiles, clear_blocks, rows);
 }
 
 template <typename TG, typename TO>
@@ -192,10 +197,27 @@ int launch_grad(const void *grad, int64_t ldg, const int32_t *word_id, void *out
   const GradLayout L = grad_layout(N, V, D);
   float factor;
   const Dropout drop = make_dropout(p, seed, step, scale, &factor);
+  const unsigned chunks = (unsigned)L.sort_chunks;
+  // each launch of the sort sets its share of the rows to zero
+  const bool dense = ldo == D;
+  ClearShare clear{(char *)out, size * ldo, size * D * (dense ? (int64_t)V : 1),
+                   dense ? 1 : (int64_t)V, 0, N == 0 || chunks == 1 ? 1u : 2u * L.passes,
+                   N <= kFewTokens ? 0u : chunks};
+  const int64_t units = (clear.width + 15) / 16 * clear.rows / clear.parts;
+  const int64_t clear_blocks = accumulate ? 0 : (units + kSortThreads - 1) / kSortThreads;
+  // A share of more than 64 MB in workgroups of 16 KB each, which start in their
+  // order and so write one stretch after another (512 MB 113 us against 129, 410 in
+  // four shares 127 against 134); a smaller one in 1,024 that stride through it
+  // (205 MB in four shares 84 against 87, 64 MB 20.9 against 23.5).
+  const int64_t most = units > kClearApart ? kMaxBlocks : 1024;
+  const unsigned extra = (unsigned)(clear_blocks < most ? clear_blocks : most);
   if (N > 0 && N <= kFewTokens) {
+    // a large table is cleared by a launch of its own, as one stretch
+    const bool apart = !accumulate && units > kClearApart;
+    if (apart) clear_kernel<<<extra, kSortThreads, 0, s>>>(clear);
 #define LDA_FEW(W)                                                                               \
   launch_few<TG, TO, W>(grad, ldg, word_id, out, ldo, N, V, D, factor, drop, accumulate,         \
-                        L.col_tiles, s)
+                        !accumulate && !apart, L.col_tiles, s)
     switch (L.width) {
       case 8: LDA_FEW(8); break;
       case 4: LDA_FEW(4); break;
@@ -205,14 +227,6 @@ int launch_grad(const void *grad, int64_t ldg, const int32_t *word_id, void *out
 #undef LDA_FEW
     return launch_status();
   }
-  const unsigned chunks = (unsigned)L.sort_chunks;
-  // each launch of the sort sets its share of the rows to zero
-  const bool dense = ldo == D;
-  ClearShare clear{(char *)out, size * ldo, size * D * (dense ? (int64_t)V : 1),
-                   dense ? 1 : (int64_t)V, 0, N == 0 || chunks == 1 ? 1u : 2u * L.passes, chunks};
-  const int64_t units = (clear.width + 15) / 16 * clear.rows / clear.parts;
-  const int64_t clear_blocks = accumulate ? 0 : (units + kSortThreads - 1) / kSortThreads;
-  const unsigned extra = (unsigned)(clear_blocks < 1024 ? clear_blocks : 1024);
   if (N == 0) {
     if (extra) clear_kernel<<<extra, kSortThreads, 0, s>>>(clear);
     return launch_status();

@@ -16,9 +16,10 @@
 // Measured on MI355X: 1M tokens of 256 bfloat16 over 32,768 Zipf words 167 us (3.3
 // TB/s of the 558 MB that have to move): the sums 115 us at 4.7 TB/s, bound by
 // memory, the sort 42, a chain of six launches, and the joins 11; 32,768 tokens
-// of 2,048 bfloat16 into 50,000 float rows, dropped out, 134 us (4.1 TB/s): 82 of
-// clearing at 5.0 TB/s with the sort under it, 47 of sums; 4,096 tokens of 1,000
-// floats 23 us, three launches of 4 to 10 us, each a few round trips.
+// of 2,048 bfloat16 into 50,000 float rows, dropped out, 129 us (4.2 TB/s): clearing
+// at 5.0 TB/s with the sort under it, then 47 of sums; 4,096 tokens of 1,000
+// floats 23 us, three launches of 4 to 10 us, each a few round trips; up to 128
+// tokens of 512 columns into 10,000 rows 5 us, one into 400 MB 64 (6.3 TB/s).
 #pragma once
 
 #include "elements.hpp"
@@ -47,8 +48,8 @@ struct ClearShare {
 
 // 16 bytes from p on, or n if there are fewer, to zero.  STREAM: past the caches,
 // so that the gradient's reads do not wait for them to write zeros back (32,768
-// tokens of 2,048 columns into 50,000 float rows: 133 us against 140; without
-// much to read afterwards, 1 token of 1,000 into 100,000, 94 against 79).
+// tokens of 2,048 columns into 50,000 float rows: 127 us against 140; the rows of
+// few_kernel, one by one and with little to read, 94 against 79).
 template <bool STREAM>
 __device__ __forceinline__ void clear_bytes(char *p, int64_t n) {
   auto *memory = reinterpret_cast<words4_any *>(p);
@@ -546,15 +547,14 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(
 // A few tokens, without a sort: each wavefront has one token and a tile of
 // columns, finds the tokens of the same word by comparing all of them (two to a
 // lane), and, if its own is the first of them, adds them up.  The workgroups
-// before those clear the rows without tokens, kFewRows to a wavefront.
+// before those clear the rows without tokens, `rows` to a wavefront.
 constexpr int kFewTokens = 128;
-constexpr int kFewRows = 16;
 
 template <typename TG, typename TO, int W, bool DROP>
 __global__ __launch_bounds__(256) void few_kernel(
     const typename TG::store *__restrict__ grad, int64_t ldg, const int32_t *__restrict__ word_id,
     int32_t N, typename TO::store *__restrict__ out, int64_t ldo, int32_t V, int32_t D, float factor,
-    Dropout drop, bool accumulate, uint32_t col_tiles, uint32_t clear_blocks) {
+    Dropout drop, bool accumulate, uint32_t col_tiles, uint32_t clear_blocks, int32_t rows) {
   constexpr int U = 8;
   const int lane = threadIdx.x & 63;
   const int32_t low = lane < N ? word_id[lane] : -1;
@@ -562,9 +562,8 @@ __global__ __launch_bounds__(256) void few_kernel(
   if (blockIdx.x < clear_blocks) {
     const int64_t width = (int64_t)D * (int64_t)sizeof(typename TO::store);
     const uint32_t unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    for (int64_t first = (int64_t)unit * kFewRows; first < V;
-         first += (int64_t)clear_blocks * 4 * kFewRows) {
-      for (int64_t row = first; row < first + kFewRows && row < V; ++row) {
+    for (int64_t first = (int64_t)unit * rows; first < V; first += (int64_t)clear_blocks * 4 * rows) {
+      for (int64_t row = first; row < first + rows && row < V; ++row) {
         if (__ballot(low == row) | __ballot(high == row)) continue;
         char *p = reinterpret_cast<char *>(out + row * ldo);
         for (int64_t at = lane * 16; at < width; at += 1024) clear_bytes<false>(p + at, width - at);

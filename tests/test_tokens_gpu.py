@@ -150,6 +150,12 @@ def test_rows_at_any_distance(dtype, pad, at):
     lda.embed_grad(out, ids, V, 2.0, 0.2, 5, 6, out=total)
     assert torch.equal(total, lda.embed_grad(want, ids, V, 2.0, 0.2, 5, 6))
     assert int(torch.isfinite(buf).sum()) == V * D
+    many = ids.repeat(7)  # through the sort, into rows apart and into one stretch
+    wide_many, _ = _wide(_np(want).repeat(7, 0), dtype, pad, at)
+    total, buf = _wide(np.zeros((V, D)), dtype, pad, at)
+    lda.embed_grad(wide_many, many, V, out=total)
+    assert torch.equal(total, lda.embed_grad(wide_many.contiguous(), many, V))
+    assert int(torch.isfinite(buf).sum()) == V * D
     # one row for all
     one = dense[:1].expand(N, D)
     assert torch.equal(lda.embed_grad(one, ids, V), lda.embed_grad(one.contiguous(), ids, V))
