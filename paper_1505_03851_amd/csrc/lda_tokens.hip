@@ -7,7 +7,7 @@
 // lda_penalise_logits  penalties for repeated tokens, biases, masks.
 // lda_draw_logits      one token per row of logits under those rules.
 //
-// Device code: elements.hpp (element types), keep_bits.hpp (the dropout
+// Device code: elements.hpp (element types), wave_ops.hpp, keep_bits.hpp (the dropout
 // mask), token_rows.hpp, token_grad.hpp, logits.hpp.
 #include <hip/hip_runtime.h>
 
