@@ -203,7 +203,9 @@ int launch_grad(const void *grad, int64_t ldg, const int32_t *word_id, void *out
   ClearShare clear{(char *)out, size * ldo, size * D * (dense ? (int64_t)V : 1),
                    dense ? 1 : (int64_t)V, 0, N == 0 || chunks == 1 ? 1u : 2u * L.passes,
                    N <= kFewTokens ? 0u : chunks};
-  const int64_t units = (clear.width + 15) / 16 * clear.rows / clear.parts;
+  // (a share of a table of a few bytes is at least one unit, so that every launch has
+  // a workgroup that clears: which of them the unit falls to, clear_share decides)
+  const int64_t units = ((clear.width + 15) / 16 * clear.rows + clear.parts - 1) / clear.parts;
   const int64_t clear_blocks = accumulate ? 0 : (units + kSortThreads - 1) / kSortThreads;
   // A share of more than 64 MB in workgroups of 16 KB each, which start in their
   // order and so write one stretch after another (512 MB 113 us against 129, 410 in

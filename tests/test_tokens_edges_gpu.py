@@ -1,0 +1,38 @@
+"""The token operators at the edges of their ranges, against the oracle in 64
+bits or against the same call away from the edge.  Tolerances are those of
+test_tokens_gpu.py."""
+import numpy as np
+import pytest
+
+from oracle import tokens as ref
+from test_tokens_gpu import EPS, TYPES, _close, _gpu, _lda, _np, _rounded, _torch_type
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- the embedding's gradient: tables smaller than a sorting launch's shares
+
+
+@pytest.mark.parametrize("dtype,V,D", [
+    ("float32", 1, 1), ("float32", 4, 1), ("float32", 1, 4), ("float32", 2, 2), ("float32", 5, 1),
+    ("bfloat16", 8, 1), ("bfloat16", 2, 4), ("bfloat16", 3, 3), ("float16", 1, 8), ("float16", 1, 1)])
+@pytest.mark.parametrize("N", [200, 4096, 4097, 5000, 70_001])
+def test_embed_grad_into_a_few_bytes(dtype, V, D, N):
+    """Rows without tokens are zero, whatever the memory held."""
+    import torch
+    lda = _lda()
+    g = np.random.default_rng([V, D, N])
+    grad = _rounded(g.normal(0, 1, (N, D)), dtype)
+    # no token of any word; of every word but the middle one; of every word
+    every = g.integers(0, V, N).astype(np.int32)
+    for ids in (np.full(N, -1, dtype=np.int32), np.where(every == V // 2, V, every).astype(np.int32),
+                every):
+        want, size, tokens = ref.embed_grad(grad, ids, V, 1.0)
+        out = torch.full((V, D), 5.0, device="cuda", dtype=_torch_type(dtype))
+        lda.embed_grad(_gpu(grad, dtype), _gpu(ids), V, out=out)
+        _close(_np(out), want, (tokens[:, None] + 2) * EPS * size, dtype, (dtype, V, D, N))
+        # rows apart: what lies between them is kept
+        wide = torch.full((V, D + 3), 5.0, device="cuda", dtype=_torch_type(dtype))
+        lda.embed_grad(_gpu(grad, dtype), _gpu(ids), V, out=wide[:, 1:1 + D])
+        assert torch.equal(wide[:, 1:1 + D], out)
+        assert bool((wide[:, 0] == 5).all()) and bool((wide[:, 1 + D:] == 5).all())
