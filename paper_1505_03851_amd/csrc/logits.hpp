@@ -505,7 +505,8 @@ __global__ __launch_bounds__(kDrawThreads) void draw_kernel(
       if (c) x = ruled(x, c, r);
     }
     if (r.bias) x += bias;
-    if (!(allowed >> (token & 31) & 1)) x = -INFINITY;
+    // (what lies past the row's end may have met a rule: its number in the history)
+    if (!there || !(allowed >> (token & 31) & 1)) x = -INFINITY;
     float v = INFINITY;
     if (d.greedy)
       v = x == top ? 0.0f : INFINITY;

@@ -36,3 +36,32 @@ def test_embed_grad_into_a_few_bytes(dtype, V, D, N):
         lda.embed_grad(_gpu(grad, dtype), _gpu(ids), V, out=wide[:, 1:1 + D])
         assert torch.equal(wide[:, 1:1 + D], out)
         assert bool((wide[:, 0] == 5).all()) and bool((wide[:, 1 + D:] == 5).all())
+
+
+# ---- the draw: tokens of the history past the row's end
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [1, 300, 16_000, 20_001, 32_769, 33_001, 49_999, 131_071])
+def test_draw_ignores_history_past_the_row(dtype, V):
+    """Ids in [V, the next multiple of 1,024) under a negative repetition, which
+    turns -inf into +inf: no token of that number is drawn."""
+    import torch
+    lda = _lda()
+    B = 12
+    g = np.random.default_rng(V)
+    x = _rounded(g.normal(0, 2, (B, V)), dtype)
+    x[:, :max(0, V - 40)] = -np.inf  # the last group is drawn
+    past = np.arange(V, (V + 1023) // 1024 * 1024 + 3, dtype=np.int32)
+    history = _gpu(np.tile(past, (B, 1)))
+    n = torch.full((B,), len(past), dtype=torch.int32, device="cuda")
+    seed, pos = torch.arange(B, device="cuda"), torch.arange(B, dtype=torch.int32, device="cuda")
+    t = torch.full((B,), 0.9, device="cuda")
+    t[::5] = 0.0
+    minus = torch.full((B,), -1.5, device="cuda")
+    want = lda.draw_logits(_gpu(x, dtype), seed, pos, t)
+    for prompt in (None, n):
+        got = lda.draw_logits(_gpu(x, dtype), seed, pos, t, history=history, lengths=n,
+                              prompt=prompt, repetition=minus)
+        assert int(got[0].max()) < V and int(got[0].min()) >= 0, (dtype, V)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (dtype, V)
