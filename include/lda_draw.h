@@ -546,8 +546,9 @@ int lda_dropout(const void *x, int64_t ld_x, void *out, int64_t ld_out, int64_t 
  *   x = x + bias[b][v]
  *   x = -inf                 if bit v % 32 of mask[b][v / 32] is 0
  * history is int32 [B][capacity] (capacity up to LDA_HISTORY_MAX), row b holding
- * lengths[b] tokens (at most capacity; a negative length counts as 0), the first prompt[b] of them the
- * prompt (NULL: 0) and the rest generated; tokens outside [0, V) are ignored.
+ * lengths[b] tokens (at most capacity), the first prompt[b] of them the prompt
+ * (NULL: 0) and the rest generated; a negative length or prompt counts as 0, and
+ * tokens outside [0, V) are ignored.
  * lengths, prompt int32 [B]; repetition, frequency, presence fp32 [B]; bias
  * fp32 rows, ld_bias apart; mask 32-bit words, ld_mask apart (0: one row for
  * all).  The order of the history does not matter.

@@ -106,7 +106,8 @@ struct History {
 __device__ __forceinline__ History row_history(const Rules &r, int64_t b) {
   if (!r.history) return History{nullptr, 0, 0};
   const int32_t n = r.lengths[b] < r.capacity ? r.lengths[b] : r.capacity;
-  return History{r.history + b * r.ld_history, n > 0 ? n : 0, r.prompt ? r.prompt[b] : 0};
+  const int32_t prompt = r.prompt ? r.prompt[b] : 0;
+  return History{r.history + b * r.ld_history, n > 0 ? n : 0, prompt > 0 ? prompt : 0};
 }
 
 // Four tokens from number i on; those past the end are -1.
@@ -128,7 +129,7 @@ __device__ __forceinline__ words4 history_load(const History &h, uint32_t i) {
 // difference wraps into the range, it is to a place past the row's end.)
 __device__ __forceinline__ void history_count(const History &h, uint32_t i, words4 t,
                                               uint32_t first, uint32_t size, uint32_t *count) {
-  const int32_t prompt = h.prompt - (int32_t)i;  // (i is below 2^31)
+  const int32_t prompt = h.prompt - (int32_t)i;  // (neither is negative)
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const uint32_t at = t[j] - first;

@@ -65,3 +65,32 @@ def test_draw_ignores_history_past_the_row(dtype, V):
                               prompt=prompt, repetition=minus)
         assert int(got[0].max()) < V and int(got[0].min()) >= 0, (dtype, V)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (dtype, V)
+
+
+# ---- rules: a prompt below zero is an empty one
+
+
+@pytest.mark.parametrize("V", [700, 40_000])
+def test_prompt_below_zero(V):
+    import torch
+    lda = _lda()
+    B, cap = 6, 9000
+    g = np.random.default_rng(V)
+    x = g.normal(0, 3, (B, V))
+    h = g.integers(0, V, (B, cap)).astype(np.int32)
+    n = np.full(B, cap, dtype=np.int32)
+    f32 = lambda a: _gpu(np.full(B, a, dtype=np.float32))  # noqa: E731
+    rules = dict(history=_gpu(h), lengths=_gpu(n), repetition=f32(1.2), frequency=f32(0.3),
+                 presence=f32(0.4))
+    seed, pos = torch.arange(B, device="cuda"), torch.arange(B, dtype=torch.int32, device="cuda")
+    want = lda.penalise_logits(_gpu(x, "float32"), **rules)
+    drawn = lda.draw_logits(_gpu(x, "float32"), seed, pos, **rules)
+    exact, size = ref.penalise(_rounded(x, "float32"), h, n, None, *(
+        _np(rules[k]) for k in ("repetition", "frequency", "presence")))
+    _close(_np(want), exact, 6 * EPS * size, "float32")
+    for p in (-1, -9000, -2 ** 31 + 9001, -2 ** 31 + 5000, -2 ** 31 + 3, -2 ** 31):
+        prompt = torch.full((B,), p, dtype=torch.int32, device="cuda")
+        got = lda.penalise_logits(_gpu(x, "float32"), prompt=prompt, **rules)
+        assert torch.equal(got, want), p
+        z = lda.draw_logits(_gpu(x, "float32"), seed, pos, prompt=prompt, **rules)
+        assert torch.equal(z[0], drawn[0]) and torch.equal(z[1], drawn[1]), p
