@@ -8,7 +8,7 @@
 // lda_draw_logits      one token per row of logits under those rules.
 //
 // Device code: elements.hpp (element types), wave_ops.hpp, keep_bits.hpp (the dropout
-// mask), token_rows.hpp, token_grad.hpp, logits.hpp.
+// mask), token_rows.hpp, token_grad.hpp with grad_columns.hpp, logits.hpp.
 #include <hip/hip_runtime.h>
 
 #include <math.h>
@@ -25,6 +25,7 @@ namespace {
 
 // A launch holds fewer than 2^32 work-items; kernels stride over the rest.
 constexpr int64_t kMaxBlocks = 1 << 20;
+constexpr int64_t kMaxWaves = 1 << 26;  // of a launch whose kernel does not stride
 // 16-byte units of a table (64 MB) from which clearing it bounds a call.
 constexpr int64_t kClearApart = (64 << 20) / 16;
 
@@ -105,7 +106,12 @@ GradLayout grad_layout(int64_t N, int32_t V, int32_t D) {
   L.bits = (need + L.passes - 1) / L.passes;
   L.sort_chunks = (N + kSortChunk - 1) / kSortChunk;
   L.width = D > 256 ? 8 : D > 128 ? 4 : D > 64 ? 2 : 1;
-  L.col_tiles = (uint32_t)((D + 64 * L.width - 1) / (64 * L.width));
+  switch (L.width) {
+    case 8: L.col_tiles = column_tiles<8>(D); break;
+    case 4: L.col_tiles = column_tiles<4>(D); break;
+    case 2: L.col_tiles = column_tiles<2>(D); break;
+    default: L.col_tiles = column_tiles<1>(D);
+  }
   // A wavefront's time grows with its run, and that of joining a frequent word's
   // parts with the number of runs, so the run grows with the root of N: 32 chunk^2
   // holds it.  Measured against half and twice the run: 1,000 tokens 13.6 us
@@ -114,6 +120,8 @@ GradLayout grad_layout(int64_t N, int32_t V, int32_t D) {
   // 168 (176, 179).
   L.chunk = 8;
   while (L.chunk < 512 && (int64_t)32 * L.chunk * L.chunk < N) L.chunk *= 2;
+  // (rows of many millions of columns: longer runs, up to what a launch holds)
+  while ((N + L.chunk - 1) / L.chunk * L.col_tiles >= kMaxWaves) L.chunk *= 2;
   L.chunks = (uint32_t)((N + L.chunk - 1) / L.chunk);
   L.ld_part = ((int64_t)D + 7) & ~(int64_t)7;
   size_t at = 0;
@@ -178,7 +186,7 @@ void launch_few(const void *grad, int64_t ldg, const int32_t *word_id, void *out
   const int64_t width = (int64_t)sizeof(SO) * D;
   const int32_t rows = width >= 4096 ? 1 : width < 256 ? 16 : (int32_t)(4096 / width);
   const unsigned clear_blocks = clear ? grid_of(((int64_t)V + 4 * rows - 1) / (4 * rows)) : 0u;
-  const unsigned grid = clear_blocks + (unsigned)((N * col_tiles + 3) / 4);
+  const unsigned grid = clear_blocks + grid_of((N * col_tiles + 3) / 4);
   if (drop.q)
     few_kernel<TG, TO, W, true><<<grid, 256, 0, s>>>((const SG *)grad, ldg, word_id, (int32_t)N,
                                                      (SO *)out, ldo, V, D, factor, drop, accumulate,

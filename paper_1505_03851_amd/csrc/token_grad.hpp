@@ -23,6 +23,7 @@
 #pragma once
 
 #include "elements.hpp"
+#include "grad_columns.hpp"
 #include "keep_bits.hpp"
 #include "wave_ops.hpp"
 
@@ -347,7 +348,7 @@ struct GradPlan {
 // begin at `own`.
 template <typename TO, int W>
 __device__ __forceinline__ void write_row(typename TO::store *out, int64_t ldo, uint32_t word,
-                                          int32_t own, int n, float factor, bool accumulate,
+                                          uint32_t own, int n, float factor, bool accumulate,
                                           float (&sum)[W]) {
   typename TO::store *p = out + (int64_t)word * ldo + own;
   if (n == W) {
@@ -391,8 +392,8 @@ __device__ __forceinline__ void add_row(const Packed<TG, W> &v, uint32_t row, in
   for (int j = 0; j < W; ++j) sum[j] += x[j];
 }
 
-// W columns of a row, `offset` bytes into it; the row's address stays in scalar
-// registers.
+// W columns of a row, `offset` bytes into what `grad` has of it; the row's address
+// stays in scalar registers.
 template <typename TG, int W, bool STREAM>
 __device__ __forceinline__ Packed<TG, W> load_row(const typename TG::store *grad, int64_t ldg,
                                                   uint32_t row, uint32_t offset) {
@@ -401,19 +402,6 @@ __device__ __forceinline__ Packed<TG, W> load_row(const typename TG::store *grad
   const auto *p = reinterpret_cast<const __attribute__((address_space(1))) char *>(base);
   return load_packed<TG, W, STREAM>((const typename TG::store *)(p + offset), W);
 }
-
-// A lane's columns: n of the W from `own` on exist; it reads, without a branch,
-// the W columns from `col` on, which end where they do (in the last lanes some are
-// the lane's before).
-template <int W>
-struct Columns {
-  int32_t own, n, col;
-  __device__ __forceinline__ Columns(uint32_t tile, int32_t D) {
-    own = (int32_t)(tile * 64 + (threadIdx.x & 63)) * W;
-    n = D - own < W ? (D - own > 0 ? D - own : 0) : W;
-    col = own < D - W ? own : D - W;
-  }
-};
 
 // One wavefront: `chunk` sorted positions, 64 W columns.  It reads the words and
 // row numbers of 64 positions at a time, one to a lane; the ends of the words'
@@ -435,9 +423,11 @@ __global__ __launch_bounds__(256) void reduce_kernel(
   if (c >= g.chunks) return;
   const uint32_t tile = item - c * col_tiles;
   const Columns<W> columns(tile, D);
-  const int32_t own = columns.own, n = columns.n, col = columns.col;
+  const uint32_t own = columns.own;
+  const int32_t n = columns.n, col = columns.col;
   const bool straddles = DROP && D % W != 0 && tile == col_tiles - 1;
-  const uint32_t offset = (uint32_t)col * (uint32_t)sizeof(typename TG::store);
+  grad += columns.first;
+  const uint32_t offset = columns.offset * (uint32_t)sizeof(typename TG::store);
   const uint32_t begin = c * g.chunk;
   const uint32_t end = g.N - begin < g.chunk ? g.N : begin + g.chunk;
   bool began_here = begin == 0 || token[begin - 1].word != token[begin].word;
@@ -500,7 +490,8 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(
   for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
     const uint32_t i = item / col_tiles;
     const Columns<W> columns(item - i * col_tiles, D);
-    const int32_t own = columns.own, n = columns.n, col = columns.col;
+    const uint32_t own = columns.own;
+    const int32_t n = columns.n, col = columns.col;
     const uint32_t c0 = crossing[1 + i];
     const uint32_t word = token[(c0 + 1) * g.chunk - 1].word;
     // the chunk in which the word ends: the last whose first token is one of it,
@@ -571,43 +562,44 @@ __global__ __launch_bounds__(256) void few_kernel(
     }
     return;
   }
-  const uint32_t item =
-      __builtin_amdgcn_readfirstlane((blockIdx.x - clear_blocks) * 4 + (threadIdx.x >> 6));
-  const uint32_t t = item / col_tiles, tile = item - t * col_tiles;
-  if (t >= (uint32_t)N) return;
-  const int32_t word = t < 64 ? __builtin_amdgcn_readlane(low, t)
-                              : __builtin_amdgcn_readlane(high, t - 64);
-  if ((uint32_t)word >= (uint32_t)V) return;
-  uint64_t a = __ballot(low == word), b = __ballot(high == word);
-  if ((a ? (uint32_t)__builtin_ctzll(a) : 64 + (uint32_t)__builtin_ctzll(b)) != t) return;
-  const Columns<W> columns(tile, D);
-  const bool straddles = DROP && D % W != 0 && tile == col_tiles - 1;
-  const uint32_t offset = (uint32_t)columns.col * (uint32_t)sizeof(typename TG::store);
-  float sum[W] = {};
-  while (a | b) {
-    Packed<TG, W> v[U];
-    uint32_t row[U];
-    int n = 0;
+  const uint32_t items = (uint32_t)N * col_tiles;
+  uint32_t item = __builtin_amdgcn_readfirstlane((blockIdx.x - clear_blocks) * 4 + (threadIdx.x >> 6));
+  for (; item < items; item += (gridDim.x - clear_blocks) * 4) {
+    const uint32_t t = item / col_tiles, tile = item - t * col_tiles;
+    const int32_t word = t < 64 ? __builtin_amdgcn_readlane(low, t)
+                                : __builtin_amdgcn_readlane(high, t - 64);
+    if ((uint32_t)word >= (uint32_t)V) continue;
+    uint64_t a = __ballot(low == word), b = __ballot(high == word);
+    if ((a ? (uint32_t)__builtin_ctzll(a) : 64 + (uint32_t)__builtin_ctzll(b)) != t) continue;
+    const Columns<W> columns(tile, D);
+    const bool straddles = DROP && D % W != 0 && tile == col_tiles - 1;
+    const uint32_t offset = columns.offset * (uint32_t)sizeof(typename TG::store);
+    float sum[W] = {};
+    while (a | b) {
+      Packed<TG, W> v[U];
+      uint32_t row[U];
+      int n = 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (a | b) {
-        row[u] = a ? (uint32_t)__builtin_ctzll(a) : 64 + (uint32_t)__builtin_ctzll(b);
-        if (a)
-          a &= a - 1;
-        else
-          b &= b - 1;
-        n = u + 1;
-      } else {
-        row[u] = t;
+      for (int u = 0; u < U; ++u) {
+        if (a | b) {
+          row[u] = a ? (uint32_t)__builtin_ctzll(a) : 64 + (uint32_t)__builtin_ctzll(b);
+          if (a)
+            a &= a - 1;
+          else
+            b &= b - 1;
+          n = u + 1;
+        } else {
+          row[u] = t;
+        }
+        v[u] = load_row<TG, W, false>(grad + columns.first, ldg, row[u], offset);
       }
-      v[u] = load_row<TG, W, false>(grad, ldg, row[u], offset);
-    }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (u < n) add_row<TG, W, DROP>(v[u], row[u], columns.col, straddles, drop, sum);
+      for (int u = 0; u < U; ++u) {
+        if (u < n) add_row<TG, W, DROP>(v[u], row[u], columns.col, straddles, drop, sum);
+      }
     }
+    write_row<TO, W>(out, ldo, (uint32_t)word, columns.own, columns.n, factor, accumulate, sum);
   }
-  write_row<TO, W>(out, ldo, (uint32_t)word, columns.own, columns.n, factor, accumulate, sum);
 }
 
 }  // namespace lda

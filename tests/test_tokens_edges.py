@@ -1,0 +1,51 @@
+"""The token operators at the edges of their ranges, on the CPU."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+CLANG = shutil.which("clang++", path="/opt/rocm/llvm/bin" + os.pathsep + os.environ["PATH"])
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_1505_03851_amd import _lib
+    return _lib.load()
+
+
+# ---- the embedding's gradient of rows of up to 2^31 - 1 columns
+
+
+@pytest.fixture(scope="module")
+def grad_columns(tmp_path_factory):
+    if CLANG is None:
+        pytest.skip("no clang++")
+    exe = str(tmp_path_factory.mktemp("columns") / "grad_columns")
+    subprocess.run([CLANG, "-x", "c++", "-std=c++17", "-O1", "-w",
+                    "-I", os.path.join(HERE, "leaf_host"),
+                    "-I", os.path.join(ROOT, "paper_1505_03851_amd", "csrc"),
+                    os.path.join(HERE, "leaf_host", "grad_columns.cpp"), "-o", exe], check=True)
+    return exe
+
+
+@pytest.mark.parametrize("D", [1, 2, 5, 7, 8, 63, 64, 65, 129, 257, 511, 512, 513, 1003, 2055,
+                               2 ** 30 - 1, 2 ** 30, 2 ** 30 + 9, 2 ** 30 + 1000, 2 ** 31 - 513,
+                               2 ** 31 - 512, 2 ** 31 - 511, 2 ** 31 - 8, 2 ** 31 - 1])
+def test_columns_of_a_row(grad_columns, D):
+    """Every column is written by one lane, and read at its own address."""
+    run = subprocess.run([grad_columns, str(D)], stdout=subprocess.PIPE, text=True, timeout=60)
+    assert run.returncode == 0, run.stdout
+
+
+def test_runs_fit_a_launch(lib):
+    """A wavefront's run of tokens grows with the columns, so that the launch holds
+    its wavefronts (2^26): the parts of words that cross runs stay below 2^38 bytes
+    and the workspace with them."""
+    f = lib.lda_embed_grad_workspace_bytes
+    for D in (2 ** 20, 2 ** 24, 2 ** 28 + 5, 2 ** 30, 2 ** 31 - 1):
+        for N in (129, 5000, 1 << 20, 2 ** 31 - 1):
+            assert f(N, 5, D) <= 2 ** 38 + 64 * N + 2 ** 20, (N, D)
+    assert f(1 << 20, 32_768, 256) < 2 ** 25 + 64 * 2 ** 20  # the usual run: 256 tokens

@@ -94,3 +94,52 @@ def test_prompt_below_zero(V):
         assert torch.equal(got, want), p
         z = lda.draw_logits(_gpu(x, "float32"), seed, pos, prompt=prompt, **rules)
         assert torch.equal(z[0], drawn[0]) and torch.equal(z[1], drawn[1]), p
+
+
+# ---- the embedding's gradient of very long rows
+
+
+def _marked(D, at, dtype, rows=1):
+    import torch
+    x = torch.zeros(rows, D, dtype=_torch_type(dtype), device="cuda")
+    for r in range(rows):
+        for k, c in enumerate(at):
+            x[r, c] = 1 + k + 16 * r
+    return x
+
+
+def _check_marks(row, at, times):
+    import torch
+    assert row[at].tolist() == [times * (1 + k) for k in range(len(at))]
+    assert int(torch.count_nonzero(row)) == len(at)
+
+
+def test_embed_grad_of_long_rows():
+    """Columns past 4 GiB into a row, and past 2^31 - 512; without a sort and with
+    one; more tiles than a launch has wavefronts."""
+    import torch
+    lda = _lda()
+    D = 2 ** 31 - 1
+    at = [0, 511, 2 ** 30 - 1, 2 ** 30, 2 ** 30 + 7, D - 600, D - 512, D - 9, D - 8, D - 1]
+    grad = _marked(D, at, "float32", 2)
+    out = torch.full((2, D), 7.0, device="cuda")
+    lda.embed_grad(grad, torch.tensor([1, 1], dtype=torch.int32, device="cuda"), 2, out=out)
+    assert out[1][at].tolist() == [2 * (1 + k) + 16 for k in range(len(at))]
+    assert int(torch.count_nonzero(out)) == len(at)
+    del grad, out
+    torch.cuda.empty_cache()
+    D = 2 ** 30 + 1003
+    at = [0, 511, 2 ** 30 - 1, 2 ** 30, 2 ** 30 + 7, D - 513, D - 9, D - 8, D - 1]
+    ids = torch.full((129,), -1, dtype=torch.int32, device="cuda")
+    ids[10:100] = 0
+    if torch.cuda.mem_get_info()[0] > lda.embed_grad_workspace_bytes(129, 1, D) + (20 << 30):
+        out = lda.embed_grad(_marked(D, at, "float32").expand(129, D), ids, 1)
+        _check_marks(out[0], at, 90.0)
+        del out
+        torch.cuda.empty_cache()
+    D = 2 ** 28 + 9
+    at = [0, 511, 2 ** 27, 2 ** 28, D - 1]
+    out = lda.embed_grad(_marked(D, at, "float16").expand(128, D), ids[:128], 1)
+    _check_marks(out[0], at, 90.0)
+    del out
+    torch.cuda.empty_cache()
