@@ -414,7 +414,13 @@ __global__ __launch_bounds__(64 * kGroupWaves) void group_kernel(
     float x[kSteps][8];
     rule_group<T>(q, first, h.size ? count : nullptr, r, x);
     const GroupSum sum = group_sum<FLOOR>(x, q.n, first + kGroup <= V, top, d);
-    if (lane == 0 && g < per_row) mine[g] = sum;
+    if (lane == 0 && g < per_row) {
+      // (with a floor the row's other workgroups still read the groups' largest)
+      if (FLOOR)
+        mine[g].sum = sum.sum;
+      else
+        mine[g] = sum;
+    }
     __syncthreads();
   }
 }

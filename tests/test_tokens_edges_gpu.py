@@ -143,3 +143,32 @@ def test_embed_grad_of_long_rows():
     _check_marks(out[0], at, 90.0)
     del out
     torch.cuda.empty_cache()
+
+
+# ---- the draw with a floor: the sums made again while other workgroups read
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_floor_of_long_rows(dtype):
+    """Rows in three launches draw what the same rows draw in one (they are 32,768
+    logits, and the same with -inf after them), whatever the workspace held, at
+    temperatures that keep every group and at ones that keep few.  The shares are
+    sums of the same weights: 64 eps."""
+    import torch
+    lda = _lda()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(6)
+    B, V, more = 96, 32_768, 20_000
+    x = (torch.randn(B, V, device="cuda", generator=g) * 2).to(_torch_type(dtype))
+    low = torch.full((B, more), -np.inf, device="cuda", dtype=x.dtype)
+    seed, pos = torch.arange(B, device="cuda"), torch.arange(B, dtype=torch.int32, device="cuda")
+    t = torch.linspace(0.2, 8.0, B, device="cuda")
+    m = torch.full((B,), 0.02, device="cuda")
+    m[::4] = 0.3
+    want = lda.draw_logits(x, seed, pos, t, m)
+    long = torch.cat([x, low], 1)
+    ws = torch.empty(lda.draw_logits_workspace_bytes(B, V + more), dtype=torch.uint8, device="cuda")
+    for held in (0x00, 0x7F, 0xFF):
+        z, prob = lda.draw_logits(long, seed, pos, t, m, workspace=ws.fill_(held))
+        assert torch.equal(z, want[0]), (dtype, held)
+        assert float(((prob - want[1]).abs() / want[1]).max()) <= 64 * EPS, (dtype, held)
