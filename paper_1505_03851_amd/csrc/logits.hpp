@@ -100,14 +100,13 @@ __device__ __forceinline__ uint32_t count_slot(uint32_t at) {
 // A row's history; the first `prompt` of its tokens are not generated.
 struct History {
   const int32_t *tokens;
-  int32_t size, prompt;  // 0 tokens where there is no history
+  int32_t size, prompt;  // 0 tokens where there is no history; the prompt as given
 };
 
 __device__ __forceinline__ History row_history(const Rules &r, int64_t b) {
   if (!r.history) return History{nullptr, 0, 0};
   const int32_t n = r.lengths[b] < r.capacity ? r.lengths[b] : r.capacity;
-  const int32_t prompt = r.prompt ? r.prompt[b] : 0;
-  return History{r.history + b * r.ld_history, n > 0 ? n : 0, prompt > 0 ? prompt : 0};
+  return History{r.history + b * r.ld_history, n > 0 ? n : 0, r.prompt ? r.prompt[b] : 0};
 }
 
 // Four tokens from number i on; those past the end are -1.
@@ -155,8 +154,14 @@ __device__ __forceinline__ Tokens load_tokens(const History &h) {
 // The uses of the tokens [first, first + size) in a row's history, counted in
 // LDS (which the caller has cleared and synchronised) by the whole workgroup;
 // `ahead`: load_tokens of it.
-__device__ __forceinline__ void count_history(const History &h, Tokens ahead, uint32_t first,
+__device__ __forceinline__ void count_history(History h, Tokens ahead, uint32_t first,
                                               uint32_t size, uint32_t *count) {
+  // A negative prompt is an empty one.  The maximum is taken here and not where the
+  // prompt is read (the compiler would move it back there): it waits for the read,
+  // which is to be on its way with the logits' (penalties of 256 rows of 100,000
+  // logits 28.8 us against 30.1).
+  asm volatile("" : "+v"(h.prompt));
+  h.prompt = h.prompt > 0 ? h.prompt : 0;
   const uint32_t step = 4 * blockDim.x;
   for (uint32_t i = 4 * threadIdx.x, start = 0; start < (uint32_t)h.size;
        i += 2 * step, start += 2 * step) {
