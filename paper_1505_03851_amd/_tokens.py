@@ -19,6 +19,8 @@ from ._lib import _require
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # LDA_F32, LDA_BF16, LDA_F16
 _I32, _I64, _F32, _U8 = torch.int32, torch.int64, torch.float32, torch.uint8
 _U64, _U32 = 2 ** 64 - 1, 2 ** 32 - 1
+_MAX_I32 = 2 ** 31 - 1
+_UNSUPPORTED = _lib.STATUS["LDA_ERR_UNSUPPORTED"]
 _Tensor = torch.Tensor
 _current_device = _lib._current_device or torch.cuda.current_device
 
@@ -144,6 +146,8 @@ def embed(table, word_id, scale: float = 1.0, p: float = 0.0, seed: int = 0, ste
     ``stream``: where it runs (None: the current stream)."""
     dev = table.get_device()
     V, D, ld = _rows(table, "table", dev)
+    if V > _MAX_I32 or D > _MAX_I32:  # the library would take what 32 bits hold of it
+        _lib._check(_UNSUPPORTED)
     N = word_id.numel() if isinstance(word_id, _Tensor) else -1
     ids = _vector(word_id, "word_id", _I32, N, dev)
     dtype = table.dtype
@@ -159,6 +163,8 @@ def embed(table, word_id, scale: float = 1.0, p: float = 0.0, seed: int = 0, ste
 @functools.lru_cache(maxsize=256)
 def embed_grad_workspace_bytes(N: int, V: int, D: int) -> int:
     """Bytes of device workspace ``embed_grad`` needs (0: none, or unsupported)."""
+    if max(V, D) > _MAX_I32:
+        return 0
     return int(_lib.load().lda_embed_grad_workspace_bytes(int(N), int(V), int(D)))
 
 
@@ -178,6 +184,8 @@ def embed_grad(grad, word_id, V: int, scale: float = 1.0, p: float = 0.0, seed: 
     N, D, ld = _rows(grad, "grad", dev)
     ids = _vector(word_id, "word_id", _I32, N, dev)
     V, own = int(V), grad.dtype
+    if V > _MAX_I32 or D > _MAX_I32:  # the library would take what 32 bits hold of it
+        _lib._check(_UNSUPPORTED)
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
@@ -287,6 +295,8 @@ def penalise_logits(logits, history=None, lengths=None, prompt=None, repetition=
     ``logits``.  ``stream``: where it runs (None: the current stream)."""
     dev = logits.get_device()
     B, V, ld = _rows(logits, "logits", dev)
+    if V > _MAX_I32:
+        _lib._check(_UNSUPPORTED)
     rules = _rules(dev, B, V, history, lengths, prompt, repetition, frequency, presence, bias, mask)
     if out is None:
         out, ldo = logits.new_empty((B, V)), V
@@ -300,6 +310,8 @@ def penalise_logits(logits, history=None, lengths=None, prompt=None, repetition=
 @functools.lru_cache(maxsize=256)
 def draw_logits_workspace_bytes(B: int, V: int) -> int:
     """Bytes of device workspace ``draw_logits`` needs (0: none, or unsupported)."""
+    if V > _MAX_I32:
+        return 0
     return int(_lib.load().lda_draw_logits_workspace_bytes(int(B), int(V)))
 
 
@@ -319,6 +331,8 @@ def draw_logits(logits, seed, position, temperature=None, min_p=None, history=No
     one.  ``stream``: where it runs (None: the current stream)."""
     dev = logits.get_device()
     B, V, ld = _rows(logits, "logits", dev)
+    if V > _MAX_I32:
+        _lib._check(_UNSUPPORTED)
     rules = _rules(dev, B, V, history, lengths, prompt, repetition, frequency, presence, bias, mask)
     seeds = _vector(seed, "seed", _I64, B, dev)
     places = _vector(position, "position", _I32, B, dev)

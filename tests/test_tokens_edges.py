@@ -49,3 +49,17 @@ def test_runs_fit_a_launch(lib):
         for N in (129, 5000, 1 << 20, 2 ** 31 - 1):
             assert f(N, 5, D) <= 2 ** 38 + 64 * N + 2 ** 20, (N, D)
     assert f(1 << 20, 32_768, 256) < 2 ** 25 + 64 * 2 ** 20  # the usual run: 256 tokens
+
+
+# ---- sizes past 32 bits
+
+
+def test_workspace_of_sizes_past_32_bits():
+    """2^32 + a few is not a few: unsupported, as the header says of what is 0."""
+    import paper_1505_03851_amd as lda
+    many = 2 ** 32 + 40_000
+    assert lda.embed_grad_workspace_bytes(1000, 40_000, 8) > 0
+    assert lda.draw_logits_workspace_bytes(3, 40_000) > 0
+    assert lda.embed_grad_workspace_bytes(1000, many, 8) == 0
+    assert lda.embed_grad_workspace_bytes(1000, 8, many) == 0
+    assert lda.draw_logits_workspace_bytes(3, many) == 0

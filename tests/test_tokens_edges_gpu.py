@@ -172,3 +172,30 @@ def test_floor_of_long_rows(dtype):
         z, prob = lda.draw_logits(long, seed, pos, t, m, workspace=ws.fill_(held))
         assert torch.equal(z, want[0]), (dtype, held)
         assert float(((prob - want[1]).abs() / want[1]).max()) <= 64 * EPS, (dtype, held)
+
+
+# ---- sizes past 32 bits, where the library counts in 32
+
+
+def test_sizes_past_32_bits_are_refused():
+    """V or D of 2^32 + a few, which 32 bits would take for a few.  The large
+    tensors are views of a few numbers but for one row of logits."""
+    import torch
+    lda = _lda()
+    many = 2 ** 32 + 5
+    ids = torch.tensor([0, 4, 5], dtype=torch.int32, device="cuda")
+    row = torch.zeros(1, 8, device="cuda")
+    half = torch.zeros(1, many, dtype=torch.float16, device="cuda")
+    i, s = ids[:1], torch.zeros(1, dtype=torch.int64, device="cuda")
+    out = torch.zeros(many, 1, dtype=torch.float16, device="cuda")
+    for call in (lambda: lda.embed(row.expand(many, 8), ids),
+                 lambda: lda.embed(row.expand(2 ** 31, 8), ids),
+                 lambda: lda.embed(half, i, out=torch.empty_like(half)),
+                 lambda: lda.embed_grad(half, i, 1, out=torch.empty_like(half)),
+                 lambda: lda.embed_grad(half[:, :1].expand(3, 1), ids, many, out=out),
+                 lambda: lda.embed_grad(half[:, :1].expand(3, 1), ids, many),
+                 lambda: lda.penalise_logits(half, out=torch.empty_like(half)),
+                 lambda: lda.draw_logits(half, s, i)):
+        with pytest.raises(lda.LdaError) as e:
+            call()
+        assert e.value.status == lda.STATUS["LDA_ERR_UNSUPPORTED"]
