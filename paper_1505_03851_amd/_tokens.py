@@ -4,7 +4,9 @@ and the token draw.  Argument marshalling only, as in ``_lib``.
 
 Matrices are 2-D tensors whose rows are contiguous; the rows themselves may lie
 at any distance (a slice of a wider buffer, an expanded row).  Tensors that a
-call allocates belong to the stream it runs on.
+call allocates belong to the stream it runs on.  A tensor that a call is given to
+write into counts as changed in place: a backward pass that saved what it held
+raises.
 """
 from __future__ import annotations
 
@@ -23,6 +25,7 @@ _MAX_I32 = 2 ** 31 - 1
 _UNSUPPORTED = _lib.STATUS["LDA_ERR_UNSUPPORTED"]
 _Tensor = torch.Tensor
 _current_device = _lib._current_device or torch.cuda.current_device
+_mark_written = torch.autograd.graph.increment_version
 
 
 class LogitRules(ctypes.Structure):
@@ -151,12 +154,15 @@ def embed(table, word_id, scale: float = 1.0, p: float = 0.0, seed: int = 0, ste
     N = word_id.numel() if isinstance(word_id, _Tensor) else -1
     ids = _vector(word_id, "word_id", _I32, N, dev)
     dtype = table.dtype
-    if out is None:
+    given = out is not None
+    if not given:
         out, ldo = table.new_empty((N, D)), D
     else:
         ldo = _rows(out, "out", dev, dtype, (N, D), True)[2]
     _run("lda_embed", dev, table.data_ptr(), ld, ids, out.data_ptr(), ldo, N, V, D, DTYPES[dtype],
          scale, _probability(p), int(seed) & _U64, int(step) & _U32)
+    if given:
+        _mark_written(out)
     return out
 
 
@@ -186,7 +192,8 @@ def embed_grad(grad, word_id, V: int, scale: float = 1.0, p: float = 0.0, seed: 
     V, own = int(V), grad.dtype
     if V > _MAX_I32 or D > _MAX_I32:  # the library would take what 32 bits hold of it
         _lib._check(_UNSUPPORTED)
-    if out is None:
+    given = out is not None
+    if not given:
         if accumulate:
             raise ValueError("accumulate needs out")
         if dtype is not None and dtype not in (_F32, own):
@@ -207,6 +214,8 @@ def embed_grad(grad, word_id, V: int, scale: float = 1.0, p: float = 0.0, seed: 
     _run("lda_embed_grad", dev, grad.data_ptr(), ld, ids, out.data_ptr(), ldo, N, V, D, DTYPES[own],
          DTYPES[out.dtype], scale, _probability(p), int(seed) & _U64, int(step) & _U32,
          1 if accumulate else 0, None if workspace is None else workspace.data_ptr(), need)
+    if given:
+        _mark_written(out)
     return out
 
 
@@ -234,7 +243,8 @@ def dropout(x, p: float, seed: int, step: int = 0, out=None) -> torch.Tensor:
     a = _as_rows(x, "x")
     rows, cols, ld = _rows(a, "x", dev)
     p = _probability(p)
-    if out is None:
+    given = out is not None
+    if not given:
         out = x.new_empty(x.shape)
         ldo = cols
     else:
@@ -244,6 +254,8 @@ def dropout(x, p: float, seed: int, step: int = 0, out=None) -> torch.Tensor:
     if rows and cols:
         _run("lda_dropout", dev, x.data_ptr(), ld, out.data_ptr(), ldo, rows, cols, DTYPES[x.dtype],
              p, int(seed) & _U64, int(step) & _U32)
+    if given:
+        _mark_written(out)
     return out
 
 
@@ -298,12 +310,15 @@ def penalise_logits(logits, history=None, lengths=None, prompt=None, repetition=
     if V > _MAX_I32:
         _lib._check(_UNSUPPORTED)
     rules = _rules(dev, B, V, history, lengths, prompt, repetition, frequency, presence, bias, mask)
-    if out is None:
+    given = out is not None
+    if not given:
         out, ldo = logits.new_empty((B, V)), V
     else:
         ldo = _rows(out, "out", dev, logits.dtype, (B, V), True)[2]
     _run("lda_penalise_logits", dev, logits.data_ptr(), ld, out.data_ptr(), ldo, B, V,
          DTYPES[logits.dtype], rules)
+    if given:
+        _mark_written(out)
     return out
 
 
@@ -338,7 +353,8 @@ def draw_logits(logits, seed, position, temperature=None, min_p=None, history=No
     places = _vector(position, "position", _I32, B, dev)
     heat = None if temperature is None else _vector(temperature, "temperature", _F32, B, dev)
     floor = None if min_p is None else _vector(min_p, "min_p", _F32, B, dev)
-    if out is None:
+    given = out is not None
+    if not given:
         z, prob = logits.new_empty(B, dtype=_I32), logits.new_empty(B, dtype=_F32)
         to = z.data_ptr(), prob.data_ptr()
     else:
@@ -354,4 +370,6 @@ def draw_logits(logits, seed, position, temperature=None, min_p=None, history=No
         workspace = logits.new_empty(need, dtype=_U8)
     _run("lda_draw_logits", dev, logits.data_ptr(), ld, B, V, DTYPES[logits.dtype], rules, heat,
          floor, seeds, places, *to, None if workspace is None else workspace.data_ptr(), need)
+    if given:
+        _mark_written((z, prob))
     return z, prob

@@ -199,3 +199,49 @@ def test_sizes_past_32_bits_are_refused():
         with pytest.raises(lda.LdaError) as e:
             call()
         assert e.value.status == lda.STATUS["LDA_ERR_UNSUPPORTED"]
+
+
+# ---- autograd
+
+
+def _outs():
+    """(name, a call that writes into the tensors it is given, those tensors)"""
+    import torch
+    lda = _lda()
+    x = torch.randn(20, 40, device="cuda")
+    i = torch.arange(20, dtype=torch.int32, device="cuda")
+    y, G = torch.empty_like(x), torch.zeros(30, 40, device="cuda")
+    z, prob = torch.empty_like(i), torch.empty(20, device="cuda")
+    return {
+        "embed": (lambda: lda.embed(x, i, out=y), [y]),
+        "embed_grad": (lambda: lda.embed_grad(x, i, 30, out=G), [G]),
+        "embed_grad, added": (lambda: lda.embed_grad(x, i, 30, out=G, accumulate=True), [G]),
+        "dropout": (lambda: lda.dropout(x, 0.5, 1, out=y), [y]),
+        "dropout in place": (lambda: lda.dropout(x, 0.5, 1, out=x), [x]),
+        "penalise": (lambda: lda.penalise_logits(x, out=y), [y]),
+        "penalise in place": (lambda: lda.penalise_logits(x, out=x), [x]),
+        "draw": (lambda: lda.draw_logits(x, i.long(), i, out=(z, prob)), [z, prob]),
+    }
+
+
+@pytest.mark.parametrize("name", ["embed", "embed_grad", "embed_grad, added", "dropout",
+                                  "dropout in place", "penalise", "penalise in place", "draw"])
+def test_what_is_overwritten_is_marked(name):
+    """A tensor that a call wrote into has another version, so that a backward
+    pass that saved it says so and does not use the wrong values."""
+    call, written = _outs()[name]
+    before = [t._version for t in written]
+    call()
+    assert all(t._version > v for t, v in zip(written, before)), name
+
+
+@pytest.mark.parametrize("op", ["dropout", "penalise_logits"])
+def test_backward_through_an_overwritten_tensor_raises(op):
+    import torch
+    lda = _lda()
+    x = torch.randn(20, 40, device="cuda", requires_grad=True)
+    y = x.exp()  # its backward needs y
+    with torch.no_grad():
+        lda.dropout(y, 0.5, 1, out=y) if op == "dropout" else lda.penalise_logits(y, out=y)
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.sum().backward()
