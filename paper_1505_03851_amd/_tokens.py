@@ -6,7 +6,10 @@ Matrices are 2-D tensors whose rows are contiguous; the rows themselves may lie
 at any distance (a slice of a wider buffer, an expanded row).  Tensors that a
 call allocates belong to the stream it runs on.  A tensor that a call is given to
 write into counts as changed in place: a backward pass that saved what it held
-raises.
+raises.  No call records a gradient: where gradients are recorded, one whose
+result would have one (embed, embed_grad, dropout, penalise_logits) refuses
+tensors that require it.  ``embed_grad`` and ``dropout`` are the backward passes,
+for a torch.autograd.Function or a training loop to call.
 """
 from __future__ import annotations
 
@@ -133,6 +136,14 @@ def _vector(t, name: str, dtype, n: int, dev: int) -> int:
     return t.data_ptr()
 
 
+def _cut_off(*names: str) -> None:
+    """Refuses tensors that require a gradient (some of ``names``), where those are
+    recorded."""
+    if torch.is_grad_enabled():
+        raise ValueError(f"{' or '.join(names)} requires a gradient, which is not recorded here: "
+                         "call this under torch.no_grad(), or with a detached tensor")
+
+
 def _probability(p) -> float:
     p = float(p)
     if not 0.0 <= p < 1.0:
@@ -147,6 +158,8 @@ def embed(table, word_id, scale: float = 1.0, p: float = 0.0, seed: int = 0, ste
     (lda_embed).  table [V][D] float32, bfloat16 or float16; word_id int32 [N];
     out [N][D] of the table's type.  A word outside [0, V) gives a row of zeros.
     ``stream``: where it runs (None: the current stream)."""
+    if table.requires_grad:
+        _cut_off("table")
     dev = table.get_device()
     V, D, ld = _rows(table, "table", dev)
     if V > _MAX_I32 or D > _MAX_I32:  # the library would take what 32 bits hold of it
@@ -159,6 +172,8 @@ def embed(table, word_id, scale: float = 1.0, p: float = 0.0, seed: int = 0, ste
         out, ldo = table.new_empty((N, D)), D
     else:
         ldo = _rows(out, "out", dev, dtype, (N, D), True)[2]
+        if out.requires_grad:
+            _cut_off("out")
     _run("lda_embed", dev, table.data_ptr(), ld, ids, out.data_ptr(), ldo, N, V, D, DTYPES[dtype],
          scale, _probability(p), int(seed) & _U64, int(step) & _U32)
     if given:
@@ -186,6 +201,8 @@ def embed_grad(grad, word_id, V: int, scale: float = 1.0, p: float = 0.0, seed: 
     the GPU works.  ``workspace``: a uint8 tensor of at least
     ``embed_grad_workspace_bytes(N, V, D)`` bytes, or None to allocate one.
     ``stream``: where it runs (None: the current stream)."""
+    if grad.requires_grad:
+        _cut_off("grad")
     dev = grad.get_device()
     N, D, ld = _rows(grad, "grad", dev)
     ids = _vector(word_id, "word_id", _I32, N, dev)
@@ -201,6 +218,8 @@ def embed_grad(grad, word_id, V: int, scale: float = 1.0, p: float = 0.0, seed: 
         out, ldo = grad.new_empty((V, D), dtype=dtype or own), D
     else:
         ldo = _rows(out, "out", dev, None, (V, D), True)[2]
+        if out.requires_grad:
+            _cut_off("out")
         if out.dtype not in (_F32, own) or dtype not in (None, out.dtype):
             raise TypeError("out must be float32 or the gradient's type, and dtype its own")
     need = embed_grad_workspace_bytes(N, V, D)
@@ -239,6 +258,8 @@ def dropout(x, p: float, seed: int, step: int = 0, out=None) -> torch.Tensor:
     shape (rows: its last dimension; a vector is one row), or a matrix of
     contiguous rows.  ``out`` may be ``x``.  ``stream``: where it runs (None: the
     current stream)."""
+    if x.requires_grad:
+        _cut_off("x")
     dev = x.get_device()
     a = _as_rows(x, "x")
     rows, cols, ld = _rows(a, "x", dev)
@@ -250,6 +271,8 @@ def dropout(x, p: float, seed: int, step: int = 0, out=None) -> torch.Tensor:
     else:
         if not isinstance(out, _Tensor) or out.shape != x.shape:
             raise ValueError("out must be a tensor of x's shape")
+        if out.requires_grad:
+            _cut_off("out")
         ldo = _rows(_as_rows(out, "out"), "out", dev, x.dtype, (rows, cols), True)[2]
     if rows and cols:
         _run("lda_dropout", dev, x.data_ptr(), ld, out.data_ptr(), ldo, rows, cols, DTYPES[x.dtype],
@@ -310,11 +333,18 @@ def penalise_logits(logits, history=None, lengths=None, prompt=None, repetition=
     if V > _MAX_I32:
         _lib._check(_UNSUPPORTED)
     rules = _rules(dev, B, V, history, lengths, prompt, repetition, frequency, presence, bias, mask)
+    if (logits.requires_grad or (bias is not None and bias.requires_grad)
+            or (repetition is not None and repetition.requires_grad)
+            or (frequency is not None and frequency.requires_grad)
+            or (presence is not None and presence.requires_grad)):
+        _cut_off("logits", "a rule")
     given = out is not None
     if not given:
         out, ldo = logits.new_empty((B, V)), V
     else:
         ldo = _rows(out, "out", dev, logits.dtype, (B, V), True)[2]
+        if out.requires_grad:
+            _cut_off("out")
     _run("lda_penalise_logits", dev, logits.data_ptr(), ld, out.data_ptr(), ldo, B, V,
          DTYPES[logits.dtype], rules)
     if given:
@@ -341,9 +371,10 @@ def draw_logits(logits, seed, position, temperature=None, min_p=None, history=No
     float32 [B]: where it is not above 0 the row takes its largest logit.
     ``min_p`` float32 [B]: tokens below that share of the likeliest token's
     probability are not drawn.  A row with nothing to draw gives z = -1 and
-    prob = 0.  ``out``: (z, prob) to overwrite.  ``workspace``: a uint8 tensor of
-    at least ``draw_logits_workspace_bytes(B, V)`` bytes, or None to allocate
-    one.  ``stream``: where it runs (None: the current stream)."""
+    prob = 0; neither has a gradient.  ``out``: (z, prob) to overwrite.
+    ``workspace``: a uint8 tensor of at least ``draw_logits_workspace_bytes(B, V)``
+    bytes, or None to allocate one.  ``stream``: where it runs (None: the current
+    stream)."""
     dev = logits.get_device()
     B, V, ld = _rows(logits, "logits", dev)
     if V > _MAX_I32:

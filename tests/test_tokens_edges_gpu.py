@@ -245,3 +245,32 @@ def test_backward_through_an_overwritten_tensor_raises(op):
         lda.dropout(y, 0.5, 1, out=y) if op == "dropout" else lda.penalise_logits(y, out=y)
     with pytest.raises(RuntimeError, match="inplace"):
         y.sum().backward()
+
+
+def test_no_gradient_is_lost_in_silence():
+    """A call that would cut a tensor off from its gradient is refused; without
+    gradients, and where the result has none (a draw), it runs."""
+    import torch
+    lda = _lda()
+    x = torch.randn(20, 40, device="cuda")
+    i = torch.arange(20, dtype=torch.int32, device="cuda")
+    h, f, b = i[:, None].contiguous(), torch.ones(20, device="cuda"), torch.zeros(40, device="cuda")
+    calls = []
+    for t in (torch.nn.Parameter(x), x.clone().requires_grad_(), x.clone().requires_grad_() * 2):
+        calls += [lambda t=t: lda.embed(t, i), lambda t=t: lda.embed_grad(t, i, 30),
+                  lambda t=t: lda.dropout(t, 0.5, 1), lambda t=t: lda.penalise_logits(t),
+                  lambda t=t: lda.embed(x, i, out=t), lambda t=t: lda.dropout(x, 0.5, 1, out=t),
+                  lambda t=t: lda.embed_grad(x, i, 20, out=t),
+                  lambda t=t: lda.penalise_logits(x, out=t)]
+    need = f.clone().requires_grad_()
+    calls += [lambda k=k: lda.penalise_logits(x, h, i, **{k: need})
+              for k in ("repetition", "frequency", "presence")]
+    calls.append(lambda: lda.penalise_logits(x, bias=b.clone().requires_grad_()))
+    for call in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+    z, prob = lda.draw_logits(x.clone().requires_grad_(), i.long(), i)
+    z2, prob2 = lda.draw_logits(x, i.long(), i)
+    assert torch.equal(z, z2) and torch.equal(prob, prob2) and not prob.requires_grad
