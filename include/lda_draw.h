@@ -478,9 +478,10 @@ int lda_draw_routed_scratch(const float *theta, const float *phi, const int32_t 
 /*
  * Rows: a matrix argument is a pointer and the distance between its rows in
  * elements (ld_*); a row's elements are contiguous.  An input's rows may lie
- * at any distance of 0 or more (0: one row for all), an output's at its width
- * or more (LDA_ERR_VALUE otherwise).  Pointers are aligned to their element
- * (LDA_ERR_ALIGN), no more: rows of odd length and views are taken as they are.
+ * at any distance of 0 or more (0: one row for all; a rule's at 0 or at its
+ * width or more), an output's at its width or more (LDA_ERR_VALUE otherwise).
+ * Pointers are aligned to their element (LDA_ERR_ALIGN), no more: rows of odd
+ * length and views are taken as they are.
  *
  * Dropout: with probability p (0 <= p < 1, else LDA_ERR_VALUE; 0: none) an
  * element is 0, whatever it was; otherwise it is multiplied by the reciprocal
@@ -550,8 +551,8 @@ int lda_dropout(const void *x, int64_t ld_x, void *out, int64_t ld_out, int64_t 
  * (NULL: 0) and the rest generated; a negative length or prompt counts as 0, and
  * tokens outside [0, V) are ignored.
  * lengths, prompt int32 [B]; repetition, frequency, presence fp32 [B]; bias
- * fp32 rows, ld_bias apart; mask 32-bit words, ld_mask apart (0: one row for
- * all).  The order of the history does not matter.
+ * fp32 rows, ld_bias apart; mask 32-bit words, ld_mask apart.  The order of the
+ * history does not matter.
  */
 #define LDA_HISTORY_MAX 1073741824
 typedef struct lda_logit_rules {

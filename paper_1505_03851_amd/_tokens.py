@@ -291,7 +291,7 @@ def _rules(dev, B, V, history, lengths, prompt, repetition, frequency, presence,
             raise ValueError("history must have a row for each row of logits")
         if lengths is None:
             raise ValueError("history needs lengths")
-        if apart < capacity:
+        if 0 < apart < capacity:
             raise ValueError("history's rows overlap")
         past = (history.data_ptr(), apart, capacity, _vector(lengths, "lengths", _I32, B, dev),
                 None if prompt is None else _vector(prompt, "prompt", _I32, B, dev),

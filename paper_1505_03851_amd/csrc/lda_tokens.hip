@@ -303,7 +303,7 @@ int make_rules(const lda_logit_rules *r, int64_t B, int32_t V, Rules *out) {
     if (!r->lengths) return LDA_ERR_NULL;
     if (r->capacity < 0) return LDA_ERR_SHAPE;
     if (r->capacity > LDA_HISTORY_MAX) return LDA_ERR_UNSUPPORTED;
-    if (r->ld_history < r->capacity) return LDA_ERR_VALUE;
+    if (r->ld_history != 0 && r->ld_history < r->capacity) return LDA_ERR_VALUE;
   }
   if (r->bias && r->ld_bias != 0 && r->ld_bias < V) return LDA_ERR_VALUE;
   if (r->mask && r->ld_mask != 0 && r->ld_mask < ((int64_t)V + 31) / 32) return LDA_ERR_VALUE;

@@ -53,7 +53,7 @@ constexpr int kShortGroups = 2 * kDrawWaves;  // of a row that one launch draws 
 constexpr uint32_t kSeen = 0x80000000u;
 
 struct Rules {
-  const int32_t *history;  // [B][ld_history], or null
+  const int32_t *history;  // [B][ld_history], or null; ld_history 0: one row
   int64_t ld_history;
   const int32_t *lengths, *prompt;  // [B]; prompt null: 0
   const float *repetition, *frequency, *presence;  // [B] or null

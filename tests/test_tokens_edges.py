@@ -63,3 +63,20 @@ def test_workspace_of_sizes_past_32_bits():
     assert lda.embed_grad_workspace_bytes(1000, many, 8) == 0
     assert lda.embed_grad_workspace_bytes(1000, 8, many) == 0
     assert lda.draw_logits_workspace_bytes(3, many) == 0
+
+
+# ---- one history for every row
+
+
+def test_history_rows(lib):
+    """A distance of 0 (one row for all) passes the checks, one below the capacity
+    does not.  B = 0 returns after the checks of the rules."""
+    import ctypes
+    from paper_1505_03851_amd import _lib
+    from paper_1505_03851_amd._tokens import LogitRules
+    A, value = 4096, _lib.STATUS["LDA_ERR_VALUE"]
+    for apart, want in ((0, 0), (5, 0), (9, 0), (4, value), (1, value), (-5, value)):
+        r = ctypes.byref(LogitRules(A, apart, 5, A, None, None, None, None, None, 0, None, 0))
+        assert lib.lda_penalise_logits(A, 40, A, 40, 0, 40, 0, r, None) == want, apart
+        assert lib.lda_draw_logits(A, 40, 0, 40, 0, r, None, None, A, A, A, A, A, 1 << 20,
+                                   None) == want, apart

@@ -274,3 +274,27 @@ def test_no_gradient_is_lost_in_silence():
     z, prob = lda.draw_logits(x.clone().requires_grad_(), i.long(), i)
     z2, prob2 = lda.draw_logits(x, i.long(), i)
     assert torch.equal(z, z2) and torch.equal(prob, prob2) and not prob.requires_grad
+
+
+# ---- one history for every row
+
+
+@pytest.mark.parametrize("V", [900, 40_000])
+def test_one_history_for_all_rows(V):
+    import torch
+    lda = _lda()
+    B, cap = 7, 300
+    g = np.random.default_rng(V)
+    x = _gpu(g.normal(0, 3, (B, V)), "float32")
+    h = _gpu(g.integers(0, V, (1, cap)).astype(np.int32))
+    n = _gpu(g.integers(0, cap + 1, B).astype(np.int32))
+    f = torch.full((B,), 0.7, device="cuda")
+    seed, pos = torch.arange(B, device="cuda"), torch.arange(B, dtype=torch.int32, device="cuda")
+    one = dict(history=h.expand(B, cap), lengths=n, frequency=f)
+    each = dict(one, history=h.repeat(B, 1))
+    assert torch.equal(lda.penalise_logits(x, **one), lda.penalise_logits(x, **each))
+    for a, b in zip(lda.draw_logits(x, seed, pos, **one), lda.draw_logits(x, seed, pos, **each)):
+        assert torch.equal(a, b)
+    wide = torch.zeros(B * 3 + cap, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):  # rows that overlap
+        lda.penalise_logits(x, history=wide.as_strided((B, cap), (3, 1)), lengths=n)
