@@ -542,7 +542,7 @@ int lda_dropout(const void *x, int64_t ld_x, void *out, int64_t ld_out, int64_t 
  * pointer is a rule that does not apply).  For token v of row b, in this order
  * and in fp32:
  *   x = x > 0 ? x / repetition[b] : x * repetition[b]   if v is in the history
- *   x = x - frequency[b] * c                            c: uses of v among the
+ *   x = x - frequency[b] * c if c > 0                   c: uses of v among the
  *   x = x - presence[b]      if c > 0                      generated tokens
  *   x = x + bias[b][v]
  *   x = -inf                 if bit v % 32 of mask[b][v / 32] is 0

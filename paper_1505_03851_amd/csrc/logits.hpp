@@ -5,7 +5,7 @@
 // the row's generated tokens:
 //   x = seen ? (x > 0 ? x / repetition : x * repetition) : x   (seen: anywhere in
 //                                        the history, the prompt included)
-//   x = x - frequency * c
+//   x = x - frequency * c                where c > 0
 //   x = x - presence                     where c > 0
 //   x = x + bias[v]
 //   x = -inf                             where the mask's bit v is 0
@@ -86,7 +86,8 @@ __device__ __forceinline__ float rounded(float x) {
 __device__ __forceinline__ float ruled(float x, uint32_t count, const RowRules &r) {
   x = x > 0.0f ? x / r.repetition : rounded(x * r.repetition);
   const uint32_t c = count & ~kSeen;
-  x -= rounded(r.frequency * (float)c);
+  const float cut = rounded(r.frequency * (float)c);
+  x -= c ? cut : 0.0f;  // (an infinite frequency times 0 is NaN)
   return x - (c ? r.presence : 0.0f);
 }
 

@@ -298,3 +298,31 @@ def test_one_history_for_all_rows(V):
     wide = torch.zeros(B * 3 + cap, dtype=torch.int32, device="cuda")
     with pytest.raises(ValueError):  # rows that overlap
         lda.penalise_logits(x, history=wide.as_strided((B, cap), (3, 1)), lengths=n)
+
+
+# ---- rules: an infinite penalty reaches the tokens it is for
+
+
+@pytest.mark.parametrize("V", [900, 40_000])
+def test_infinite_frequency(V):
+    """A frequency of +inf takes the generated tokens out and leaves those of the
+    prompt, and those not seen, as they are; -inf makes the generated ones +inf."""
+    import torch
+    lda = _lda()
+    B, cap, first = 5, 400, 150
+    g = np.random.default_rng(V)
+    x = _rounded(g.normal(0, 3, (B, V)), "float32")
+    h = g.integers(0, V, (B, cap)).astype(np.int32)
+    n = np.full(B, cap, dtype=np.int32)
+    made = np.zeros((B, V), dtype=bool)
+    for b in range(B):
+        made[b, h[b, first:]] = True
+    seed, pos = torch.arange(B, device="cuda"), torch.arange(B, dtype=torch.int32, device="cuda")
+    rules = dict(history=_gpu(h), lengths=_gpu(n), prompt=torch.full_like(pos, first))
+    for sign in (1, -1):
+        f = torch.full((B,), sign * np.inf, device="cuda")
+        got = _np(lda.penalise_logits(_gpu(x, "float32"), frequency=f, **rules))
+        assert np.array_equal(got, np.where(made, -sign * np.inf, x)), sign
+        z, prob = lda.draw_logits(_gpu(x, "float32"), seed, pos, frequency=f, **rules)
+        want = lda.draw_logits(_gpu(got, "float32"), seed, pos)
+        assert torch.equal(z, want[0]) and torch.equal(prob, want[1]), sign
