@@ -154,7 +154,10 @@ void launch_reduce(const void *grad, int64_t ldg, void *out, int64_t ldo, int32_
   // 72.4 against 70.7).  In float a lane's 32 bytes are two accesses to one line
   // (16,384 of 2,048: 131 against 129).
   constexpr bool kMayStream = sizeof(SG) == 2;
-  const bool stream = kMayStream && (int64_t)g.N * D * (int64_t)sizeof(SG) >= (int64_t)128 << 20;
+  // (one row for all tokens stays in the caches: 32,768 of 2,048 bfloat16 70 us
+  // against 82 past them, 1M of 256 132 against 187)
+  const int64_t read = (ldg ? (int64_t)g.N : 1) * D * (int64_t)sizeof(SG);
+  const bool stream = kMayStream && read >= (int64_t)128 << 20;
 #define LDA_SUM(DROP, STREAM)                                                                    \
   reduce_kernel<TG, TO, W, DROP, STREAM><<<grid, 256, 0, s>>>(                                   \
       (const SG *)grad, ldg, (SO *)out, ldo, D, factor, drop, accumulate, L.col_tiles, g, token, \

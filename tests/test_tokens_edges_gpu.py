@@ -326,3 +326,19 @@ def test_infinite_frequency(V):
         z, prob = lda.draw_logits(_gpu(x, "float32"), seed, pos, frequency=f, **rules)
         want = lda.draw_logits(_gpu(got, "float32"), seed, pos)
         assert torch.equal(z, want[0]) and torch.equal(prob, want[1]), sign
+
+
+# ---- the gradient of a broadcast, larger than the caches if it were written out
+
+
+@pytest.mark.parametrize("dtype,D,p", [("bfloat16", 1024, 0.0), ("float16", 1003, 0.1)])
+def test_embed_grad_of_one_row_for_many(dtype, D, p):
+    import torch
+    lda = _lda()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(D)
+    N, V = (150 << 20) // (2 * D), 3000
+    ids = torch.randint(-1, V + 1, (N,), device="cuda", generator=g, dtype=torch.int32)
+    one = torch.randn(1, D, device="cuda", generator=g).to(_torch_type(dtype)).expand(N, D)
+    got = lda.embed_grad(one, ids, V, 1.5, p, 3, 4)
+    assert torch.equal(got, lda.embed_grad(one.contiguous(), ids, V, 1.5, p, 3, 4))
