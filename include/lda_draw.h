@@ -71,8 +71,10 @@ extern "C" {
 #define LDA_ERR_UNSUPPORTED (-3) /* K > LDA_MAX_K, N > LDA_MAX_N, or a table
                                     too large                                */
 #define LDA_ERR_HIP (-4)         /* the HIP runtime reported an error        */
-#define LDA_ERR_ALIGN (-5)       /* a pointer is not 4-byte aligned          */
-#define LDA_ERR_WORKSPACE (-6)   /* routing workspace too small or mismatched */
+#define LDA_ERR_ALIGN (-5)       /* a pointer is not aligned to its element
+                                    (8 bytes: offsets, workspaces)           */
+#define LDA_ERR_WORKSPACE (-6)   /* a workspace too small, or a route that does
+                                    not belong to the tokens                 */
 #define LDA_ERR_VALUE (-7)       /* an element type, a probability or a row
                                     stride out of range                      */
 

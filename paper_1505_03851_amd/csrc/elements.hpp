@@ -84,9 +84,9 @@ struct Packed {
 };
 
 // p[0 .. W) as it is in memory; only the first `n` are read (the rest: 0)
-// where n < W.  STREAM: what is read or written passes the caches by (it is
-// larger than they are and touched once), so that it does not put out what they
-// hold, nor wait for what they have to write back.
+// where n < W.  STREAM: what is read or written passes the caches by, so that it
+// does not put out what they hold, nor wait for what they have to write back; meant
+// for what is larger than they are and touched once.
 template <typename T, int W, bool STREAM = false>
 __device__ __forceinline__ Packed<T, W> load_packed(const typename T::store *p, int n) {
   using R = Raw<W * (int)sizeof(typename T::store)>;

@@ -176,7 +176,7 @@ void launch_reduce(const void *grad, int64_t ldg, void *out, int64_t ldo, int32_
                                                        L.col_tiles, g, token, part, crossing);
 }
 
-// N of 1 to kFewTokens: one launch, no workspace (64 tokens of 512 columns: 5 us
+// N of 1 to kFewTokens: one launch, no workspace (64 tokens of 512 columns: 6 us
 // against 11 with the sort).
 template <typename TG, typename TO, int W>
 void launch_few(const void *grad, int64_t ldg, const int32_t *word_id, void *out, int64_t ldo,
@@ -286,8 +286,8 @@ int launch_grad(const void *grad, int64_t ldg, const int32_t *word_id, void *out
 
 // The groups (and wavefronts) of a workgroup: the most that still give every
 // compute unit two workgroups, since each workgroup reads its row's history.
-// (256 rows of 100,000 logits and 4,096 tokens: 35 us with eight, 36 with four;
-// eight of half a group, 42.)
+// (256 rows of 100,000 logits and 4,096 tokens: 28.9 us with eight, 30.4 with four,
+// 39 with one.)
 int group_waves(int64_t B, int64_t V) {
   const int64_t groups = (V + kGroup - 1) / kGroup;
   int waves = kGroupWaves;

@@ -15,27 +15,30 @@
 // w_v / sum w.  It is taken in two steps, the group of kGroup tokens by
 // E_g / (sum of the group's weights), then the token inside it, so a row needs
 // V / kGroup + kGroup variates and not V, and the second step reads one group.
-// Which token wins depends on rounding only where the best two are within
-// rounding of each other (about 1e-7 of the draws), in whatever order the sums
-// are made; a search of partial sums for u * S would hang on the rounding of
-// every one of V partial sums.
+// Which token wins depends on rounding only where the best two keys are within
+// rounding of each other, in whatever order the sums are made: with a probability of
+// at most the relative errors of the two, each a few 2^-24 and 2^-24 of (max - x) /
+// temperature, so about 1e-6 of the draws and more where logits are large (none of
+// 6M draws from 2,000 logits differed from the draw in 64 bits).  A search of
+// partial sums for u * S would hang on the rounding of every one of V partial sums.
 //
 // What bounds them is not memory but a wavefront's chain (the row's numbers, its
 // history, the counts in LDS, the rules) and, with every rule on, vector
 // instructions: about 20 a logit under the rules, of which the division is half
 // (it is the exact one, so that two logits that tie after a penalty tie here
 // too), and 8 for its weight.  So a workgroup reads its row's history once for
-// eight groups (one group to a workgroup: 47 us against 34 for 256 rows), rows
-// are addressed from scalar registers to keep seven wavefronts on a SIMD, and
-// the logits are on their way while the history is counted.
+// eight groups (one group to a workgroup: 39 us against 29 for the penalties of 256
+// rows, 51.5 against 37 for 64 draws), rows are addressed from scalar registers (70
+// vector registers are left: seven wavefronts fit a SIMD), and the logits are on
+// their way while the history is counted.
 //
 // Measured on MI355X: 256 rows of 100,000 bfloat16 logits under a history of up
-// to 4,096 tokens, a bias and masks 28 us (3.8 TB/s of the 109 MB that have to
-// move; 17 us with no rules, 23 without the history); 64 draws from 100,000 with
+// to 4,096 tokens, a bias and masks 28 us (3.9 TB/s of the 109 MB that have to
+// move; 17.6 us with no rules, 21 without the history); 64 draws from 100,000 with
 // a history of up to 8,192, bias, masks, temperatures and floors 36 us (17 the
-// sums, 12 the sums above the floors, 9 the races); 256 plain draws from 49,999
-// floats 18.5 us (13 and 7); one draw from 32,768, in one launch, 11.5 us on the
-// GPU and 14 a call.
+// sums, 12 the sums above the floors, 9 the races, in a trace, which keeps them
+// apart); 256 plain draws from 49,999 floats 18.6 us (13 and 7); one draw from
+// 32,768, in one launch, 10.5 us on the GPU and 13.5 a call.
 #pragma once
 
 #include "elements.hpp"

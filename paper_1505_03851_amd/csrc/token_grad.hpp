@@ -16,10 +16,11 @@
 // Measured on MI355X: 1M tokens of 256 bfloat16 over 32,768 Zipf words 167 us (3.3
 // TB/s of the 558 MB that have to move): the sums 115 us at 4.7 TB/s, bound by
 // memory, the sort 42, a chain of six launches, and the joins 11; 32,768 tokens
-// of 2,048 bfloat16 into 50,000 float rows, dropped out, 129 us (4.2 TB/s): clearing
-// at 5.0 TB/s with the sort under it, then 47 of sums; 4,096 tokens of 1,000
+// of 2,048 bfloat16 into 50,000 float rows, dropped out, 130 us (4.2 TB/s): clearing
+// at 4.9 TB/s with the sort under it, then 47 of sums (added to what is there: 89 us,
+// the rows that occur alone); 4,096 tokens of 1,000
 // floats 23 us, three launches of 4 to 10 us, each a few round trips; up to 128
-// tokens of 512 columns into 10,000 rows 5 us, one into 400 MB 64 (6.3 TB/s).
+// tokens of 512 columns into 10,000 rows 6 us, one into 400 MB 64 (6.3 TB/s).
 #pragma once
 
 #include "elements.hpp"

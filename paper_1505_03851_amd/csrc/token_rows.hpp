@@ -11,8 +11,8 @@
 // take 25 us of vector instructions on 67M elements, under the 33 us of memory.)
 //
 // Measured on MI355X: 16,384 rows of 4,096 bfloat16 out of 100,000, dropped out,
-// 33 us (5.7 TB/s of the 187 MB that have to move); 32,768 rows of 4,096 dropped
-// out 85 us (6.3 TB/s of 537 MB); 64 rows of 1,024, 3.2 us on the GPU and 8 a call.
+// 32.5 us (5.8 TB/s of the 187 MB that have to move); 32,768 rows of 4,096 dropped
+// out 85 us (6.3 TB/s of 537 MB); 64 rows of 1,024, 3.4 us on the GPU and 8 a call.
 #pragma once
 
 #include "elements.hpp"
@@ -31,10 +31,16 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(
     const typename T::store *x, int64_t ldx, const int32_t *__restrict__ word_id,
     typename T::store *out, int64_t ldo, int64_t N, int32_t V, int64_t D, float factor,
     Dropout drop, int lanes_log2, uint32_t col_tiles, int64_t tiles) {
-  // What passes the caches by (16,384 rows of 4,096 bfloat16 looked up: 35 us
-  // against 45; 32,768 dropped out: 86 with both against 94, 2,048: 7.0 against
-  // 9.2; half that many float rows looked up: 43 against 49, but dropped out 105
-  // against 98, since a lane's 32 bytes are two accesses to one line).
+  // What passes the caches by, whatever its size: rows looked up are stored so, and
+  // 16-bit rows dropped out are read and stored so.  Alone, 16,384 rows of 4,096
+  // bfloat16 looked up take 35 us against 45, 32,768 dropped out 86 against 94, 2,048
+  // 7.0 against 9.2; 8,192 float rows looked up 43 against 49 where few words are
+  // frequent but 54 against 47 where all are alike; float rows dropped out 105
+  // against 98, since a lane's 32 bytes are two accesses to one line.  With a kernel
+  // after it that reads what was written: 64 rows of 1,024 bfloat16 looked up 4.9
+  // against 4.7, 2,048 of 4,096 16.7 against 16.3, 32,768 170 against 176; dropped
+  // out 5.4 against 5.2, 17.1 against 18.1, 178 against 181; 2,048 of 4,096 floats
+  // looked up 27 against 24.
   constexpr bool kStreamStore = GATHER || sizeof(typename T::store) == 2;
   constexpr bool kStreamLoad = !GATHER && sizeof(typename T::store) == 2;
   const int lane = (int)threadIdx.x & ((1 << lanes_log2) - 1);
