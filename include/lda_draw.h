@@ -602,6 +602,113 @@ int lda_draw_logits(const void *logits, int64_t ld_logits, int64_t B, int32_t V,
                     const int64_t *seed, const int32_t *position, int32_t *z, float *prob,
                     void *workspace, size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Between a layer's last activations and the next token: the norm of the
+ * residual stream and its gradient, rows in 8 bits, their product with weights
+ * in 8 bits (the logits, say), and the choice of a token from logits by a given
+ * uniform number.  Conventions as above: rows at any distance, pointers aligned
+ * to their element, nothing is allocated, nothing waits, every call may be
+ * captured into a graph.
+ *
+ * LDA_I8: the element type of rows in 8 bits, where a call's text names it.
+ */
+#define LDA_I8 3
+
+/*
+ * The norm of rows: h = x + residual, out = h * weight / sqrt(mean(h^2) + eps),
+ * in fp32 from x to out, each output rounded once.  x, residual (NULL: none) and
+ * sum (NULL: h is not stored) are [N][D] of element type `dtype`, weight [D] of
+ * that type or LDA_F32 (weight_dtype).  out [N][D] is of type out_dtype: dtype, or
+ * LDA_I8: then row n is held as whole numbers from -127 to 127 that stand for
+ * themselves times scale[n] (fp32 [N]): scale = (the largest magnitude of the
+ * row) / 127.  A row of zeros has the scale 0; one with a NaN or an infinity has
+ * a NaN for a scale and zeros for numbers.  scale is not used for other types.
+ * eps is above 0 in fp32, finite (LDA_ERR_VALUE).  out (not in 8 bits) and sum may
+ * be x or residual themselves (same ld), but not each other.  N = 0 is a no-op; N up
+ * to LDA_MAX_N.  Squares are summed in fp32: rows whose squares are above its
+ * range have no norm.
+ */
+int lda_add_norm(const void *x, int64_t ld_x, const void *residual, int64_t ld_residual,
+                 const void *weight, void *out, int64_t ld_out, void *sum, int64_t ld_sum,
+                 float *scale, int64_t N, int32_t D, int32_t dtype, int32_t weight_dtype,
+                 int32_t out_dtype, double eps, void *stream);
+
+/*
+ * The norm's gradient.  With h [N][D] (what lda_add_norm stored as sum, or x where
+ * it had no residual), s = 1 / sqrt(mean(h^2) + eps), v = h s and grad the gradient of its
+ * output:
+ *   dx = s (grad weight - v mean(grad weight v)) + residual_grad
+ *   dweight = the sum over the rows of grad v
+ * dx is the gradient of h, so of x and of the residual alike; residual_grad (NULL:
+ * none) is what reaches h along the residual stream.  grad, h, residual_grad and dx
+ * are of element type `dtype`; weight of that type or LDA_F32; dweight fp32 [D], with
+ * `accumulate` added to what it holds.  dx may be grad, h or residual_grad itself (same
+ * ld).  Sums are fp32 in an order that depends on N and D alone: the same call
+ * gives the same bits.  N = 0: dweight is cleared (or, accumulating, left).  `workspace`:
+ * device memory, 8-byte aligned, at least lda_norm_grad_workspace_bytes(N, D)
+ * bytes (LDA_ERR_WORKSPACE), free to use again once the call's kernels are done.
+ */
+size_t lda_norm_grad_workspace_bytes(int64_t N, int32_t D);
+int lda_norm_grad(const void *grad, int64_t ld_grad, const void *h, int64_t ld_h,
+                  const void *residual_grad, int64_t ld_residual, const void *weight, void *dx,
+                  int64_t ld_dx, float *dweight, int64_t N, int32_t D, int32_t dtype,
+                  int32_t weight_dtype, double eps, int32_t accumulate, void *workspace,
+                  size_t workspace_bytes, void *stream);
+
+/*
+ * Rows in 8 bits: scale[n] = (the largest magnitude of row n) / 127 and q[n][c] =
+ * 127 x[n][c] / (that magnitude), to the nearest whole number, halves to the even
+ * one: of x as it is, no rounding on the way moves a half.  x [N][D] is of element type
+ * `dtype`; q int8 [N][D]; scale fp32 [N].  Rows of zeros, and rows with a NaN or an
+ * infinity, as in lda_add_norm.
+ */
+int lda_quantise_rows(const void *x, int64_t ld_x, int8_t *q, int64_t ld_q, float *scale,
+                      int64_t N, int32_t D, int32_t dtype, void *stream);
+
+/*
+ * Product of rows and weights in 8 bits:
+ *   out[m][n] = (sum over k of q[m][k] weight[n][k]) * scale[m] * weight_scale[n] + bias[n]
+ * q int8 [M][K], weight int8 [N][K] (a channel's weights contiguous); scale [M],
+ * weight_scale [N] and bias [N] (NULL: none) fp32; out [M][N] of element type `dtype`.
+ * All int8 numbers are taken, -128 too.  The sum is exact; it is rounded to fp32, multiplied
+ * by the two scales in this order, the bias added, and rounded to the output's type.  K up to
+ * LDA_PROJECT_MAX_K (LDA_ERR_UNSUPPORTED above: the sum would pass 32 bits); M up
+ * to LDA_MAX_N.  A row with a NaN for a scale gives NaN.
+ */
+#define LDA_PROJECT_MAX_K 131071
+int lda_project_int8(const int8_t *q, int64_t ld_q, const float *scale, const int8_t *weight,
+                     int64_t ld_weight, const float *weight_scale, const float *bias, void *out,
+                     int64_t ld_out, int64_t M, int32_t N, int32_t K, int32_t dtype,
+                     void *stream);
+
+/*
+ * One token per row of logits [B][V], chosen by the row's uniform number: z[b]
+ * (int32) and prob[b] (fp32), its share of the weights that stay.  Token v has the weight
+ * w_v = exp((x_v - max) / temperature[b]).  Tokens are ordered by falling logit,
+ * equal ones by number.  Of them stay, one rule after another:
+ *   the first top_k[b]                                    (int32; not above 0: all)
+ *   the fewest first ones whose weights reach top_p[b] of the sum of what is left
+ *                                          (fp32; not below 1: all; at least one stays)
+ *   those of at least min_p[b]    (fp32; not above 0: all; above 1 as 1: the largest stay)
+ * With S_v the sum of the weights that stay up to token v, in the order of their
+ * numbers, z is the smallest v with u[b] S < S_v (strict "<", as in the draws of
+ * topics), and the last that stays if there is none (u not below 1).  u fp32 in
+ * [0, 1); below 0 or NaN it counts as 0.  Where the temperature is not above 0 (or NaN)
+ * z is the lowest token with the largest logit and prob 1, whatever the rules; a NULL
+ * temperature, top_k, top_p or min_p is 1, or no such rule.  A NaN logit is never
+ * chosen; logits of +inf share the choice.  A row with nothing to choose (all -inf) gives
+ * z = -1 and prob = 0.
+ * Weights are computed in fp64 and held as whole multiples of 2^-F of the
+ * largest, F = 46 up to V = 131,072 and 63 - ceil(log2 V) above: their sums are exact, so
+ * a row's token does not depend on its place, nor on how the work is split.  A
+ * weight that rounds to 0 is never chosen.
+ * Rules on the logits (lda_penalise_logits) come before; B up to LDA_LOGITS_MAX_ROWS.
+ */
+int lda_sample_logits(const void *logits, int64_t ld_logits, int64_t B, int32_t V, int32_t dtype,
+                      const float *u, const float *temperature, const int32_t *top_k,
+                      const float *top_p, const float *min_p, int32_t *z, float *prob,
+                      void *stream);
+
 /* The W (butterfly width) the library uses for K, or LDA_ERR_UNSUPPORTED /
  * LDA_ERR_SHAPE for a K it rejects. */
 int lda_butterfly_width(int32_t K);

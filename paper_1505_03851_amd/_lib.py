@@ -118,8 +118,9 @@ def load() -> ctypes.CDLL:
     lib.lda_count_topics_indexed.argtypes = [P, P, P, I64, I32, I32, I32, P, ctypes.c_size_t,
                                              P, P, P]
     lib.lda_count_topics_indexed.restype = ctypes.c_int
-    from . import _tokens
+    from . import _layers, _tokens
     _tokens.bind(lib)
+    _layers.bind(lib)
     _lib = lib
     return lib
 

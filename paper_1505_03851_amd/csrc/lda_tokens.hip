@@ -16,6 +16,7 @@
 
 #include "lda_draw.h"
 #include "status.hpp"
+#include "arguments.hpp"
 #include "token_rows.hpp"
 #include "token_grad.hpp"
 #include "logits.hpp"
@@ -31,19 +32,6 @@ constexpr int64_t kClearApart = (64 << 20) / 16;
 
 unsigned grid_of(int64_t tiles) {
   return (unsigned)(tiles < 1 ? 1 : tiles < kMaxBlocks ? tiles : kMaxBlocks);
-}
-
-bool aligned(const void *p, int bytes) {
-  return !(reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1));
-}
-
-int dtype_size(int32_t dtype) {
-  switch (dtype) {
-    case LDA_F32: return 4;
-    case LDA_BF16:
-    case LDA_F16: return 2;
-    default: return 0;
-  }
 }
 
 bool probability(double p) { return p >= 0.0 && p < 1.0; }
