@@ -306,7 +306,6 @@ struct NormGradArgs {
 template <typename T, int WAVES, int UNITS>
 __global__ __launch_bounds__(kNormThreads) void norm_grad_kernel(NormGradArgs<T> a) {
   static_assert(WAVES == 1 || 64 * WAVES == kNormThreads, "a row to a wavefront or a workgroup");
-  using S = typename T::store;
   constexpr int kLanes = 64 * WAVES, kRows = kNormThreads / kLanes;
   constexpr int kColumns = kLanes * UNITS * 8;
   __shared__ float sums[2][2][16];

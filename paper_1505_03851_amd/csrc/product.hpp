@@ -9,9 +9,11 @@
 // operand, so that a lane's four sums are those of four channels next to each other:
 // row l % 16 of q, channels 4 (l / 16) + 0 .. 3.
 //
-// direct_product_kernel: a tile of 16 MT rows and 16 NT channels to a workgroup, whose
-// wavefronts share the length of K and read what they multiply straight into
-// registers; their sums meet in LDS (whole numbers: in any order the same).
+// direct_product_kernel: a tile of 16 rows and 16 channels to a workgroup, whose wavefronts
+// share the length of K and read what they multiply straight into registers; their sums
+// meet in LDS (whole numbers: in any order the same).  For up to 16 rows.
+//
+// tiled_product_kernel: larger tiles, through LDS.
 #pragma once
 
 #include "elements.hpp"
@@ -20,6 +22,11 @@ namespace lda {
 
 typedef int32_t ints4 __attribute__((ext_vector_type(4)));
 typedef ints4 ints4_any __attribute__((aligned(1), may_alias));
+
+template <int N>
+struct Count {
+  static constexpr int value = N;
+};
 
 constexpr int kStep = 64;  // bytes of K that one matrix instruction takes
 
@@ -42,10 +49,12 @@ __device__ __forceinline__ ints4 load_bytes(const int8_t *p, int n) {
   return v;
 }
 
-template <typename T, int MT, int NT>
-__global__ __launch_bounds__(512) void direct_product_kernel(ProductArgs<T> a, uint32_t col_tiles, int64_t tiles) {
-  constexpr int kRows = 16 * MT, kCols = 16 * NT, kPitch = kCols + 4;
-  __shared__ int32_t joined[kRows * kPitch];
+// The wavefronts of a workgroup share the length of K.
+template <typename T>
+__global__ __launch_bounds__(512) void direct_product_kernel(ProductArgs<T> a, uint32_t col_tiles,
+                                                             int64_t tiles) {
+  constexpr int kTile = 16, kPitch = kTile + 4;
+  __shared__ int32_t joined[kTile * kPitch];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int waves = (int)blockDim.x >> 6;
   const int line = lane & 15, part = lane >> 4;
@@ -55,69 +64,322 @@ __global__ __launch_bounds__(512) void direct_product_kernel(ProductArgs<T> a, u
   const int whole = to * kStep <= a.K ? to : to - 1;
   for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const int64_t row_tile = tile / col_tiles;
-    const int64_t m0 = row_tile * kRows, n0 = (tile - row_tile * col_tiles) * kCols;
-    for (int i = (int)threadIdx.x; i < kRows * kPitch; i += (int)blockDim.x) joined[i] = 0;
-    const int8_t *q[MT], *w[NT];
+    const int64_t m0 = row_tile * kTile, n0 = (tile - row_tile * col_tiles) * kTile;
+    for (int i = (int)threadIdx.x; i < kTile * kPitch; i += (int)blockDim.x) joined[i] = 0;
+    const int64_t m_in = m0 + line < a.M ? m0 + line : a.M - 1;
+    const int64_t n_in = n0 + line < a.N ? n0 + line : a.N - 1;
+    const int8_t *q = a.q + m_in * a.ldq + 16 * part, *w = a.w + n_in * a.ldw + 16 * part;
+    ints4 sum = {0, 0, 0, 0};
+    // (loads first: a matrix instruction keeps the compiler from unrolling a loop)
+    const auto steps_at = [&](auto count, int s) {
+      constexpr int kCount = decltype(count)::value;
+      ints4 x[kCount], y[kCount];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int64_t m = m0 + 16 * i + line;
-      q[i] = a.q + (m < a.M ? m : a.M - 1) * a.ldq + 16 * part;
-    }
+      for (int i = 0; i < kCount; ++i) {
+        y[i] = *reinterpret_cast<const ints4_any *>(w + (s + i) * kStep);
+        x[i] = *reinterpret_cast<const ints4_any *>(q + (s + i) * kStep);
+      }
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int64_t n = n0 + 16 * j + line;
-      w[j] = a.w + (n < a.N ? n : a.N - 1) * a.ldw + 16 * part;
-    }
-    ints4 sum[MT][NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int j = 0; j < NT; ++j) sum[i][j] = ints4{0, 0, 0, 0};
-#pragma unroll(MT * NT >= 8 ? 2 : 4)
-    for (int s = from; s < whole; ++s) {
-      ints4 x[MT], y[NT];
-#pragma unroll
-      for (int j = 0; j < NT; ++j) y[j] = *reinterpret_cast<const ints4_any *>(w[j] + s * kStep);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) x[i] = *reinterpret_cast<const ints4_any *>(q[i] + s * kStep);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-          sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(y[j], x[i], sum[i][j], 0, 0, 0);
-    }
+      for (int i = 0; i < kCount; ++i)
+        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(y[i], x[i], sum, 0, 0, 0);
+    };
+    int s = from;
+    for (; s + 8 <= whole; s += 8) steps_at(Count<8>(), s);
+    if (s + 4 <= whole) steps_at(Count<4>(), s), s += 4;
+    if (s + 2 <= whole) steps_at(Count<2>(), s), s += 2;
+    if (s < whole) steps_at(Count<1>(), s);
     if (from < to && whole < to) {
       const int n = a.K - whole * kStep - 16 * part;
-      ints4 x[MT], y[NT];
-#pragma unroll
-      for (int j = 0; j < NT; ++j) y[j] = load_bytes(w[j] + whole * kStep, n);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) x[i] = load_bytes(q[i] + whole * kStep, n);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-          sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(y[j], x[i], sum[i][j], 0, 0, 0);
+      sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(load_bytes(w + whole * kStep, n),
+                                                  load_bytes(q + whole * kStep, n), sum, 0, 0, 0);
     }
     __syncthreads();  // cleared
     if (from < to) {
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            atomicAdd(&joined[(16 * i + line) * kPitch + 16 * j + 4 * part + r], sum[i][j][r]);
+      for (int r = 0; r < 4; ++r) atomicAdd(&joined[line * kPitch + 4 * part + r], sum[r]);
     }
     __syncthreads();
-    for (int i = (int)threadIdx.x; i < kRows * kCols; i += (int)blockDim.x) {
-      const int64_t m = m0 + i / kCols, n = n0 + i % kCols;
+    for (int i = (int)threadIdx.x; i < kTile * kTile; i += (int)blockDim.x) {
+      const int64_t m = m0 + i / kTile, n = n0 + i % kTile;
       if (m >= a.M || n >= a.N) continue;
-      float v = (float)joined[(i / kCols) * kPitch + i % kCols] * a.scale[m] * a.weight_scale[n];
+      float v = (float)joined[i / kTile * kPitch + i % kTile] * a.scale[m] * a.weight_scale[n];
       if (a.bias) v += a.bias[n];
       a.out[m * a.ldo + n] = T::down(v);
     }
     __syncthreads();  // read before the next tile clears it
+  }
+}
+
+// ---- tiles through LDS
+//
+// A workgroup takes BM rows by BN channels: WM x WN wavefronts with (BM / WM) x
+// (BN / WN) of them each, GROUPS times over, the groups sharing the length of K.  It
+// passes by in stages of 128 bytes for each group, each line of which goes from memory to
+// LDS without passing registers, STAGES - 1 of them ahead of the one that is multiplied.  A
+// line's 16-byte pieces lie in LDS in the order piece ^ (line % 8): a matrix operand's
+// 16 lines would otherwise be in the same banks.  Lines past the last are the last one
+// again (their sums are not stored); pieces past K are piece 0 again, and the rows'
+// operand is cleared there.  ANY: lines that do not start at 16 bytes, or K that is no
+// multiple of 16, pass through registers.
+//
+// Workgroups start at different stages, each XCD's at others: lines often lie a
+// power of two apart, so that the same stage of all of them is in a few of the memory's
+// channels.
+//
+// A workgroup takes tile after tile, the next one's first stage on its way while this
+// one's sums go out: by rows through LDS, whole lines of memory at a time.
+
+constexpr int kStage = 128;
+
+typedef __attribute__((address_space(3))) void *lds_pointer;
+typedef const __attribute__((address_space(1))) void *global_pointer;
+
+// Waits until at most N of this wavefront's loads are on their way, and all it asked of
+// LDS is done; then for the other wavefronts.
+template <int N>
+__device__ __forceinline__ void arrive() {
+  static_assert(N < 64, "six bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (0 << 8) | ((N >> 4) << 14));
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <typename T, int BM, int BN, int WM, int WN, int GROUPS, int STAGES, bool ANY>
+__global__ __launch_bounds__(64 * WM * WN * GROUPS) void tiled_product_kernel(ProductArgs<T> a,
+                                                                               uint32_t row_tiles,
+                                                                               uint32_t tiles) {
+  using S = typename T::store;
+  constexpr int kWaves = WM * WN * GROUPS, kRows = BM / WM, kCols = BN / WN;
+  constexpr int MT = kRows / 16, NT = kCols / 16;
+  // a wavefront's loads a stage, 8 lines each
+  constexpr int kQ = BM * GROUPS / 8 / kWaves, kW = BN * GROUPS / 8 / kWaves;
+  constexpr int kBytes = (BM + BN) * GROUPS * kStage;  // of a stage
+  constexpr int kFirstW = BM * GROUPS;                 // lines of a stage before the weights'
+  static_assert(kQ * 8 * kWaves == BM * GROUPS && kW * 8 * kWaves == BN * GROUPS, "whole loads");
+  static_assert(STAGES >= 2 && STAGES <= 4 && (!ANY || STAGES == 2), "stages");
+  static_assert(GROUPS == 1 || (GROUPS - 1) * BM * BN * 4 <= kBytes, "room for the groups' sums");
+  // one array to a stage: the compiler then knows that a stage is not written while
+  // another one is read
+  __shared__ __attribute__((aligned(16))) int8_t stage0[kBytes], stage1[kBytes],
+      stage2[STAGES > 2 ? kBytes : 16], stage3[STAGES > 3 ? kBytes : 16];
+  const int lane = (int)threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int group = wave / (WM * WN), place = wave % (WM * WN);
+  const int line = lane & 15, part = lane >> 4;
+  const int first_q = place / WN * kRows, first_w = place % WN * kCols;
+  const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+  const int stages = (a.K + kStage * GROUPS - 1) / (kStage * GROUPS);
+  const int turn = (int)((blockIdx.x % 8 * 4 + blockIdx.x / 8) % (uint32_t)stages);
+  const auto turned = [&](int s) { return s + turn < stages ? s + turn : s + turn - stages; };
+
+  int64_t m0, n0;
+  uint32_t q_at[kQ], w_at[kW];
+  const auto take = [&](uint32_t tile) {
+    m0 = (int64_t)(tile % row_tiles) * BM;
+    n0 = (int64_t)(tile / row_tiles) * BN;
+#pragma unroll
+    for (int i = 0; i < kQ; ++i) {
+      const int64_t r = (wave * kQ + i) * 8 % BM + (lane >> 3), most = a.M - 1 - m0;
+      q_at[i] = (uint32_t)((r < most ? r : most) * a.ldq);
+    }
+#pragma unroll
+    for (int i = 0; i < kW; ++i) {
+      const int64_t r = (wave * kW + i) * 8 % BN + (lane >> 3), most = a.N - 1 - n0;
+      w_at[i] = (uint32_t)((r < most ? r : most) * a.ldw);
+    }
+  };
+  // f(address in memory, line of the stage, its first byte's place in K) of this lane's loads
+  const auto each_load = [&](int stage, auto f) {
+    const int8_t *q = a.q + m0 * a.ldq, *w = a.w + n0 * a.ldw;
+#pragma unroll
+    for (int i = 0; i < kQ; ++i) {
+      const int at = (stage * GROUPS + (wave * kQ + i) * 8 / BM) * kStage + piece;
+      f(i, q + (q_at[i] + (uint32_t)(at < a.K ? at : 0)), (wave * kQ + i) * 8, at);
+    }
+#pragma unroll
+    for (int i = 0; i < kW; ++i) {
+      const int at = (stage * GROUPS + (wave * kW + i) * 8 / BN) * kStage + piece;
+      f(kQ + i, w + (w_at[i] + (uint32_t)(at < a.K ? at : 0)), kFirstW + (wave * kW + i) * 8, at);
+    }
+  };
+  const auto bring = [&](int s, int8_t *to) {
+    each_load(turned(s), [&](int, const int8_t *from, int first, int) {
+      __builtin_amdgcn_global_load_lds((global_pointer)from, (lds_pointer)(to + first * kStage), 16,
+                                       0, 0);
+    });
+  };
+  ints4 held[ANY ? kQ + kW : 1];
+  const auto fetch = [&](int s) {
+    const int stage = turned(s);
+    if ((stage + 1) * GROUPS * kStage <= a.K)
+      each_load(stage, [&](int i, const int8_t *from, int, int) {
+        held[i] = *reinterpret_cast<const ints4_any *>(from);
+      });
+    else
+      each_load(stage, [&](int i, const int8_t *from, int, int at) { held[i] = load_bytes(from, a.K - at); });
+  };
+  const auto keep = [&](int8_t *to) {
+    each_load(0, [&](int i, const int8_t *, int first, int) {
+      *reinterpret_cast<ints4 *>(to + first * kStage + lane * 16) = held[i];
+    });
+  };
+  ints4 sum[MT][NT];
+  const auto multiply = [&](int s, const int8_t *from) {
+    const int k0 = (turned(s) * GROUPS + group) * kStage;
+    const bool tail = k0 + kStage > a.K;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int8_t *at = from + ((4 * half + part) ^ (line & 7)) * 16 + line * kStage;
+      ints4 x[MT], y[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        y[j] = *reinterpret_cast<const ints4 *>(at + (kFirstW + group * BN + first_w + 16 * j) * kStage);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        x[i] = *reinterpret_cast<const ints4 *>(at + (group * BM + first_q + 16 * i) * kStage);
+      if (tail && k0 + (4 * half + part) * 16 >= a.K) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) x[i] = ints4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+          sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(y[j], x[i], sum[i][j], 0, 0, 0);
+    }
+  };
+  // stage s, in `here`; the stage STAGES - 1 after it goes to `free`, which was read last
+  const auto step = [&](int s, const int8_t *here, int8_t *free) {
+    const bool more = s + STAGES - 1 < stages;
+    if constexpr (ANY) {
+      arrive<0>();
+      if (more) fetch(s + 1);
+      multiply(s, here);
+      if (more) keep(free);
+    } else {
+      if (s + STAGES - 2 < stages)
+        arrive<(STAGES - 2) * (kQ + kW)>();
+      else
+        arrive<0>();
+      if (more) bring(s + STAGES - 1, free);
+      multiply(s, here);
+    }
+  };
+  const auto first_stage = [&](int8_t *to) {
+    if constexpr (ANY) {
+      fetch(0);
+      keep(to);
+    } else {
+      bring(0, to);
+    }
+  };
+
+  uint32_t tile = blockIdx.x;
+  take(tile);
+  first_stage(stage0);
+  while (true) {
+    if (STAGES > 2 && stages > 1) bring(1, stage1);
+    if (STAGES > 3 && stages > 2) bring(2, stage2);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) sum[i][j] = ints4{0, 0, 0, 0};
+    for (int s = 0; s < stages; s += STAGES) {
+      if constexpr (STAGES == 2) {
+        step(s, stage0, stage1);
+        if (s + 1 < stages) step(s + 1, stage1, stage0);
+      } else if constexpr (STAGES == 3) {
+        step(s, stage0, stage2);
+        if (s + 1 < stages) step(s + 1, stage1, stage0);
+        if (s + 2 < stages) step(s + 2, stage2, stage1);
+      } else {
+        step(s, stage0, stage3);
+        if (s + 1 < stages) step(s + 1, stage1, stage0);
+        if (s + 2 < stages) step(s + 2, stage2, stage1);
+        if (s + 3 < stages) step(s + 3, stage3, stage2);
+      }
+    }
+    arrive<0>();  // everyone has read the last stage
+    if constexpr (GROUPS > 1) {  // the first group adds the others' sums to its own
+      ints4 *room = reinterpret_cast<ints4 *>(stage1) + (size_t)place * MT * NT * 64 + lane;
+      constexpr int kGroup = BM * BN / 4;
+      if (group > 0) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) room[(group - 1) * kGroup + (i * NT + j) * 64] = sum[i][j];
+      }
+      arrive<0>();
+      if (group == 0) {
+#pragma unroll
+        for (int g = 0; g < GROUPS - 1; ++g)
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) sum[i][j] += room[g * kGroup + (i * NT + j) * 64];
+      }
+      arrive<0>();  // read, before rows go out through the same memory
+    }
+    const int64_t m_out = m0 + first_q, n_out = n0 + first_w;
+    tile += gridDim.x;
+    const bool more = tile < tiles;
+    if (more) {
+      take(tile);
+      first_stage(stage0);
+    }
+    // The sums leave through this wavefront's share of the second stage's memory, as
+    // many rows at a time as fit.
+    constexpr int kPitch = kCols * (int)sizeof(S) + 16;
+    constexpr int kShare = kBytes / (WM * WN) / 16 * 16;
+    constexpr int kRoom = kShare / kPitch / 16 * 16;
+    constexpr int kPass = kRoom < kRows ? kRoom : kRows;
+    static_assert(kPass >= 16, "room for 16 rows");
+    constexpr int kLaneCols = 16 / (int)sizeof(S), kLanes = kCols / kLaneCols;  // of a row
+    int8_t *room = stage1 + place * kShare;
+    float ws[NT][4], b[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int64_t n = n_out + 16 * j + 4 * part;
+      const int left = a.N - n < 0 ? 0 : a.N - n < 4 ? (int)(a.N - n) : 4;
+      load_elements<F32, 4>(a.weight_scale + (left ? n : 0), left, ws[j]);
+      load_elements<F32, 4>(a.bias + (a.bias && left ? n : 0), a.bias ? left : 0, b[j]);
+    }
+#pragma unroll
+    for (int r0 = 0; r0 < kRows && group == 0; r0 += kPass) {
+#pragma unroll
+      for (int i = r0 / 16; i < (r0 + kPass < kRows ? r0 + kPass : kRows) / 16; ++i) {
+        const int64_t m = m_out + 16 * i + line;
+        const float s = a.scale[m < a.M ? m : a.M - 1];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          Packed<T, 4> v;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v.v[r] = T::down((float)sum[i][j][r] * s * ws[j][r] + b[j][r]);
+          *reinterpret_cast<Packed<T, 4> *>(room + (16 * i - r0 + line) * kPitch +
+                                            (16 * j + 4 * part) * (int)sizeof(S)) = v;
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+      // (LDS works in order within a wavefront)
+#pragma unroll
+      for (int i = 0; i < kPass; i += 64 / kLanes) {
+        const int r = i + lane / kLanes, c = lane % kLanes * kLaneCols;
+        const int64_t m = m_out + r0 + r, n = n_out + c;
+        if (r0 + r >= kRows || r >= kPass || m >= a.M || n >= a.N) continue;
+        const auto *from = reinterpret_cast<const Packed<T, kLaneCols> *>(
+            room + r * kPitch + c * (int)sizeof(S));
+        S *to = a.out + m * a.ldo + n;
+        if (a.N - n >= kLaneCols) {
+          *reinterpret_cast<words4_any *>(to) = __builtin_bit_cast(words4, *from);
+        } else {
+          for (int e = 0; e < (int)(a.N - n); ++e) to[e] = from->v[e];
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    if (!more) break;
+    if (STAGES > 2) arrive<0>();  // everyone has read what the next stage's loads overwrite
   }
 }
 
