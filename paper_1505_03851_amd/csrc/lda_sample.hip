@@ -25,9 +25,20 @@ template <typename T>
 int launch_sample(const void *logits, int64_t ld, int64_t B, int32_t V, const float *u,
                   const float *temperature, const int32_t *top_k, const float *top_p,
                   const float *min_p, int32_t *z, float *prob, hipStream_t s) {
-  sample_kernel<T><<<(unsigned)(B < kMaxRows ? B : kMaxRows), kSampleThreads, 0, s>>>(
-      (const typename T::store *)logits, ld, B, V, weight_digits(V), u, temperature, top_k, top_p,
-      min_p, z, prob);
+  // chunks of a lane that stay in registers: 4 or as many as fit in 64
+  constexpr int kMost = 64 / (2 * (int)sizeof(typename T::store));
+  const int64_t chunks = ((int64_t)V + 8 * kSampleThreads - 1) / (8 * kSampleThreads);
+#define LDA_SAMPLE(CHUNKS)                                                                      \
+  sample_kernel<T, CHUNKS><<<(unsigned)(B < kMaxRows ? B : kMaxRows), kSampleThreads, 0, s>>>( \
+      (const typename T::store *)logits, ld, B, V, weight_digits(V), u, temperature, top_k,    \
+      top_p, min_p, z, prob)
+  if (chunks <= 4)
+    LDA_SAMPLE(4);
+  else if (chunks <= kMost)
+    LDA_SAMPLE(kMost);
+  else
+    LDA_SAMPLE(0);
+#undef LDA_SAMPLE
   return launch_status();
 }
 
