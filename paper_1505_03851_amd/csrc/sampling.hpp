@@ -35,6 +35,7 @@ constexpr int kSampleThreads = 1024;
 constexpr int kSampleWaves = kSampleThreads / 64;
 constexpr int kBins = 2 * kSampleThreads;
 constexpr int kListed = kSampleThreads;  // tokens of a list, one to a lane
+constexpr int kCompared = 256;           // of those that are compared with each other
 constexpr int kFewest = 512;             // the largest top_k that is looked for by a bound
 
 // Logits as keys that rise as they fall, from the bits of a float, bfloat16 or half.
@@ -136,6 +137,8 @@ struct SampleShared {
   uint32_t tops[kSampleWaves];
   uint64_t pick_before, pick_at;
   uint32_t bin, listed;
+  unsigned long long mass[kCompared], before[kCompared], total;
+  uint32_t rank[kCompared], worst[kSampleWaves];
 };
 
 // The sum of the lanes' x up to this one, and of all; the wavefronts' sums stay in
@@ -196,7 +199,7 @@ __device__ __forceinline__ void clear_bins(SampleShared &sh) {
 // The search over the members' keys from lo to hi for the first up to which the amounts
 // reach target(sum of all), which is at least 1.  each(add) calls add(key, amount) for the
 // members (others than those of lo .. hi are passed over, their amount not asked for).
-// `levels` 1: the last key of the interval that holds it, after one level.
+// Where `levels` come to their end first: the last key of the interval that holds it.
 template <typename Target, typename Each>
 __device__ Found search(SampleShared &sh, uint32_t lo, uint32_t hi, int levels, Target target_of,
                         Each each) {
@@ -228,6 +231,7 @@ __device__ Found search(SampleShared &sh, uint32_t lo, uint32_t hi, int levels, 
 // wavefronts by lane, others through `room`.
 __device__ __forceinline__ uint64_t sorted(uint64_t v, int width, uint64_t *room) {
   const int t = (int)threadIdx.x;
+  const bool idle = uniform((uint32_t)t & ~63u) >= (uint32_t)width;
   for (int size = 2; size <= width; size *= 2)
     for (int apart = size / 2; apart > 0; apart /= 2) {
       uint64_t other;
@@ -236,6 +240,8 @@ __device__ __forceinline__ uint64_t sorted(uint64_t v, int width, uint64_t *room
         room[t] = v;
         __syncthreads();
         other = room[t ^ apart];
+      } else if (idle) {
+        continue;
       } else {
         other = (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), apart) << 32 |
                 (uint32_t)__shfl_xor((int)(uint32_t)v, apart);
@@ -325,10 +331,12 @@ struct SampleRow {
 // The tokens that stay by their order: logits above `last`, and of those at it the
 // numbers below `end`.
 struct Stay {
-  float last;
+  float last, above;
   uint32_t end;
+  __device__ __forceinline__ Stay(float l, uint32_t e)
+      : last(l), above(uniform(nextafterf(l, __builtin_inff()))), end(e) {}
   __device__ __forceinline__ bool operator()(float x, uint32_t i) const {
-    return x > last || (x == last && i < end);
+    return x >= (i < end ? last : above);
   }
 };
 
@@ -351,9 +359,78 @@ struct SampleSettings {
   double floor;  // in steps
 };
 
-// The choice among the n tokens of the list.
+// The choice among the n tokens of the list, up to 256, each compared with all others: its
+// rank and the weight of those before it, in their order and then by number.
 template <typename T>
-__device__ void choose_listed(SampleShared &sh, int n, const Weights &weights,
+__device__ void choose_compared(SampleShared &sh, int n, const Weights &weights,
+                                const SampleSettings &s, int32_t *z, float *prob) {
+  const int t = (int)threadIdx.x;
+  const int width = n <= 64 ? 64 : n <= 128 ? 128 : 256;  // (a wavefront's lanes share a `part`)
+  const int i = t & (width - 1), part = (int)uniform((uint32_t)t / (uint32_t)width);
+  const int parts = kSampleThreads / width;
+  if (t < kCompared) {
+    sh.mass[t] = sh.before[t] = 0;
+    sh.rank[t] = 0;
+  }
+  if (t == 0) sh.total = 0;
+  const uint64_t mine = i < n ? sh.list.place[i] : ~0ull;
+  uint64_t weight = 0;
+  double w = 0.0;
+  if (part == 0) {
+    const float x = Keys<T>::logit((uint32_t)(mine >> 32));
+    w = weights.of(x, i < n && x > weights.least);
+    weight = Weights::steps(w);
+    sh.list.weight[i] = weight;
+  }
+  __syncthreads();
+  uint32_t rank = 0;
+  uint64_t mass = 0;
+  for (int j = part; j < n; j += parts)
+    if (sh.list.place[j] < mine) {
+      ++rank;
+      mass += sh.list.weight[j];
+    }
+  if (i < n && rank) {
+    atomicAdd(&sh.rank[i], rank);
+    atomicAdd(&sh.mass[i], (unsigned long long)mass);
+  }
+  __syncthreads();
+  if (part == 0) {
+    weight = s.k == 0 || sh.rank[i] < s.k ? weight : 0;
+    const uint64_t sum = wave_inclusive_sum(weight);
+    if ((t & 63) == 63) atomicAdd(&sh.total, (unsigned long long)sum);
+  }
+  __syncthreads();
+  if (part == 0) {
+    const bool stays = !(s.p < 1.0f) || sh.mass[i] < share_of(sh.total, s.p);
+    weight = stays && w >= s.floor ? weight : 0;
+    sh.list.weight[i] = weight;
+  }
+  __syncthreads();
+  const uint32_t number = (uint32_t)mine;
+  uint64_t before = 0, all = 0;
+  for (int j = part; j < n; j += parts) {
+    const uint64_t other = sh.list.weight[j];
+    all += other;
+    before += (uint32_t)sh.list.place[j] < number ? other : 0;
+  }
+  if (t == 0) sh.total = 0;
+  if (i < n && before) atomicAdd(&sh.before[i], (unsigned long long)before);
+  __syncthreads();
+  if (i == 0) atomicAdd(&sh.total, (unsigned long long)all);
+  __syncthreads();
+  if (part == 0 && weight) {
+    const uint64_t point = point_of(sh.total, s.u) - sh.before[i];  // (wraps where it lies before)
+    if (point < weight) {
+      *z = (int32_t)number;
+      *prob = (float)((double)weight / (double)sh.total);
+    }
+  }
+}
+
+// The choice among the n tokens of the list, sorted.
+template <typename T>
+__device__ void choose_sorted(SampleShared &sh, int n, const Weights &weights,
                               const SampleSettings &s, int32_t *z, float *prob) {
   const int t = (int)threadIdx.x, width = sort_width(n);
   const uint64_t place = sorted(t < n ? sh.list.place[t] : ~0ull, width, sh.list.weight);
@@ -400,8 +477,12 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
     row.load();
     float best = -infinity;  // of this lane
     row.all([&](uint32_t, float x) { best = fmaxf(best, x); });
-    const uint32_t wave_best = wave_min(Keys<T>::of(best));
-    if (lane == 0) sh.tops[wave] = wave_best;
+    const uint32_t best_key = Keys<T>::of(best);
+    const uint32_t wave_best = wave_min(best_key), wave_worst = ~wave_min(~best_key);
+    if (lane == 0) {
+      sh.tops[wave] = wave_best;
+      sh.worst[wave] = wave_worst;
+    }
     if (t == 0) sh.listed = 0;
     __syncthreads();
     uint32_t top_key = uniform(sh.tops[0]);
@@ -459,10 +540,13 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
     if (all_listed || (s.k && s.k <= kFewest)) {
       float bound = -infinity;
       if (!all_listed) {
-        const uint32_t mine = Keys<T>::of(best);
+        uint32_t worst_key = 0;
+        for (int i = 0; i < kSampleWaves; ++i) worst_key = sh.worst[i] > worst_key ? sh.worst[i] : worst_key;
+        const uint32_t end = Keys<T>::of(-infinity) - 1;
+        worst_key = uniform(worst_key < end ? worst_key : end);
         const Found f = search(
-            sh, top_key, Keys<T>::of(-infinity) - 1, 1, [&](uint64_t) { return s.k; },
-            [&](auto add) { add(mine, one); });
+            sh, top_key, worst_key, 2, [&](uint64_t) { return s.k; },
+            [&](auto add) { add(best_key, one); });
         // (not there: fewer lanes than k hold any)
         if (f.there) bound = uniform(Keys<T>::logit(f.key));
       }
@@ -476,7 +560,10 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       __syncthreads();
       const int n = (int)uniform(sh.listed);
       if (n <= kListed) {
-        choose_listed<T>(sh, n, weights, s, z + b, prob + b);
+        if (n <= kCompared)
+          choose_compared<T>(sh, n, weights, s, z + b, prob + b);
+        else
+          choose_sorted<T>(sh, n, weights, s, z + b, prob + b);
         __syncthreads();
         continue;
       }
@@ -515,9 +602,13 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       if (t == 0) sh.listed = 0;
       const Found f = reached(sh, 0, target_once);
       if (!f.there) return;
-      __syncthreads();  // bins and list share their memory
+      // (the bin's logits, and a hundredth of a bin around them for the roundings)
+      const double bin = 1.0 / (double)per_bin;
+      const float high = uniform((float)((double)top - ((double)f.key - 0.01) * bin));
+      const float low_end = f.key == kBins - 1 ? -infinity : (float)((double)top - ((double)f.key + 1.01) * bin);
+      const float low = uniform(low_end);
       row.all([&](uint32_t i, float x) {
-        if (stay(x, i) && bin_of(x) == f.key) {
+        if (x <= high && x >= low && stay(x, i) && bin_of(x) == f.key) {
           const uint32_t at = atomicAdd(&sh.listed, 1);
           if (at < (uint32_t)kListed) sh.list.place[at] = (uint64_t)Keys<T>::of(x) << 32 | i;
         }
@@ -560,8 +651,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
 
     // ---- the choice
     // (a lane's weights add up to 2^53 at most, exactly in double)
-    const auto staying = [&](uint32_t i, float x) {
-      const double w = weights.of(x, stay(x, i));
+    const auto staying = [&](uint32_t, float x) {
+      const double w = weights.of(x, true);
       return w >= s.floor ? Weights::rounded(w) : 0.0;
     };
     double mine = 0.0;
