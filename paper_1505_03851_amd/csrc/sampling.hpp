@@ -100,10 +100,10 @@ struct Weights {
     p = fma_by(p, f, 0.24022650695910075);
     p = fma_by(p, f, 0.6931471805599462);
     p = fma(p, f, 1.0);
-    const uint64_t bits = __builtin_bit_cast(uint64_t, p);
-    const uint32_t high =
-        (uint32_t)(bits >> 32) + ((uint32_t)__builtin_bit_cast(uint64_t, m) << 20);
-    return __builtin_bit_cast(double, (uint64_t)(there ? high : 0) << 32 | (uint32_t)bits);
+    words2 bits = __builtin_bit_cast(words2, p);
+    bits[1] += __builtin_bit_cast(words2, m)[0] << 20;
+    bits[1] = there ? bits[1] : 0;
+    return __builtin_bit_cast(double, bits);
   }
   // the same as a whole number, by the last place of 2^52
   static __device__ __forceinline__ double rounded(double w) { return (w + 0x1p52) - 0x1p52; }
@@ -266,25 +266,28 @@ template <typename T, int CHUNKS>
 struct SampleRow {
   using S = typename T::store;
   static constexpr int kWords = 2 * (int)sizeof(S);  // of a chunk
-  typedef uint32_t held __attribute__((ext_vector_type(CHUNKS ? CHUNKS : 2)));
+  // sixteen registers that a scalar numbers: word w of chunk i is register i kPart + w % kPart
+  // of vector w / kPart
+  static constexpr int kPart = CHUNKS ? 16 / CHUNKS : 1;
+  typedef uint32_t held __attribute__((ext_vector_type(16)));
   typedef uint32_t chunk __attribute__((ext_vector_type(kWords)));
 
   const S *x;
   int32_t V;
   int each;
-  held words[kWords];
+  held words[CHUNKS ? kWords / kPart : 1];
 
   __device__ __forceinline__ uint32_t first(int wave, int i) const {
     return (((uint32_t)wave * (uint32_t)each + (uint32_t)i) * 64 + (threadIdx.x & 63)) * 8;
   }
-  // -inf past the end
+  // NaN past the end: never chosen
   __device__ __forceinline__ chunk read(int wave, int i) const {
     const uint32_t at = first(wave, i);
     const int n = i >= each || at >= (uint32_t)V ? 0 : (uint32_t)V - at < 8 ? (int)((uint32_t)V - at) : 8;
     Packed<T, 8> p = load_packed<T, 8>(x + (n ? at : 0), n);
     if (n < 8) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) p.v[j] = j < n ? p.v[j] : T::down(-__builtin_inff());
+      for (int j = 0; j < 8; ++j) p.v[j] = j < n ? p.v[j] : T::down(__builtin_nanf(""));
     }
     return __builtin_bit_cast(chunk, p);
   }
@@ -301,11 +304,11 @@ struct SampleRow {
       for (int i = 0; i < CHUNKS; ++i) {
         const chunk c = read(wave, i);
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) words[w][i] = c[w];
+        for (int w = 0; w < kWords; ++w) words[w / kPart][i * kPart + w % kPart] = c[w];
       }
     }
   }
-  // f(number, logit) of all of this lane's
+  // f(number of a chunk's first, place in the chunk, logit) of all of this lane's
   template <typename F>
   __device__ __forceinline__ void all(F f) const {
     const int wave = (int)uniform(threadIdx.x >> 6);
@@ -314,14 +317,14 @@ struct SampleRow {
       chunk c;
       if constexpr (CHUNKS > 0) {
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) c[w] = words[w][i];
+        for (int w = 0; w < kWords; ++w) c[w] = words[w / kPart][i * kPart + w % kPart];
       } else {
         c = read(wave, i);
       }
       const uint32_t at = first(wave, i);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        f(at + j, element(c, j));
+        f(at, j, element(c, j));
         if (j & 1) __builtin_amdgcn_sched_barrier(0);  // (two weights' registers at a time)
       }
     }
@@ -329,14 +332,14 @@ struct SampleRow {
 };
 
 // The tokens that stay by their order: logits above `last`, and of those at it the
-// numbers below `end`.
+// numbers below `end` (2^31 - 1 at most).
 struct Stay {
   float last, above;
   uint32_t end;
   __device__ __forceinline__ Stay(float l, uint32_t e)
       : last(l), above(uniform(nextafterf(l, __builtin_inff()))), end(e) {}
-  __device__ __forceinline__ bool operator()(float x, uint32_t i) const {
-    return x >= (i < end ? last : above);
+  __device__ __forceinline__ bool operator()(float x, uint32_t at, int j) const {
+    return x >= (j < (int32_t)(end - at) ? last : above);
   }
 };
 
@@ -476,7 +479,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
                      uniform(low > 0.0f ? ldexp(fmin((double)low, 1.0), digits) : 0.0)};
     row.load();
     float best = -infinity;  // of this lane
-    row.all([&](uint32_t, float x) { best = fmaxf(best, x); });
+    row.all([&](uint32_t, int, float x) { best = fmaxf(best, x); });
     const uint32_t best_key = Keys<T>::of(best);
     const uint32_t wave_best = wave_min(best_key), wave_worst = ~wave_min(~best_key);
     if (lane == 0) {
@@ -516,8 +519,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
             return point + 1;
           },
           [&](auto add) {
-            row.all([&](uint32_t i, float x) {
-              if (x == top) add(i, one);
+            row.all([&](uint32_t at, int j, float x) {
+              if (x == top) add(at + j, one);
             });
           });
       if (t == 0) {
@@ -535,10 +538,15 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
     least = uniform(least < top ? least : nextafterf(top, -infinity));
     const Weights weights{uniform((double)top), per, uniform(0x1.8p52 + (double)digits), least};
 
+    const auto list = [&](uint32_t number, float x) {
+      const uint32_t n = atomicAdd(&sh.listed, 1);
+      if (n < (uint32_t)kListed) sh.list.place[n] = (uint64_t)Keys<T>::of(x) << 32 | number;
+    };
+
     // ---- few: a list
     const bool all_listed = V <= kListed;
     if (all_listed || (s.k && s.k <= kFewest)) {
-      float bound = -infinity;
+      float bound = -3.4028234663852886e38f;
       if (!all_listed) {
         uint32_t worst_key = 0;
         for (int i = 0; i < kSampleWaves; ++i) worst_key = sh.worst[i] > worst_key ? sh.worst[i] : worst_key;
@@ -551,11 +559,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
         if (f.there) bound = uniform(Keys<T>::logit(f.key));
       }
       __syncthreads();  // bins and list share their memory
-      row.all([&](uint32_t i, float x) {
-        if (x >= bound && x > -infinity) {
-          const uint32_t at = atomicAdd(&sh.listed, 1);
-          if (at < (uint32_t)kListed) sh.list.place[at] = (uint64_t)Keys<T>::of(x) << 32 | i;
-        }
+      row.all([&](uint32_t at, int j, float x) {
+        if (x >= bound) list(at + j, x);
       });
       __syncthreads();
       const int n = (int)uniform(sh.listed);
@@ -576,7 +581,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
     float lowest = least;
     if (heat > 2.0f) {
       float mine = top;
-      row.all([&](uint32_t, float x) { mine = x > least ? fminf(mine, x) : mine; });
+      row.all([&](uint32_t, int, float x) { mine = x > least ? fminf(mine, x) : mine; });
       const uint32_t key = ~wave_min(~Keys<T>::of(mine));
       __syncthreads();  // `tops` is read
       if (lane == 0) sh.tops[wave] = key;
@@ -593,11 +598,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       uint64_t target = 0;
       const auto target_once = [&](uint64_t all) { return target = uniform(target_of(all)); };
       clear_bins(sh);
-      row.all([&](uint32_t i, float x) {
-        if (stay(x, i)) {
-          const uint64_t a = amount(x);
-          if (a) atomicAdd(&sh.bins[bin_of(x)], (unsigned long long)a);
-        }
+      row.all([&](uint32_t at, int j, float x) {
+        if (stay(x, at, j)) atomicAdd(&sh.bins[bin_of(x)], (unsigned long long)amount(x));
       });
       if (t == 0) sh.listed = 0;
       const Found f = reached(sh, 0, target_once);
@@ -607,11 +609,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       const float high = uniform((float)((double)top - ((double)f.key - 0.01) * bin));
       const float low_end = f.key == kBins - 1 ? -infinity : (float)((double)top - ((double)f.key + 1.01) * bin);
       const float low = uniform(low_end);
-      row.all([&](uint32_t i, float x) {
-        if (x <= high && x >= low && stay(x, i) && bin_of(x) == f.key) {
-          const uint32_t at = atomicAdd(&sh.listed, 1);
-          if (at < (uint32_t)kListed) sh.list.place[at] = (uint64_t)Keys<T>::of(x) << 32 | i;
-        }
+      row.all([&](uint32_t at, int j, float x) {
+        if (x <= high && x >= low && stay(x, at, j) && bin_of(x) == f.key) list(at + j, x);
       });
       __syncthreads();
       const int n = (int)uniform(sh.listed);
@@ -629,18 +628,18 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       const Found g = search(
           sh, top_key, Keys<T>::of(-infinity) - 1, 32, [&](uint64_t) { return target; },
           [&](auto add) {
-            row.all([&](uint32_t i, float x) {
-              if (stay(x, i)) add(Keys<T>::of(x), [&] { return amount(x); });
+            row.all([&](uint32_t at, int j, float x) {
+              if (stay(x, at, j)) add(Keys<T>::of(x), [&] { return amount(x); });
             });
           });
       const float at = uniform(Keys<T>::logit(g.key));
       const uint64_t each = uniform(amount(at)), many = (target - g.before + each - 1) / each;
-      const uint32_t end = at == stay.last ? stay.end : 0xFFFFFFFFu;
+      const uint32_t end = at == stay.last ? stay.end : 0x7FFFFFFFu;
       const Found h = search(
           sh, 0, (uint32_t)V - 1, 32, [&](uint64_t) { return many; },
           [&](auto add) {
-            row.all([&](uint32_t i, float x) {
-              if (x == at && i < end) add(i, one);
+            row.all([&](uint32_t first, int j, float x) {
+              if (x == at && first + j < end) add(first + j, one);
             });
           });
       stay = Stay{at, h.key + 1};
@@ -651,13 +650,13 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
 
     // ---- the choice
     // (a lane's weights add up to 2^53 at most, exactly in double)
-    const auto staying = [&](uint32_t, float x) {
+    const auto staying = [&](float x) {
       const double w = weights.of(x, true);
       return w >= s.floor ? Weights::rounded(w) : 0.0;
     };
     double mine = 0.0;
-    row.all([&](uint32_t i, float x) {
-      if (stay(x, i)) mine += staying(i, x);
+    row.all([&](uint32_t at, int j, float x) {
+      if (stay(x, at, j)) mine += staying(x);
     });
     uint64_t total;
     block_inclusive_sum(sh, 0, (uint64_t)mine, &total);
@@ -677,7 +676,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float x = row.element(c, j);
-        if (stay(x, at + j)) sum += staying(at + j, x);
+        if (stay(x, at, j)) sum += staying(x);
         if (j & 1) __builtin_amdgcn_sched_barrier(0);
       }
       uint64_t all;
@@ -691,7 +690,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
 #pragma unroll 1
         for (int j = 0; j < 8; ++j) {
           const float x = T::up(row.x[at + j < (uint32_t)V ? at + j : (uint32_t)V - 1]);
-          const uint64_t w = at + j < (uint32_t)V && stay(x, at + j) ? (uint64_t)staying(at + j, x) : 0;
+          const uint64_t w = at + j < (uint32_t)V && stay(x, at, j) ? (uint64_t)staying(x) : 0;
           if (rest < w) {
             z[b] = (int32_t)(at + j);
             prob[b] = (float)((double)w / (double)total);
