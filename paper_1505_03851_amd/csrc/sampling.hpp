@@ -18,12 +18,13 @@
 //     it, k and a few, goes to a list, one to a lane, which is sorted by logit, cut, sorted
 //     by number and searched.
 //   * Otherwise a cut is found in two steps: all add their amounts (1 for top_k, their
-//     weight for top_p) to 2,048 bins in LDS, evenly spaced in x over the logits that have a
+//     weight for top_p) to 1,024 bins in LDS, evenly spaced in x over the logits that have a
 //     weight; those of the bin where the running sum reaches its target go to a list, which
-//     is sorted.  Where they are more than 1,024 (equal logits, most often) the bins narrow
-//     down on the logit's bits instead, then on the tokens' numbers.
-//   * z is found by the wavefronts' sums (each holds a stretch of the row), then that stretch's
-//     chunks, one to a wavefront, lanes and elements.
+//     is compared or sorted.  Where they are more than 1,024 (equal logits, most often) bins
+//     narrow down on the logit's bits instead, then on the tokens' numbers.
+//   * Each wavefront holds a stretch of the row and has bins of its own, so the sums of the
+//     stretches' weights that stay are there after the last cut.  z is found by them, then by
+//     the stretch's chunks, one to a wavefront, lanes and elements.
 #pragma once
 
 #include "elements.hpp"
@@ -34,6 +35,8 @@ namespace lda {
 constexpr int kSampleThreads = 1024;
 constexpr int kSampleWaves = kSampleThreads / 64;
 constexpr int kBins = 2 * kSampleThreads;
+constexpr int kSpaced = kSampleThreads;  // bins of a wavefront
+constexpr int kQueue = 1024;             // logits on a wavefront's way to their weights
 constexpr int kListed = kSampleThreads;  // tokens of a list, one to a lane
 constexpr int kCompared = 256;           // of those that are compared with each other
 constexpr int kFewest = 512;             // the largest top_k that is looked for by a bound
@@ -132,8 +135,11 @@ struct SampleShared {
     struct {
       uint64_t place[kListed], weight[kListed];  // place: key << 32 | number
     } list;
+    float queue[kSampleWaves][kQueue];
+    unsigned long long spaced[kSampleWaves][kSpaced];
   };
   uint64_t sums[2][kSampleWaves];
+  unsigned long long kept[kSampleWaves];
   uint32_t tops[kSampleWaves];
   uint64_t pick_before, pick_at;
   uint32_t bin, listed;
@@ -165,13 +171,12 @@ struct Found {
   bool there;       // false: all of them do not reach the target
 };
 
-// The bin where the running sum over the bins, from `before` on, reaches target(sum of
+// Where the running sum over the lanes' two bins, from `before` on, reaches target(sum of
 // all).
 template <typename Target>
-__device__ Found reached(SampleShared &sh, uint64_t before, Target target_of) {
+__device__ Found reached(SampleShared &sh, uint64_t before, uint64_t one, uint64_t two,
+                         Target target_of) {
   const int t = (int)threadIdx.x;
-  __syncthreads();
-  const uint64_t one = sh.bins[2 * t], two = sh.bins[2 * t + 1];
   uint64_t all;
   const uint64_t upto = before + block_inclusive_sum(sh, 0, one + two, &all);
   const uint64_t target = target_of(before + all);
@@ -214,7 +219,8 @@ __device__ Found search(SampleShared &sh, uint32_t lo, uint32_t hi, int levels, 
         if (a) atomicAdd(&sh.bins[(key - lo) >> shift], (unsigned long long)a);
       }
     });
-    const Found f = reached(sh, before, [&](uint64_t all) {
+    __syncthreads();
+    const Found f = reached(sh, before, sh.bins[2 * threadIdx.x], sh.bins[2 * threadIdx.x + 1], [&](uint64_t all) {
       if (first) target = uniform(target_of(all));
       return target;
     });
@@ -308,9 +314,9 @@ struct SampleRow {
       }
     }
   }
-  // f(number of a chunk's first, place in the chunk, logit) of all of this lane's
+  // f(number of its first, chunk) of this lane's chunks
   template <typename F>
-  __device__ __forceinline__ void all(F f) const {
+  __device__ __forceinline__ void chunks(F f) const {
     const int wave = (int)uniform(threadIdx.x >> 6);
 #pragma unroll 1
     for (int i = 0; i < each; ++i) {
@@ -321,13 +327,19 @@ struct SampleRow {
       } else {
         c = read(wave, i);
       }
-      const uint32_t at = first(wave, i);
+      f(first(wave, i), c);
+    }
+  }
+  // f(number of a chunk's first, place in the chunk, logit) of all of this lane's
+  template <typename F>
+  __device__ __forceinline__ void all(F f) const {
+    chunks([&](uint32_t at, const chunk &c) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         f(at, j, element(c, j));
         if (j & 1) __builtin_amdgcn_sched_barrier(0);  // (two weights' registers at a time)
       }
-    }
+    });
   }
 };
 
@@ -362,68 +374,83 @@ struct SampleSettings {
   double floor;  // in steps
 };
 
-// The choice among the n tokens of the list, up to 256, each compared with all others: its
-// rank and the weight of those before it, in their order and then by number.
-template <typename T>
-__device__ void choose_compared(SampleShared &sh, int n, const Weights &weights,
-                                const SampleSettings &s, int32_t *z, float *prob) {
+// Of up to 256 listed tokens: each compared with all others.  The lanes of a list's width
+// (wavefronts of `part` 0) get their token's place, its amount (amount(logit)), its rank and
+// the amounts of those before it; sh.list.weight holds the amounts.
+struct Compared {
+  int i, part, parts;
+  uint64_t place, amount, before;
+  uint32_t rank;
+};
+
+template <typename T, typename Amount>
+__device__ __forceinline__ Compared compared(SampleShared &sh, int n, Amount amount) {
   const int t = (int)threadIdx.x;
   const int width = n <= 64 ? 64 : n <= 128 ? 128 : 256;  // (a wavefront's lanes share a `part`)
-  const int i = t & (width - 1), part = (int)uniform((uint32_t)t / (uint32_t)width);
-  const int parts = kSampleThreads / width;
+  Compared c{t & (width - 1), (int)uniform((uint32_t)t / (uint32_t)width), kSampleThreads / width,
+             0, 0, 0, 0};
   if (t < kCompared) {
     sh.mass[t] = sh.before[t] = 0;
     sh.rank[t] = 0;
   }
   if (t == 0) sh.total = 0;
-  const uint64_t mine = i < n ? sh.list.place[i] : ~0ull;
-  uint64_t weight = 0;
-  double w = 0.0;
-  if (part == 0) {
-    const float x = Keys<T>::logit((uint32_t)(mine >> 32));
-    w = weights.of(x, i < n && x > weights.least);
-    weight = Weights::steps(w);
-    sh.list.weight[i] = weight;
+  c.place = c.i < n ? sh.list.place[c.i] : ~0ull;
+  if (c.part == 0) {
+    c.amount = c.i < n ? amount(Keys<T>::logit((uint32_t)(c.place >> 32))) : 0;
+    sh.list.weight[c.i] = c.amount;
   }
   __syncthreads();
   uint32_t rank = 0;
   uint64_t mass = 0;
-  for (int j = part; j < n; j += parts)
-    if (sh.list.place[j] < mine) {
+  for (int j = c.part; j < n; j += c.parts)
+    if (sh.list.place[j] < c.place) {
       ++rank;
       mass += sh.list.weight[j];
     }
-  if (i < n && rank) {
-    atomicAdd(&sh.rank[i], rank);
-    atomicAdd(&sh.mass[i], (unsigned long long)mass);
+  if (c.i < n && rank) {
+    atomicAdd(&sh.rank[c.i], rank);
+    atomicAdd(&sh.mass[c.i], (unsigned long long)mass);
   }
   __syncthreads();
-  if (part == 0) {
-    weight = s.k == 0 || sh.rank[i] < s.k ? weight : 0;
+  c.rank = sh.rank[c.i];
+  c.before = sh.mass[c.i];
+  return c;
+}
+
+// The choice among the n tokens of the list, up to 256: first by their order, then by number.
+template <typename T>
+__device__ void choose_compared(SampleShared &sh, int n, const Weights &weights,
+                                const SampleSettings &s, int32_t *z, float *prob) {
+  const int t = (int)threadIdx.x;
+  const Compared c = compared<T>(
+      sh, n, [&](float x) { return Weights::steps(weights.of(x, x > weights.least)); });
+  uint64_t weight = c.amount;
+  if (c.part == 0) {
+    weight = s.k == 0 || c.rank < s.k ? weight : 0;
     const uint64_t sum = wave_inclusive_sum(weight);
     if ((t & 63) == 63) atomicAdd(&sh.total, (unsigned long long)sum);
   }
   __syncthreads();
-  if (part == 0) {
-    const bool stays = !(s.p < 1.0f) || sh.mass[i] < share_of(sh.total, s.p);
-    weight = stays && w >= s.floor ? weight : 0;
-    sh.list.weight[i] = weight;
+  if (c.part == 0) {
+    const bool stays = !(s.p < 1.0f) || c.before < share_of(sh.total, s.p);
+    weight = stays && (double)weight >= s.floor ? weight : 0;
+    sh.list.weight[c.i] = weight;
   }
   __syncthreads();
-  const uint32_t number = (uint32_t)mine;
+  const uint32_t number = (uint32_t)c.place;
   uint64_t before = 0, all = 0;
-  for (int j = part; j < n; j += parts) {
+  for (int j = c.part; j < n; j += c.parts) {
     const uint64_t other = sh.list.weight[j];
     all += other;
     before += (uint32_t)sh.list.place[j] < number ? other : 0;
   }
   if (t == 0) sh.total = 0;
-  if (i < n && before) atomicAdd(&sh.before[i], (unsigned long long)before);
+  if (c.i < n && before) atomicAdd(&sh.before[c.i], (unsigned long long)before);
   __syncthreads();
-  if (i == 0) atomicAdd(&sh.total, (unsigned long long)all);
+  if (c.i == 0) atomicAdd(&sh.total, (unsigned long long)all);
   __syncthreads();
-  if (part == 0 && weight) {
-    const uint64_t point = point_of(sh.total, s.u) - sh.before[i];  // (wraps where it lies before)
+  if (c.part == 0 && weight) {
+    const uint64_t point = point_of(sh.total, s.u) - sh.before[c.i];  // (wraps where it lies before)
     if (point < weight) {
       *z = (int32_t)number;
       *prob = (float)((double)weight / (double)sh.total);
@@ -533,9 +560,13 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
     const double per = uniform(1.4426950408889634 / (double)heat);
     // (2^-(F + 2) is nothing; rounded downwards, so that no logit with a weight is left out)
     const double nothing = (double)top - (double)(digits + 2) / per;
-    float least = (float)fmax(nothing, -3.4028234663852886e38);
-    least = (double)least > nothing ? nextafterf(least, -infinity) : least;
-    least = uniform(least < top ? least : nextafterf(top, -infinity));
+    // the largest float that is at most v, and below the top
+    const auto below = [&](double v) {
+      float x = (float)fmax(v, -3.4028234663852886e38);
+      x = (double)x > v ? nextafterf(x, -infinity) : x;
+      return uniform(x < top ? x : nextafterf(top, -infinity));
+    };
+    const float least = below(nothing);
     const Weights weights{uniform((double)top), per, uniform(0x1.8p52 + (double)digits), least};
 
     const auto list = [&](uint32_t number, float x) {
@@ -576,6 +607,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
 
     // ---- many: cuts
     Stay stay{weights.least, 0};
+    bool known = false;  // sh.kept holds the stretches' sums of what stays
     // The bins reach down to the lowest logit that has a weight; at high temperatures, where
     // all may have one, to the row's lowest.
     float lowest = least;
@@ -589,40 +621,65 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       for (int i = 0; i < kSampleWaves; ++i) mine = fminf(mine, Keys<T>::logit(sh.tops[i]));
       lowest = uniform(mine);
     }
-    const float per_bin = uniform((float)(kBins - 1) / (top - lowest));
+    const float per_bin = uniform((float)(kSpaced - 1) / (top - lowest));
     const auto bin_of = [&](float x) {
-      return (uint32_t)fminf((top - x) * per_bin, (float)(kBins - 1));
+      return (uint32_t)fminf((top - x) * per_bin, (float)(kSpaced - 1));
     };
     // Cuts after the token, in their order, up to which the amounts reach target(sum of all).
     const auto cut = [&](auto target_of, auto amount) {
       uint64_t target = 0;
       const auto target_once = [&](uint64_t all) { return target = uniform(target_of(all)); };
-      clear_bins(sh);
-      row.all([&](uint32_t at, int j, float x) {
-        if (stay(x, at, j)) atomicAdd(&sh.bins[bin_of(x)], (unsigned long long)amount(x));
-      });
+      __syncthreads();  // what was there is read
+      for (int i = t; i < kSampleWaves * kSpaced; i += kSampleThreads) (&sh.spaced[0][0])[i] = 0;
       if (t == 0) sh.listed = 0;
-      const Found f = reached(sh, 0, target_once);
+      __syncthreads();
+      row.all([&](uint32_t at, int j, float x) {
+        if (stay(x, at, j)) atomicAdd(&sh.spaced[wave][bin_of(x)], (unsigned long long)amount(x));
+      });
+      __syncthreads();
+      uint64_t mine = 0;  // (`reached` takes two to a lane: bin t is its bin 2 t)
+#pragma unroll
+      for (int i = 0; i < kSampleWaves; ++i) mine += sh.spaced[i][t];
+      const Found f = reached(sh, 0, mine, 0, target_once);
+      known = false;
       if (!f.there) return;
+      // the stretches' sums up to the bin
+      const int bin_at = (int)f.key / 2;
+      uint64_t kept = 0;
+      for (int i = lane; i < bin_at; i += 64) kept += sh.spaced[wave][i];
+      kept = wave_inclusive_sum(kept);
+      if (lane == 63) sh.kept[wave] = kept;
+      __syncthreads();  // bins and list share their memory
       // (the bin's logits, and a hundredth of a bin around them for the roundings)
       const double bin = 1.0 / (double)per_bin;
-      const float high = uniform((float)((double)top - ((double)f.key - 0.01) * bin));
-      const float low_end = f.key == kBins - 1 ? -infinity : (float)((double)top - ((double)f.key + 1.01) * bin);
+      const float high = uniform((float)((double)top - ((double)bin_at - 0.01) * bin));
+      const float low_end = bin_at == kSpaced - 1 ? -infinity : (float)((double)top - ((double)bin_at + 1.01) * bin);
       const float low = uniform(low_end);
       row.all([&](uint32_t at, int j, float x) {
-        if (x <= high && x >= low && stay(x, at, j) && bin_of(x) == f.key) list(at + j, x);
+        if (x <= high && x >= low && stay(x, at, j) && (int)bin_of(x) == bin_at) list(at + j, x);
       });
       __syncthreads();
       const int n = (int)uniform(sh.listed);
       if (n <= kListed) {
-        const uint64_t place = sorted(t < n ? sh.list.place[t] : ~0ull, sort_width(n), sh.list.weight);
-        const uint64_t a = t < n ? amount(Keys<T>::logit((uint32_t)(place >> 32))) : 0;
-        uint64_t all;
-        const uint64_t upto = f.before + block_inclusive_sum(sh, 1, a, &all);
-        if (upto - a < target && target <= upto) sh.pick_at = place;
+        uint64_t place, amount_at = 0, upto;
+        if (n <= kCompared) {
+          const Compared c = compared<T>(sh, n, amount);
+          place = c.place;
+          if (c.part == 0) amount_at = c.amount;
+          upto = f.before + c.before + amount_at;
+        } else {
+          place = sorted(t < n ? sh.list.place[t] : ~0ull, sort_width(n), sh.list.weight);
+          if (t < n) amount_at = amount(Keys<T>::logit((uint32_t)(place >> 32)));
+          uint64_t all;
+          upto = f.before + block_inclusive_sum(sh, 1, amount_at, &all);
+        }
+        if (upto - amount_at < target && target <= upto) sh.pick_at = place;
         __syncthreads();
         const uint64_t last = uniform((uint64_t)sh.pick_at);
+        if (amount_at && place <= last)
+          atomicAdd(&sh.kept[(uint32_t)place / (512u * (uint32_t)row.each)], (unsigned long long)amount_at);
         stay = Stay{uniform(Keys<T>::logit((uint32_t)(last >> 32))), (uint32_t)last + 1};
+        known = true;
         return;
       }
       const Found g = search(
@@ -654,22 +711,57 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       const double w = weights.of(x, true);
       return w >= s.floor ? Weights::rounded(w) : 0.0;
     };
-    double mine = 0.0;
-    row.all([&](uint32_t at, int j, float x) {
-      if (stay(x, at, j)) mine += staying(x);
-    });
-    uint64_t total;
-    block_inclusive_sum(sh, 0, (uint64_t)mine, &total);
+    // min_p: what is far enough below its logit is not asked for its weight
+    if (s.floor > 0.0) {
+      const double at = log2(s.floor) - (double)digits;
+      const float bar = below((double)top + (at - 1e-9) / per);
+      if (bar > stay.last) {
+        stay = Stay{bar, 0};
+        known = false;
+      } else {
+        known = known && (double)weight_of(stay.last) >= s.floor;
+      }
+    }
+    uint64_t total = 0;
+    if (known && s.p < 1.0f) {
+      __syncthreads();
+    } else {
+      // Those that stay are often few: a wavefront puts them in a row and takes the weights
+      // of 64 at a time (256 x 100,000 with min_p: 82 us against 88).
+      __syncthreads();  // `kept`, and what was where the queue is, are read
+      float *queue = sh.queue[wave];
+      uint32_t put = 0, taken = 0;
+      double mine = 0.0;
+      row.chunks([&](uint32_t at, const typename SampleRow<T, CHUNKS>::chunk &c) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float x = row.element(c, j);
+          const bool in = stay(x, at, j);
+          const uint64_t lanes = __builtin_amdgcn_ballot_w64(in);
+          const uint32_t before = __builtin_amdgcn_mbcnt_hi(
+              (uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0));
+          if (in) queue[(put + before) % kQueue] = x;
+          put += (uint32_t)__builtin_popcountll(lanes);
+        }
+        for (; put - taken >= 64; taken += 64) mine += staying(queue[(taken + lane) % kQueue]);
+      });
+      if ((uint32_t)lane < put - taken) mine += staying(queue[(taken + lane) % kQueue]);
+      const uint64_t sum = wave_inclusive_sum((uint64_t)mine);
+      if (lane == 63) sh.kept[wave] = sum;
+      __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < kSampleWaves; ++i) total += uniform((uint64_t)sh.kept[i]);
     uint64_t point = uniform(point_of(total, s.u));
     // the wavefront whose stretch holds it
     int holder = 0;
     for (; holder < kSampleWaves - 1; ++holder) {
-      const uint64_t sum = uniform(sh.sums[0][holder]);
+      const uint64_t sum = uniform((uint64_t)sh.kept[holder]);
       if (point < sum) break;
       point -= sum;
     }
     // its chunks, one to a wavefront at a time, lanes and elements
-    for (int first = 0, turn = 1; first < row.each; first += kSampleWaves, turn ^= 1) {
+    for (int first = 0, turn = 0; first < row.each; first += kSampleWaves, turn ^= 1) {
       const typename SampleRow<T, CHUNKS>::chunk c = row.read(holder, first + wave);
       const uint32_t at = row.first(holder, first + wave);
       double sum = 0.0;
