@@ -36,6 +36,8 @@ constexpr int64_t kLongBlocks = 512;
       F(1, 4);              \
     else if ((D) <= 4096)   \
       F(4, 2);              \
+    else if ((D) <= 6144)   \
+      F(4, 3);              \
     else if ((D) <= 8192)   \
       F(4, 4);              \
     else                    \
@@ -102,11 +104,12 @@ int launch_quantise(const void *x, int64_t ldx, int8_t *q, int64_t ldq, float *s
   return launch_status();
 }
 
-// The workgroups that share the rows of a gradient, each with a strip's sums of D.
+// The workgroups that share the rows of a gradient, each with a strip's sums of D: as
+// many as the GPU holds at 16 wavefronts to a compute unit.
 int32_t strips_of(int64_t N, int32_t D) {
-  const int64_t rows = D <= 2048 ? 4 : 1;  // at a time, in a workgroup
-  const int64_t all = (N + rows - 1) / rows;
-  return (int32_t)(all < kLongBlocks ? all : kLongBlocks);
+  const int64_t rows = D <= 1024 ? 4 : D <= 2048 ? 2 : 1;  // at a time, in a workgroup
+  const int64_t most = D <= 4096 ? 1024 : D <= 8192 ? 512 : 256, all = (N + rows - 1) / rows;
+  return (int32_t)(all < most ? all : most);
 }
 
 template <typename T>
@@ -121,9 +124,19 @@ int launch_norm_grad(const void *grad, int64_t ldg, const void *h, int64_t ldh,
   if (N > 0 && D > kLongest)
     norm_grad_long_kernel<T><<<(unsigned)strips, kLongThreads, 0, s>>>(a);
   else if (N > 0) {
-#define LDA_NORM_GRAD(WAVES, UNITS) \
-  norm_grad_kernel<T, WAVES, UNITS><<<(unsigned)strips, kNormThreads, 0, s>>>(a)
-    LDA_ROW_SHAPE(D, LDA_NORM_GRAD);
+#define LDA_NORM_GRAD(WAVES) \
+  norm_grad_kernel<T, WAVES> \
+      <<<(unsigned)strips, WAVES <= 4 ? kNormThreads : 64 * WAVES, 0, s>>>(a)
+    if (D <= 1024)
+      LDA_NORM_GRAD(1);
+    else if (D <= 2048)
+      LDA_NORM_GRAD(2);
+    else if (D <= 4096)
+      LDA_NORM_GRAD(4);
+    else if (D <= 8192)
+      LDA_NORM_GRAD(8);
+    else
+      LDA_NORM_GRAD(16);
 #undef LDA_NORM_GRAD
   }
   const int64_t tiles = ((int64_t)D + 63) / 64;

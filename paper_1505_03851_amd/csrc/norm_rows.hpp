@@ -303,87 +303,113 @@ struct NormGradArgs {
   bool weight_float;
 };
 
-template <typename T, int WAVES, int UNITS>
-__global__ __launch_bounds__(kNormThreads) void norm_grad_kernel(NormGradArgs<T> a) {
-  static_assert(WAVES == 1 || 64 * WAVES == kNormThreads, "a row to a wavefront or a workgroup");
-  constexpr int kLanes = 64 * WAVES, kRows = kNormThreads / kLanes;
-  constexpr int kColumns = kLanes * UNITS * 8;
+// WAVES wavefronts to a row, two units of 8 columns a lane; the rows of a workgroup go
+// together.  The next row is on its way while this one is worked on.
+template <typename T, int WAVES>
+__global__ __launch_bounds__(WAVES <= 4 ? kNormThreads : 64 * WAVES) void norm_grad_kernel(
+    NormGradArgs<T> a) {
+  using S = typename T::store;
+  constexpr int kUnits = 2, kLanes = 64 * WAVES;
+  constexpr int kThreads = WAVES <= 4 ? kNormThreads : 64 * WAVES, kRows = kThreads / kLanes;
+  constexpr int kColumns = kLanes * kUnits * 8;
   __shared__ float sums[2][2][16];
-  __shared__ float joined[WAVES == 1 ? kColumns : 1];
+  __shared__ float joined[kRows > 1 ? kColumns : 1];
   const int lane = (int)threadIdx.x & (kLanes - 1);
-  const int slot = WAVES == 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0;
-  float dw[UNITS][8];
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), slot = wave / WAVES;
+  int col[kUnits], n[kUnits];
+  float w[kUnits][8], dw[kUnits][8];
 #pragma unroll
-  for (int u = 0; u < UNITS; ++u)
+  for (int u = 0; u < kUnits; ++u) {
+    n[u] = columns_left(a.D, (u * kLanes + lane) * 8);
+    col[u] = n[u] > 0 ? (u * kLanes + lane) * 8 : 0;
+    load_weight<T>(a.weight, a.weight_float, col[u], n[u], w[u]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[u][j] = 0.0f;
-  int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * kRows + slot; row < a.N;
-       row += (int64_t)gridDim.x * kRows) {
-    float d[UNITS][8], h[UNITS][8];
+  }
+  struct Row {
+    Packed<T, 8> d[kUnits], h[kUnits], r[kUnits];
+  };
+  const auto load = [&](int64_t row) {
+    Row v;
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) {
-      const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
-      load_elements<T, 8>(a.grad + row * a.ldg + (n > 0 ? col : 0), n, d[u]);
-      load_elements<T, 8>(a.h + row * a.ldh + (n > 0 ? col : 0), n, h[u]);
+    for (int u = 0; u < kUnits; ++u) {
+      const int m = row < a.N ? n[u] : 0;
+      const int64_t at = row < a.N ? row : 0;
+      v.d[u] = load_packed<T, 8>(a.grad + at * a.ldg + col[u], m);
+      v.h[u] = load_packed<T, 8>(a.h + at * a.ldh + col[u], m);
+      if (a.residual) v.r[u] = load_packed<T, 8>(a.residual + at * a.ldr + col[u], m);
     }
+    return v;
+  };
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  int64_t row = (int64_t)blockIdx.x * kRows + slot;
+  Row next = load(row);
+  int turn = 0;
+  for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.N; base += step, row += step) {
+    const Row now = next;
+    next = load(row + step);
+    float d[kUnits][8], h[kUnits][8];
     float square = 0.0f, along = 0.0f;
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) {
-      const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
-      float w[8];
-      load_weight<T>(a.weight, a.weight_float, col, n, w);
+    for (int u = 0; u < kUnits; ++u)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
+        d[u][j] = T::up(now.d[u].v[j]);
+        h[u][j] = T::up(now.h[u].v[j]);
         square = __builtin_fmaf(h[u][j], h[u][j], square);
-        along = __builtin_fmaf(d[u][j] * w[j], h[u][j], along);
+        along = __builtin_fmaf(d[u][j] * w[u][j], h[u][j], along);
       }
+    square = wave_sum(square);
+    along = wave_sum(along);
+    if (WAVES > 1) {
+      if ((threadIdx.x & 63) == 0) {
+        sums[turn][0][wave] = square;
+        sums[turn][1][wave] = along;
+      }
+      __syncthreads();
+      square = along = 0.0f;
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) {
+        square += sums[turn][0][slot * WAVES + i];
+        along += sums[turn][1][slot * WAVES + i];
+      }
+      turn ^= 1;  // (one barrier a row: the other half is read before this one is written again)
     }
-    square = row_sum<WAVES>(square, sums[0], turn);
-    along = row_sum<WAVES>(along, sums[1], turn);
-    turn ^= 1;
     const float s = 1.0f / sqrtf(square / (float)a.D + a.eps);
     const float pull = along * s / (float)a.D;  // mean(d u)
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) {
-      const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
-      float w[8], r[8];
-      load_weight<T>(a.weight, a.weight_float, col, n, w);
-      if (a.residual)
-        load_elements<T, 8>(a.residual + row * a.ldr + (n > 0 ? col : 0), n, r);
+    for (int u = 0; u < kUnits; ++u) {
       float dx[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float unit = h[u][j] * s;
         dw[u][j] = __builtin_fmaf(d[u][j], unit, dw[u][j]);
-        dx[j] = s * __builtin_fmaf(-unit, pull, d[u][j] * w[j]);
-        if (a.residual) dx[j] += r[j];
+        dx[j] = s * __builtin_fmaf(-unit, pull, d[u][j] * w[u][j]);
+        if (a.residual) dx[j] += T::up(now.r[u].v[j]);
       }
-      if (n > 0) store_elements<T, 8>(a.dx + row * a.ldx + col, n, dx);
+      if (row < a.N && n[u] > 0) store_elements<T, 8>(a.dx + row * a.ldx + col[u], n[u], dx);
     }
   }
-  // the workgroup's strip: its wavefronts one after another
+  // the workgroup's strip: its rows' wavefronts one after another
   float *part = a.part + (int64_t)blockIdx.x * a.D;
-  if (WAVES == 1) {
-    for (int w = 0; w < kRows; ++w) {
-      if (slot == w) {
+  if (kRows > 1) {
+    for (int r = 0; r < kRows; ++r) {
+      if (slot == r) {
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u)
+        for (int u = 0; u < kUnits; ++u)
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             float &to = joined[(u * kLanes + lane) * 8 + j];
-            to = w == 0 ? dw[u][j] : to + dw[u][j];
+            to = r == 0 ? dw[u][j] : to + dw[u][j];
           }
       }
       __syncthreads();
     }
-    for (int c = (int)threadIdx.x; c < a.D; c += kNormThreads) part[c] = joined[c];
+    for (int c = (int)threadIdx.x; c < a.D; c += kThreads) part[c] = joined[c];
   } else {
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) {
-      const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
-      if (n > 0) store_elements<F32, 8>(part + col, n, dw[u]);
-    }
+    for (int u = 0; u < kUnits; ++u)
+      if (n[u] > 0) store_elements<F32, 8>(part + col[u], n[u], dw[u]);
   }
 }
 
