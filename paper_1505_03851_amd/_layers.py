@@ -21,6 +21,8 @@ from ._tokens import (_F32, _I32, _MAX_I32, _U8, _UNSUPPORTED, DTYPES, _cut_off,
 _I8 = torch.int8
 _LDA_I8 = 3
 MAX_PRODUCT_K = 131071  # LDA_PROJECT_MAX_K
+_empty_like = torch.empty_like
+_recording = torch.is_grad_enabled
 
 
 def bind(lib: ctypes.CDLL) -> None:
@@ -57,12 +59,21 @@ def _matrix(t, name: str):
 
 def _like(t, name: str, x, dev: int, dtype, shape, out: bool = False) -> tuple[int, int]:
     """(address, elements from row to row) of a tensor of ``x``'s shape."""
+    if isinstance(t, _Tensor) and t.dim() == 2 and x.dim() == 2:
+        return t.data_ptr(), _rows(t, name, dev, dtype, shape, out)[2]
     if not isinstance(t, _Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.shape != x.shape:
         raise ValueError(f"{name} must have the shape {tuple(x.shape)}, got {tuple(t.shape)}")
     a = t if t.dim() == 2 else _matrix(t, name)
     return a.data_ptr(), _rows(a, name, dev, dtype, shape, out)[2]
+
+
+def _new(x, dtype=None):
+    """A new contiguous tensor of ``x``'s shape."""
+    if x.is_contiguous():
+        return _empty_like(x, dtype=dtype)
+    return x.new_empty(x.shape, dtype=dtype)
 
 
 def _weight(t, dtype, D: int, dev: int) -> tuple[int, int]:
@@ -72,8 +83,8 @@ def _weight(t, dtype, D: int, dev: int) -> tuple[int, int]:
 
 
 def _norm(x, weight, eps, residual, out, sum_out, bits8):
-    if (x.requires_grad or (isinstance(weight, _Tensor) and weight.requires_grad)
-            or (isinstance(residual, _Tensor) and residual.requires_grad)):
+    if _recording() and (x.requires_grad or (isinstance(weight, _Tensor) and weight.requires_grad)
+                         or (isinstance(residual, _Tensor) and residual.requires_grad)):
         _cut_off("x", "weight", "residual")
     dev, dtype = x.get_device(), x.dtype
     a = x if x.dim() == 2 else _matrix(x, "x")
@@ -85,7 +96,7 @@ def _norm(x, weight, eps, residual, out, sum_out, bits8):
     written = []
     if bits8:
         if out is None:
-            q, scale = x.new_empty(x.shape, dtype=_I8), x.new_empty(x.shape[:-1], dtype=_F32)
+            q, scale = _new(x, _I8), x.new_empty(x.shape[:-1], dtype=_F32)
             to, steps = (q.data_ptr(), D), scale.data_ptr()
         else:
             q, scale = out
@@ -98,7 +109,7 @@ def _norm(x, weight, eps, residual, out, sum_out, bits8):
     else:
         steps = None
         if out is None:
-            out = x.new_empty(x.shape)
+            out = _new(x)
             to = out.data_ptr(), D
         else:
             to = _like(out, "out", x, dev, dtype, (N, D), True)
@@ -109,11 +120,11 @@ def _norm(x, weight, eps, residual, out, sum_out, bits8):
         total = _like(sum_out, "sum_out", x, dev, dtype, (N, D), True)
         written.append(sum_out)
     elif residual is not None:
-        sum_out = x.new_empty(x.shape)
+        sum_out = _new(x)
         total = sum_out.data_ptr(), D
     if sum_out is not None:
         result = (*result, sum_out)
-    if any(t.requires_grad for t in written):
+    if written and any(t.requires_grad for t in written):
         _cut_off("out", "sum_out")
     _run("lda_add_norm", dev, a.data_ptr(), ld, *r, w, *to, *total, steps, N, D, DTYPES[dtype],
          weight_type, _LDA_I8 if bits8 else DTYPES[dtype], eps)
@@ -160,9 +171,9 @@ def norm_grad(grad, h, weight, eps: float = 1e-6, residual_grad=None, out=None, 
     to what it holds.  The result does not depend on the order in which the GPU works.
     ``workspace``: a uint8 tensor of at least ``norm_grad_workspace_bytes(N, D)`` bytes,
     or None to allocate one.  ``stream``: where it runs (None: the current stream)."""
-    if (grad.requires_grad or (isinstance(h, _Tensor) and h.requires_grad)
-            or (isinstance(weight, _Tensor) and weight.requires_grad)
-            or (isinstance(residual_grad, _Tensor) and residual_grad.requires_grad)):
+    if _recording() and (grad.requires_grad or (isinstance(h, _Tensor) and h.requires_grad)
+                         or (isinstance(weight, _Tensor) and weight.requires_grad)
+                         or (isinstance(residual_grad, _Tensor) and residual_grad.requires_grad)):
         _cut_off("grad", "h", "weight", "residual_grad")
     dev, dtype = grad.get_device(), grad.dtype
     a = grad if grad.dim() == 2 else _matrix(grad, "grad")
@@ -175,7 +186,7 @@ def norm_grad(grad, h, weight, eps: float = 1e-6, residual_grad=None, out=None, 
          else _like(residual_grad, "residual_grad", grad, dev, dtype, (N, D)))
     written = []
     if out is None:
-        out = grad.new_empty(grad.shape)
+        out = _new(grad)
         to = out.data_ptr(), D
     else:
         to = _like(out, "out", grad, dev, dtype, (N, D), True)
@@ -188,7 +199,7 @@ def norm_grad(grad, h, weight, eps: float = 1e-6, residual_grad=None, out=None, 
     else:
         dw = _vector(weight_out, "weight_out", _F32, D, dev)
         written.append(weight_out)
-    if any(t.requires_grad for t in written):
+    if written and any(t.requires_grad for t in written):
         _cut_off("out", "weight_out")
     need = norm_grad_workspace_bytes(N, D)
     if workspace is not None:
@@ -221,7 +232,7 @@ def quantise_rows(x, out=None) -> tuple[torch.Tensor, torch.Tensor]:
     if D > _MAX_I32:  # the library would take what 32 bits hold of it
         _lib._check(_UNSUPPORTED)
     if out is None:
-        q, scale = x.new_empty(x.shape, dtype=_I8), x.new_empty(x.shape[:-1], dtype=_F32)
+        q, scale = _new(x, _I8), x.new_empty(x.shape[:-1], dtype=_F32)
         to, steps = (q.data_ptr(), D), scale.data_ptr()
     else:
         q, scale = out
@@ -259,8 +270,8 @@ def project_int8(q, scale, weight, weight_scale, bias=None, dtype=None,
     s = _vector(scale if scale.dim() == 1 else scale.reshape(-1), "scale", _F32, M, dev)
     ws = _vector(weight_scale, "weight_scale", _F32, N, dev)
     b = None if bias is None else _vector(bias, "bias", _F32, N, dev)
-    if (scale.requires_grad or weight_scale.requires_grad
-            or (bias is not None and bias.requires_grad)):
+    if _recording() and (scale.requires_grad or weight_scale.requires_grad
+                         or (bias is not None and bias.requires_grad)):
         _cut_off("scale", "weight_scale", "bias")
     given = out is not None
     if not given:

@@ -28,21 +28,34 @@ constexpr int64_t kLongBlocks = 512;
 // is one wavefront's, without a barrier.
 #define LDA_ROW_SHAPE(D, F) \
   do {                      \
-    if ((D) <= 512)         \
+    if ((D) <= 512) {       \
       F(1, 1);              \
-    else if ((D) <= 1024)   \
+    } else if ((D) <= 1024) { \
       F(1, 2);              \
-    else if ((D) <= 2048)   \
+    } else if ((D) <= 2048) { \
       F(1, 4);              \
-    else if ((D) <= 4096)   \
+    } else if ((D) <= 4096) { \
       F(4, 2);              \
-    else if ((D) <= 6144)   \
+    } else if ((D) <= 6144) { \
       F(4, 3);              \
-    else if ((D) <= 8192)   \
+    } else if ((D) <= 8192) { \
       F(4, 4);              \
-    else                    \
+    } else {                \
       F(4, 8);              \
+    }                       \
   } while (0)
+
+// Rows of 16 bits pass the caches by where a call reads and writes more than they hold:
+// 16,384 x 4,096 bfloat16 with a residual (537 MB) 88 us against 94, its gradient 111 against
+// 119, 32,768 x 2,048 without one (403 MB) 86 against 96; below, what the launch before wrote
+// may still be there: 16,384 x 4,096 without a residual (268 MB) 44 against 39, 8,192 x 4,096
+// with one (268 MB) 45 against 39.  A lane's 32 bytes of floats are two accesses to one line:
+// 204 against 192.
+template <typename T>
+bool past_caches(int64_t rows, int64_t columns, int arrays) {
+  const int64_t size = (int64_t)sizeof(typename T::store);
+  return size == 2 && rows * columns * arrays * size > (int64_t)320 << 20;
+}
 
 unsigned long_grid(int64_t N) { return (unsigned)(N < kLongBlocks ? N : kLongBlocks); }
 
@@ -52,15 +65,23 @@ int launch_norm(NormArgs<T> a, hipStream_t s) {
     norm_long_kernel<T, BITS8><<<long_grid(a.N), kLongThreads, 0, s>>>(a);
     return launch_status();
   }
+  constexpr bool kMayStream = sizeof(typename T::store) == 2;
   const int64_t N = a.N;
+  const bool stream = past_caches<T>(N, a.D, 2 + (a.residual != nullptr) + (a.sum != nullptr));
   for (int64_t at = 0; at < N; at += kSlice) {
     a.N = N - at < kSlice ? N - at : kSlice;
-#define LDA_NORM(WAVES, UNITS)                                                        \
-  norm_kernel<T, WAVES, UNITS, BITS8>                                                 \
+#define LDA_NORM_BY(WAVES, UNITS, STREAM)                                             \
+  norm_kernel<T, WAVES, UNITS, BITS8, STREAM>                                         \
       <<<(unsigned)(WAVES == 1 ? (a.N + 3) / 4 : a.N), WAVES == 1 ? 256 : 64 * WAVES, \
          0, s>>>(a)
+#define LDA_NORM(WAVES, UNITS)               \
+  if (stream)                                \
+    LDA_NORM_BY(WAVES, UNITS, kMayStream);   \
+  else                                       \
+    LDA_NORM_BY(WAVES, UNITS, false)
     LDA_ROW_SHAPE(a.D, LDA_NORM);
 #undef LDA_NORM
+#undef LDA_NORM_BY
     a.x += a.N * a.ldx;
     if (a.residual) a.residual += a.N * a.ldr;
     if (a.sum) a.sum += a.N * a.lds;
@@ -124,20 +145,33 @@ int launch_norm_grad(const void *grad, int64_t ldg, const void *h, int64_t ldh,
   if (N > 0 && D > kLongest)
     norm_grad_long_kernel<T><<<(unsigned)strips, kLongThreads, 0, s>>>(a);
   else if (N > 0) {
-#define LDA_NORM_GRAD(WAVES) \
-  norm_grad_kernel<T, WAVES> \
+    constexpr bool kMayStream = sizeof(S) == 2;
+    const bool stream = past_caches<T>(N, D, 3 + (residual != nullptr));
+#define LDA_NORM_GRAD_BY(WAVES, STREAM) \
+  norm_grad_kernel<T, WAVES, STREAM>    \
       <<<(unsigned)strips, WAVES <= 4 ? kNormThreads : 64 * WAVES, 0, s>>>(a)
-    if (D <= 1024)
+#define LDA_NORM_GRAD(WAVES)             \
+  if (stream)                            \
+    LDA_NORM_GRAD_BY(WAVES, kMayStream); \
+  else                                   \
+    LDA_NORM_GRAD_BY(WAVES, false)
+    if (D <= 1024) {
       LDA_NORM_GRAD(1);
-    else if (D <= 2048)
+    } else if (D <= 2048) {
       LDA_NORM_GRAD(2);
-    else if (D <= 4096)
+    } else if (D <= 4096) {
       LDA_NORM_GRAD(4);
-    else if (D <= 8192)
+    } else if (D <= 6144) {
+      LDA_NORM_GRAD(6);
+    } else if (D <= 8192) {
       LDA_NORM_GRAD(8);
-    else
+    } else if (D <= 12288) {
+      LDA_NORM_GRAD(12);
+    } else {
       LDA_NORM_GRAD(16);
+    }
 #undef LDA_NORM_GRAD
+#undef LDA_NORM_GRAD_BY
   }
   const int64_t tiles = ((int64_t)D + 63) / 64;
   join_strips_kernel<<<(unsigned)(tiles < (1 << 16) ? tiles : 1 << 16), 1024, 0, s>>>(

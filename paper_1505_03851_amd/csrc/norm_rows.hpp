@@ -149,8 +149,8 @@ struct NormArgs {
   bool weight_float;
 };
 
-// BITS8: out is int8, with a scale for each row.
-template <typename T, int WAVES, int UNITS, bool BITS8>
+// BITS8: out is int8, with a scale for each row.  STREAM: rows pass the caches by.
+template <typename T, int WAVES, int UNITS, bool BITS8, bool STREAM>
 __global__ __launch_bounds__(WAVES == 1 ? kNormThreads : 64 * WAVES) void norm_kernel(
     NormArgs<T> a) {
   using S = typename T::store;
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kNormThreads : 64 * WAVES) void norm_k
 #pragma unroll
   for (int u = 0; u < UNITS; ++u) {
     const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
-    load_elements<T, 8>(x + (n > 0 ? col : 0), n, h[u]);
+    load_elements<T, 8, STREAM>(x + (n > 0 ? col : 0), n, h[u]);
   }
   if (a.residual) {
     const S *r = a.residual + row * a.ldr;
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kNormThreads : 64 * WAVES) void norm_k
     for (int u = 0; u < UNITS; ++u) {
       const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
       float v[8];
-      load_elements<T, 8>(r + (n > 0 ? col : 0), n, v);
+      load_elements<T, 8, STREAM>(r + (n > 0 ? col : 0), n, v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) h[u][j] += v[j];
     }
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kNormThreads : 64 * WAVES) void norm_k
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
       const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
-      if (n > 0) store_elements<T, 8>(to + col, n, h[u]);
+      if (n > 0) store_elements<T, 8, STREAM>(to + col, n, h[u]);
     }
   }
   uint32_t top = 0;
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kNormThreads : 64 * WAVES) void norm_k
       h[u][j] = h[u][j] * s * w[j];
       if (BITS8 && j < n) top = magnitude(h[u][j]) > top ? magnitude(h[u][j]) : top;
     }
-    if (!BITS8 && n > 0) store_elements<T, 8>((S *)a.out + row * a.ldo + col, n, h[u]);
+    if (!BITS8 && n > 0) store_elements<T, 8, STREAM>((S *)a.out + row * a.ldo + col, n, h[u]);
   }
   if (BITS8) {
     const Steps steps = steps_of(row_largest<WAVES>(top, tops));
@@ -305,17 +305,16 @@ struct NormGradArgs {
 
 // WAVES wavefronts to a row, two units of 8 columns a lane; the rows of a workgroup go
 // together.  The next row is on its way while this one is worked on.
-template <typename T, int WAVES>
+template <typename T, int WAVES, bool STREAM>
 __global__ __launch_bounds__(WAVES <= 4 ? kNormThreads : 64 * WAVES) void norm_grad_kernel(
     NormGradArgs<T> a) {
-  using S = typename T::store;
   constexpr int kUnits = 2, kLanes = 64 * WAVES;
   constexpr int kThreads = WAVES <= 4 ? kNormThreads : 64 * WAVES, kRows = kThreads / kLanes;
   constexpr int kColumns = kLanes * kUnits * 8;
   __shared__ float sums[2][2][16];
   __shared__ float joined[kRows > 1 ? kColumns : 1];
-  const int lane = (int)threadIdx.x & (kLanes - 1);
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), slot = wave / WAVES;
+  const int lane = kRows > 1 ? (int)threadIdx.x & (kLanes - 1) : (int)threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), slot = kRows > 1 ? wave / WAVES : 0;
   int col[kUnits], n[kUnits];
   float w[kUnits][8], dw[kUnits][8];
 #pragma unroll
@@ -335,9 +334,9 @@ __global__ __launch_bounds__(WAVES <= 4 ? kNormThreads : 64 * WAVES) void norm_g
     for (int u = 0; u < kUnits; ++u) {
       const int m = row < a.N ? n[u] : 0;
       const int64_t at = row < a.N ? row : 0;
-      v.d[u] = load_packed<T, 8>(a.grad + at * a.ldg + col[u], m);
-      v.h[u] = load_packed<T, 8>(a.h + at * a.ldh + col[u], m);
-      if (a.residual) v.r[u] = load_packed<T, 8>(a.residual + at * a.ldr + col[u], m);
+      v.d[u] = load_packed<T, 8, STREAM>(a.grad + at * a.ldg + col[u], m);
+      v.h[u] = load_packed<T, 8, STREAM>(a.h + at * a.ldh + col[u], m);
+      if (a.residual) v.r[u] = load_packed<T, 8, STREAM>(a.residual + at * a.ldr + col[u], m);
     }
     return v;
   };
@@ -387,7 +386,7 @@ __global__ __launch_bounds__(WAVES <= 4 ? kNormThreads : 64 * WAVES) void norm_g
         dx[j] = s * __builtin_fmaf(-unit, pull, d[u][j] * w[u][j]);
         if (a.residual) dx[j] += T::up(now.r[u].v[j]);
       }
-      if (row < a.N && n[u] > 0) store_elements<T, 8>(a.dx + row * a.ldx + col[u], n[u], dx);
+      if (row < a.N && n[u] > 0) store_elements<T, 8, STREAM>(a.dx + row * a.ldx + col[u], n[u], dx);
     }
   }
   // the workgroup's strip: its rows' wavefronts one after another
