@@ -21,7 +21,9 @@ namespace {
 
 // Rows of a launch: fewer than 2^32 work-items.
 constexpr int64_t kSlice = 1 << 22;
-constexpr int32_t kLongest = 16384;  // columns that stay in registers
+// Rows that stay in registers, a lane's 8 columns loaded together; others go to the
+// kernels that take rows of any length.
+bool in_registers(int32_t D) { return D >= 8 && D <= 16384; }
 constexpr int64_t kLongBlocks = 512;
 
 // f(WAVES, UNITS) of the shape that holds rows of D columns.  Up to 2,048 columns a row
@@ -61,7 +63,7 @@ unsigned long_grid(int64_t N) { return (unsigned)(N < kLongBlocks ? N : kLongBlo
 
 template <typename T, bool BITS8>
 int launch_norm(NormArgs<T> a, hipStream_t s) {
-  if (a.D > kLongest) {
+  if (!in_registers(a.D)) {
     norm_long_kernel<T, BITS8><<<long_grid(a.N), kLongThreads, 0, s>>>(a);
     return launch_status();
   }
@@ -106,7 +108,7 @@ template <typename T>
 int launch_quantise(const void *x, int64_t ldx, int8_t *q, int64_t ldq, float *scale, int64_t N,
                     int32_t D, hipStream_t s) {
   QuantArgs<T> a{(const typename T::store *)x, q, scale, ldx, ldq, N, D};
-  if (D > kLongest) {
+  if (!in_registers(D)) {
     quantise_long_kernel<T><<<long_grid(N), kLongThreads, 0, s>>>(a);
     return launch_status();
   }
@@ -128,7 +130,7 @@ int launch_quantise(const void *x, int64_t ldx, int8_t *q, int64_t ldq, float *s
 // The workgroups that share the rows of a gradient, each with a strip's sums of D: as
 // many as the GPU holds at 16 wavefronts to a compute unit.
 int32_t strips_of(int64_t N, int32_t D) {
-  const int64_t rows = D <= 1024 ? 4 : D <= 2048 ? 2 : 1;  // at a time, in a workgroup
+  const int64_t rows = !in_registers(D) ? 1 : D <= 1024 ? 4 : D <= 2048 ? 2 : 1;  // at a time
   const int64_t most = D <= 4096 ? 1024 : D <= 8192 ? 512 : 256, all = (N + rows - 1) / rows;
   return (int32_t)(all < most ? all : most);
 }
@@ -142,7 +144,7 @@ int launch_norm_grad(const void *grad, int64_t ldg, const void *h, int64_t ldh,
   const int32_t strips = strips_of(N, D);
   const NormGradArgs<T> a{(const S *)grad, (const S *)h, (const S *)residual, weight, (S *)dx, part,
                           ldg, ldh, ldr, ldx, N, D, (float)eps, weight_float};
-  if (N > 0 && D > kLongest)
+  if (N > 0 && !in_registers(D))
     norm_grad_long_kernel<T><<<(unsigned)strips, kLongThreads, 0, s>>>(a);
   else if (N > 0) {
     constexpr bool kMayStream = sizeof(S) == 2;
@@ -161,12 +163,8 @@ int launch_norm_grad(const void *grad, int64_t ldg, const void *h, int64_t ldh,
       LDA_NORM_GRAD(2);
     } else if (D <= 4096) {
       LDA_NORM_GRAD(4);
-    } else if (D <= 6144) {
-      LDA_NORM_GRAD(6);
     } else if (D <= 8192) {
       LDA_NORM_GRAD(8);
-    } else if (D <= 12288) {
-      LDA_NORM_GRAD(12);
     } else {
       LDA_NORM_GRAD(16);
     }

@@ -135,6 +135,60 @@ __device__ __forceinline__ void load_weight(const void *w, bool w_float, int64_t
     load_elements<T, 8>((const typename T::store *)w + (n > 0 ? col : 0), n, v);
 }
 
+// The 8 columns of a lane's unit in a row of D >= 8: those from `at` on, of which the first
+// `skip` are not its own.  The last unit of a row whose length is no multiple of 8 starts
+// where its 8 columns end with the row's, and a unit past the end has none of its own: so
+// every lane loads 16 bytes at once, without a branch that loads would have to wait in.
+struct Columns {
+  int at, skip;
+  __device__ __forceinline__ Columns() {}
+  __device__ __forceinline__ Columns(int D, int unit)
+      : at(unit * 8 <= D - 8 ? unit * 8 : D - 8),
+        skip(unit * 8 <= D - 8 ? 0 : unit * 8 < D ? 8 - (D - unit * 8) : 8) {}
+};
+
+// Zero in the columns that are not the unit's own.
+__device__ __forceinline__ void own_columns(const Columns &c, float (&x)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = j >= c.skip ? x[j] : 0.0f;
+}
+
+template <typename T, bool STREAM = false>
+__device__ __forceinline__ void load_columns(const typename T::store *row, const Columns &c,
+                                             float (&x)[8]) {
+  load_elements<T, 8, STREAM>(row + c.at, 8, x);
+  own_columns(c, x);
+}
+
+template <typename T>
+__device__ __forceinline__ void load_weight_columns(const void *w, bool w_float, const Columns &c,
+                                                    float (&v)[8]) {
+  load_weight<T>(w, w_float, c.at, 8, v);
+  own_columns(c, v);
+}
+
+template <typename T, bool STREAM = false>
+__device__ __forceinline__ void store_columns(typename T::store *row, const Columns &c,
+                                              const float (&x)[8]) {
+  if (c.skip == 0) {
+    store_elements<T, 8, STREAM>(row + c.at, 8, x);
+  } else {
+#pragma unroll
+    for (int j = 1; j < 8; ++j)
+      if (j >= c.skip) row[c.at + j] = T::down(x[j]);
+  }
+}
+
+__device__ __forceinline__ void store_step_columns(int8_t *row, const Columns &c, const int (&q)[8]) {
+  if (c.skip == 0) {
+    store_steps(row + c.at, 8, q);
+  } else {
+#pragma unroll
+    for (int j = 1; j < 8; ++j)
+      if (j >= c.skip) row[c.at + j] = (int8_t)q[j];
+  }
+}
+
 // What a launch of the norm works on.  `residual` and `sum` (where h goes) may be NULL.
 template <typename T>
 struct NormArgs {
@@ -165,18 +219,18 @@ __global__ __launch_bounds__(WAVES == 1 ? kNormThreads : 64 * WAVES) void norm_k
   if (row >= a.N) return;  // (a whole wavefront; workgroups of one row are never here)
   const S *x = a.x + row * a.ldx;
   float h[UNITS][8];
+  Columns c[UNITS];
 #pragma unroll
   for (int u = 0; u < UNITS; ++u) {
-    const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
-    load_elements<T, 8, STREAM>(x + (n > 0 ? col : 0), n, h[u]);
+    c[u] = Columns(a.D, u * kLanes + lane);
+    load_columns<T, STREAM>(x, c[u], h[u]);
   }
   if (a.residual) {
     const S *r = a.residual + row * a.ldr;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-      const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
       float v[8];
-      load_elements<T, 8, STREAM>(r + (n > 0 ? col : 0), n, v);
+      load_columns<T, STREAM>(r, c[u], v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) h[u][j] += v[j];
     }
@@ -188,36 +242,30 @@ __global__ __launch_bounds__(WAVES == 1 ? kNormThreads : 64 * WAVES) void norm_k
     for (int j = 0; j < 8; ++j) square = __builtin_fmaf(h[u][j], h[u][j], square);
   const float s = 1.0f / sqrtf(row_sum<WAVES>(square, sums, 0) / (float)a.D + a.eps);
   if (a.sum) {
-    S *to = a.sum + row * a.lds;
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) {
-      const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
-      if (n > 0) store_elements<T, 8, STREAM>(to + col, n, h[u]);
-    }
+    for (int u = 0; u < UNITS; ++u) store_columns<T, STREAM>(a.sum + row * a.lds, c[u], h[u]);
   }
   uint32_t top = 0;
 #pragma unroll
   for (int u = 0; u < UNITS; ++u) {
-    const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
     float w[8];
-    load_weight<T>(a.weight, a.weight_float, col, n, w);
+    load_weight_columns<T>(a.weight, a.weight_float, c[u], w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       h[u][j] = h[u][j] * s * w[j];
-      if (BITS8 && j < n) top = magnitude(h[u][j]) > top ? magnitude(h[u][j]) : top;
+      if (BITS8 && j >= c[u].skip) top = magnitude(h[u][j]) > top ? magnitude(h[u][j]) : top;
     }
-    if (!BITS8 && n > 0) store_elements<T, 8, STREAM>((S *)a.out + row * a.ldo + col, n, h[u]);
+    if (!BITS8) store_columns<T, STREAM>((S *)a.out + row * a.ldo, c[u], h[u]);
   }
   if (BITS8) {
     const Steps steps = steps_of(row_largest<WAVES>(top, tops));
     if (lane == 0) a.scale[row] = steps.scale;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-      const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
       int q[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) q[j] = steps.inverse > 0.0f ? step_of(h[u][j], steps) : 0;
-      if (n > 0) store_steps((int8_t *)a.out + row * a.ldo + col, n, q);
+      store_step_columns((int8_t *)a.out + row * a.ldo, c[u], q);
     }
   }
 }
@@ -315,13 +363,12 @@ __global__ __launch_bounds__(WAVES <= 4 ? kNormThreads : 64 * WAVES) void norm_g
   __shared__ float joined[kRows > 1 ? kColumns : 1];
   const int lane = kRows > 1 ? (int)threadIdx.x & (kLanes - 1) : (int)threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), slot = kRows > 1 ? wave / WAVES : 0;
-  int col[kUnits], n[kUnits];
+  Columns c[kUnits];
   float w[kUnits][8], dw[kUnits][8];
 #pragma unroll
   for (int u = 0; u < kUnits; ++u) {
-    n[u] = columns_left(a.D, (u * kLanes + lane) * 8);
-    col[u] = n[u] > 0 ? (u * kLanes + lane) * 8 : 0;
-    load_weight<T>(a.weight, a.weight_float, col[u], n[u], w[u]);
+    c[u] = Columns(a.D, u * kLanes + lane);
+    load_weight_columns<T>(a.weight, a.weight_float, c[u], w[u]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[u][j] = 0.0f;
   }
@@ -329,14 +376,13 @@ __global__ __launch_bounds__(WAVES <= 4 ? kNormThreads : 64 * WAVES) void norm_g
     Packed<T, 8> d[kUnits], h[kUnits], r[kUnits];
   };
   const auto load = [&](int64_t row) {
+    const int64_t at = row < a.N ? row : a.N - 1;  // (the last one again: its results are not used)
     Row v;
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-      const int m = row < a.N ? n[u] : 0;
-      const int64_t at = row < a.N ? row : 0;
-      v.d[u] = load_packed<T, 8, STREAM>(a.grad + at * a.ldg + col[u], m);
-      v.h[u] = load_packed<T, 8, STREAM>(a.h + at * a.ldh + col[u], m);
-      if (a.residual) v.r[u] = load_packed<T, 8, STREAM>(a.residual + at * a.ldr + col[u], m);
+      v.d[u] = load_packed<T, 8, STREAM>(a.grad + at * a.ldg + c[u].at, 8);
+      v.h[u] = load_packed<T, 8, STREAM>(a.h + at * a.ldh + c[u].at, 8);
+      if (a.residual) v.r[u] = load_packed<T, 8, STREAM>(a.residual + at * a.ldr + c[u].at, 8);
     }
     return v;
   };
@@ -349,12 +395,13 @@ __global__ __launch_bounds__(WAVES <= 4 ? kNormThreads : 64 * WAVES) void norm_g
     next = load(row + step);
     float d[kUnits][8], h[kUnits][8];
     float square = 0.0f, along = 0.0f;
+    const bool there = row < a.N;
 #pragma unroll
     for (int u = 0; u < kUnits; ++u)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        d[u][j] = T::up(now.d[u].v[j]);
-        h[u][j] = T::up(now.h[u].v[j]);
+        d[u][j] = there && j >= c[u].skip ? T::up(now.d[u].v[j]) : 0.0f;
+        h[u][j] = j >= c[u].skip ? T::up(now.h[u].v[j]) : 0.0f;
         square = __builtin_fmaf(h[u][j], h[u][j], square);
         along = __builtin_fmaf(d[u][j] * w[u][j], h[u][j], along);
       }
@@ -386,7 +433,7 @@ __global__ __launch_bounds__(WAVES <= 4 ? kNormThreads : 64 * WAVES) void norm_g
         dx[j] = s * __builtin_fmaf(-unit, pull, d[u][j] * w[u][j]);
         if (a.residual) dx[j] += T::up(now.r[u].v[j]);
       }
-      if (row < a.N && n[u] > 0) store_elements<T, 8, STREAM>(a.dx + row * a.ldx + col[u], n[u], dx);
+      if (there) store_columns<T, STREAM>(a.dx + row * a.ldx, c[u], dx);
     }
   }
   // the workgroup's strip: its rows' wavefronts one after another
@@ -398,7 +445,8 @@ __global__ __launch_bounds__(WAVES <= 4 ? kNormThreads : 64 * WAVES) void norm_g
         for (int u = 0; u < kUnits; ++u)
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            float &to = joined[(u * kLanes + lane) * 8 + j];
+            if (j < c[u].skip) continue;
+            float &to = joined[c[u].at + j];
             to = r == 0 ? dw[u][j] : to + dw[u][j];
           }
       }
@@ -407,8 +455,7 @@ __global__ __launch_bounds__(WAVES <= 4 ? kNormThreads : 64 * WAVES) void norm_g
     for (int c = (int)threadIdx.x; c < a.D; c += kThreads) part[c] = joined[c];
   } else {
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u)
-      if (n[u] > 0) store_elements<F32, 8>(part + col[u], n[u], dw[u]);
+    for (int u = 0; u < kUnits; ++u) store_columns<F32>(part, c[u], dw[u]);
   }
 }
 
@@ -509,11 +556,12 @@ __global__ __launch_bounds__(WAVES == 1 ? kNormThreads : 64 * WAVES) void quanti
                  : (int64_t)blockIdx.x;
   if (row >= a.N) return;  // (a whole wavefront; workgroups of one row are never here)
   float x[UNITS][8];
+  Columns c[UNITS];
   uint32_t top = 0;
 #pragma unroll
   for (int u = 0; u < UNITS; ++u) {
-    const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
-    load_elements<T, 8>(a.x + row * a.ldx + (n > 0 ? col : 0), n, x[u]);
+    c[u] = Columns(a.D, u * kLanes + lane);
+    load_columns<T>(a.x + row * a.ldx, c[u], x[u]);
   }
 #pragma unroll
   for (int u = 0; u < UNITS; ++u)
@@ -523,11 +571,10 @@ __global__ __launch_bounds__(WAVES == 1 ? kNormThreads : 64 * WAVES) void quanti
   if (lane == 0) a.scale[row] = steps.scale;
 #pragma unroll
   for (int u = 0; u < UNITS; ++u) {
-    const int col = (u * kLanes + lane) * 8, n = columns_left(a.D, col);
     int q[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) q[j] = steps.inverse > 0.0f ? exact_step_of<T>(x[u][j], steps) : 0;
-    if (n > 0) store_steps(a.q + row * a.ldq + col, n, q);
+    store_step_columns(a.q + row * a.ldq, c[u], q);
   }
 }
 
