@@ -232,6 +232,23 @@ __device__ Found search(SampleShared &sh, uint32_t lo, uint32_t hi, int levels, 
   }
 }
 
+// The value of lane `lane ^ apart`, apart < 64: within 16 lanes by data-parallel moves.
+template <int CONTROL>
+__device__ __forceinline__ uint64_t moved_pair(uint64_t v) {
+  return (uint64_t)moved<CONTROL, 0xF>(0, (uint32_t)(v >> 32)) << 32 | moved<CONTROL, 0xF>(0, (uint32_t)v);
+}
+__device__ __forceinline__ uint64_t across(uint64_t v, int apart) {
+  switch (apart) {
+    case 1: return moved_pair<0xB1>(v);                     // of four lanes 1 0 3 2
+    case 2: return moved_pair<0x4E>(v);                     // 2 3 0 1
+    case 4: return moved_pair<0x1B>(moved_pair<0x141>(v));  // of eight 7 .. 0, of four 3 .. 0
+    case 8: return moved_pair<0x128>(v);                    // of sixteen turned by eight
+    default:
+      return (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), apart) << 32 |
+             (uint32_t)__shfl_xor((int)(uint32_t)v, apart);
+  }
+}
+
 // Sorts the lanes' values, of which those of lanes from `width` (a power of two from 64 on)
 // are not looked at: lane t then holds the t-th.  A bitonic network: exchanges within
 // wavefronts by lane, others through `room`.
@@ -249,8 +266,7 @@ __device__ __forceinline__ uint64_t sorted(uint64_t v, int width, uint64_t *room
       } else if (idle) {
         continue;
       } else {
-        other = (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), apart) << 32 |
-                (uint32_t)__shfl_xor((int)(uint32_t)v, apart);
+        other = across(v, apart);
       }
       const bool smaller = ((t & apart) == 0) == ((t & size) == 0 || size == width);
       v = smaller == (other < v) ? other : v;
@@ -458,29 +474,47 @@ __device__ void choose_compared(SampleShared &sh, int n, const Weights &weights,
   }
 }
 
-// The choice among the n tokens of the list, sorted.
+// The choice among the n tokens of the list, sorted.  `whole`: the list is the row, so that
+// its tokens' numbers are places too.
 template <typename T>
-__device__ void choose_sorted(SampleShared &sh, int n, const Weights &weights,
+__device__ void choose_sorted(SampleShared &sh, int n, bool whole, const Weights &weights,
                               const SampleSettings &s, int32_t *z, float *prob) {
   const int t = (int)threadIdx.x, width = sort_width(n);
-  const uint64_t place = sorted(t < n ? sh.list.place[t] : ~0ull, width, sh.list.weight);
+  const bool cuts = s.k || s.p < 1.0f;
+  uint64_t place = t < n ? sh.list.place[t] : ~0ull;
+  if (cuts || !whole) place = sorted(place, width, sh.list.weight);
+  const bool there = place != ~0ull;
   const float x = Keys<T>::logit((uint32_t)(place >> 32));
-  const double w = weights.of(x, t < n && x > weights.least);
-  uint64_t weight = s.k == 0 || (uint64_t)t < s.k ? Weights::steps(w) : 0;
-  uint64_t all;
-  const uint64_t upto = block_inclusive_sum(sh, 0, weight, &all);
-  const bool stays = !(s.p < 1.0f) || upto - weight < share_of(all, s.p);
-  weight = stays && w >= s.floor ? weight : 0;
-  sh.list.place[t] = weight;  // (read before the sums' barrier)
-  // by number; what does not stay has no part in it
-  const uint64_t number = sorted((uint64_t)(weight ? (uint32_t)place : 0xFFFFFFFFu) << 32 | (uint32_t)t,
-                                 width, sh.list.weight);
-  __syncthreads();
-  weight = t < width ? sh.list.place[(uint32_t)number] : 0;
+  const double w = weights.of(x, there && x > weights.least);
+  uint64_t weight = s.k == 0 || (uint64_t)t < s.k ? Weights::steps(w) : 0, all = 0;
+  if (cuts) {
+    const uint64_t upto = block_inclusive_sum(sh, 0, weight, &all);
+    weight = !(s.p < 1.0f) || upto - weight < share_of(all, s.p) ? weight : 0;
+  }
+  weight = w >= s.floor ? weight : 0;
+  // by number
+  uint32_t number = (uint32_t)place;
+  __syncthreads();  // what was there is read
+  if (whole && cuts) {
+    sh.list.weight[t] = 0;
+    __syncthreads();
+    if (there) sh.list.weight[number] = weight;
+    __syncthreads();
+    weight = sh.list.weight[t];
+    number = (uint32_t)t;
+  } else if (!whole) {
+    // what does not stay has no part in it
+    sh.list.place[t] = weight;
+    const uint64_t by = sorted((uint64_t)(weight ? number : 0xFFFFFFFFu) << 32 | (uint32_t)t, width,
+                               sh.list.weight);
+    __syncthreads();
+    weight = t < width ? sh.list.place[(uint32_t)by] : 0;
+    number = (uint32_t)(by >> 32);
+  }
   const uint64_t sum = block_inclusive_sum(sh, 1, weight, &all);
   const uint64_t point = point_of(all, s.u);
   if (sum - weight <= point && point < sum) {
-    *z = (int32_t)(number >> 32);
+    *z = (int32_t)number;
     *prob = (float)((double)weight / (double)all);
   }
 }
@@ -590,16 +624,21 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
         if (f.there) bound = uniform(Keys<T>::logit(f.key));
       }
       __syncthreads();  // bins and list share their memory
-      row.all([&](uint32_t at, int j, float x) {
-        if (x >= bound) list(at + j, x);
-      });
+      if (all_listed) {
+        const float x = t < V ? T::up(row.x[t]) : -infinity;
+        sh.list.place[t] = x > -infinity ? (uint64_t)Keys<T>::of(x) << 32 | (uint32_t)t : ~0ull;
+      } else {
+        row.all([&](uint32_t at, int j, float x) {
+          if (x >= bound) list(at + j, x);
+        });
+      }
       __syncthreads();
-      const int n = (int)uniform(sh.listed);
+      const int n = all_listed ? V : (int)uniform(sh.listed);
       if (n <= kListed) {
         if (n <= kCompared)
           choose_compared<T>(sh, n, weights, s, z + b, prob + b);
         else
-          choose_sorted<T>(sh, n, weights, s, z + b, prob + b);
+          choose_sorted<T>(sh, n, all_listed, weights, s, z + b, prob + b);
         __syncthreads();
         continue;
       }
