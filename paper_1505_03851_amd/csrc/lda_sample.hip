@@ -12,7 +12,7 @@
 namespace lda {
 namespace {
 
-constexpr int64_t kMaxRows = 1 << 20;  // of a launch; workgroups stride over the rest
+constexpr int64_t kSlice = 1 << 20;  // rows of a launch: fewer than 2^32 work-items
 
 // The digits of a weight: V of them, each at most 2^digits, add up in 64 bits.
 int weight_digits(int32_t V) {
@@ -28,17 +28,21 @@ int launch_sample(const void *logits, int64_t ld, int64_t B, int32_t V, const fl
   // chunks of a lane that stay in registers: 4 or as many as fit in 64
   constexpr int kMost = 64 / (2 * (int)sizeof(typename T::store));
   const int64_t chunks = ((int64_t)V + 8 * kSampleThreads - 1) / (8 * kSampleThreads);
+  for (int64_t at = 0; at < B; at += kSlice) {
+    const auto from = [&](const auto *p) { return p ? p + at : p; };
 #define LDA_SAMPLE(CHUNKS)                                                                      \
-  sample_kernel<T, CHUNKS><<<(unsigned)(B < kMaxRows ? B : kMaxRows), kSampleThreads, 0, s>>>( \
-      (const typename T::store *)logits, ld, B, V, weight_digits(V), u, temperature, top_k,    \
-      top_p, min_p, z, prob)
-  if (chunks <= 4)
-    LDA_SAMPLE(4);
-  else if (chunks <= kMost)
-    LDA_SAMPLE(kMost);
-  else
-    LDA_SAMPLE(0);
+  sample_kernel<T, CHUNKS><<<(unsigned)(B - at < kSlice ? B - at : kSlice), kSampleThreads, 0,  \
+                             s>>>((const typename T::store *)logits + at * ld, ld, V,           \
+                                  weight_digits(V), u + at, from(temperature), from(top_k),     \
+                                  from(top_p), from(min_p), z + at, prob + at)
+    if (chunks <= 4)
+      LDA_SAMPLE(4);
+    else if (chunks <= kMost)
+      LDA_SAMPLE(kMost);
+    else
+      LDA_SAMPLE(0);
 #undef LDA_SAMPLE
+  }
   return launch_status();
 }
 

@@ -249,35 +249,39 @@ __device__ __forceinline__ uint64_t across(uint64_t v, int apart) {
   }
 }
 
-// Sorts the lanes' values, of which those of lanes from `width` (a power of two from 64 on)
-// are not looked at: lane t then holds the t-th.  A bitonic network: exchanges within
-// wavefronts by lane, others through `room`.
-__device__ __forceinline__ uint64_t sorted(uint64_t v, int width, uint64_t *room) {
+// Sorts the lanes' values, of which those of lanes from WIDTH on are not looked at: lane t
+// then holds the t-th.  A bitonic network: exchanges within wavefronts by lane, others
+// through `room`.
+template <int WIDTH>
+__device__ __forceinline__ uint64_t sorted(uint64_t v, uint64_t *room) {
   const int t = (int)threadIdx.x;
-  const bool idle = uniform((uint32_t)t & ~63u) >= (uint32_t)width;
-  for (int size = 2; size <= width; size *= 2)
+  const bool idle = uniform((uint32_t)t & ~63u) >= (uint32_t)WIDTH;
+#pragma unroll
+  for (int size = 2; size <= WIDTH; size *= 2)
+#pragma unroll
     for (int apart = size / 2; apart > 0; apart /= 2) {
-      uint64_t other;
+      uint64_t other = v;
       if (apart >= 64) {
         __syncthreads();
         room[t] = v;
         __syncthreads();
         other = room[t ^ apart];
-      } else if (idle) {
-        continue;
-      } else {
+      } else if (!idle) {
         other = across(v, apart);
       }
-      const bool smaller = ((t & apart) == 0) == ((t & size) == 0 || size == width);
+      // (the lane's number made new, so that a hundred such conditions are not kept in
+      // registers from row to row)
+      int lane = t;
+      asm volatile("" : "+v"(lane));
+      const bool smaller = ((lane & apart) == 0) == ((lane & size) == 0 || size == WIDTH);
       v = smaller == (other < v) ? other : v;
     }
   return v;
 }
 
-__device__ __forceinline__ int sort_width(int n) {
-  int width = 64;
-  while (width < n) width *= 2;
-  return width;
+__device__ __forceinline__ uint64_t sorted(uint64_t v, int n, uint64_t *room) {
+  static_assert(kListed == 1024, "the widths");
+  return n <= 512 ? sorted<512>(v, room) : sorted<1024>(v, room);
 }
 
 // A row of V logits.  A wavefront holds `each` chunks of 64 times 8 of them, one stretch
@@ -479,10 +483,10 @@ __device__ void choose_compared(SampleShared &sh, int n, const Weights &weights,
 template <typename T>
 __device__ void choose_sorted(SampleShared &sh, int n, bool whole, const Weights &weights,
                               const SampleSettings &s, int32_t *z, float *prob) {
-  const int t = (int)threadIdx.x, width = sort_width(n);
+  const int t = (int)threadIdx.x;
   const bool cuts = s.k || s.p < 1.0f;
   uint64_t place = t < n ? sh.list.place[t] : ~0ull;
-  if (cuts || !whole) place = sorted(place, width, sh.list.weight);
+  if (cuts || !whole) place = sorted(place, n, sh.list.weight);
   const bool there = place != ~0ull;
   const float x = Keys<T>::logit((uint32_t)(place >> 32));
   const double w = weights.of(x, there && x > weights.least);
@@ -505,10 +509,10 @@ __device__ void choose_sorted(SampleShared &sh, int n, bool whole, const Weights
   } else if (!whole) {
     // what does not stay has no part in it
     sh.list.place[t] = weight;
-    const uint64_t by = sorted((uint64_t)(weight ? number : 0xFFFFFFFFu) << 32 | (uint32_t)t, width,
-                               sh.list.weight);
+    const uint64_t by =
+        sorted((uint64_t)(weight ? number : 0xFFFFFFFFu) << 32 | (uint32_t)t, n, sh.list.weight);
     __syncthreads();
-    weight = t < width ? sh.list.place[(uint32_t)by] : 0;
+    weight = t < n ? sh.list.place[(uint32_t)by] : 0;
     number = (uint32_t)(by >> 32);
   }
   const uint64_t sum = block_inclusive_sum(sh, 1, weight, &all);
@@ -521,7 +525,7 @@ __device__ void choose_sorted(SampleShared &sh, int n, bool whole, const Weights
 
 template <typename T, int CHUNKS>
 __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
-    const typename T::store *logits, int64_t ld, int64_t B, int32_t V, int digits,
+    const typename T::store *logits, int64_t ld, int32_t V, int digits,
     const float *u, const float *temperature, const int32_t *top_k, const float *top_p,
     const float *min_p, int32_t *z, float *prob) {
   __shared__ SampleShared sh;
@@ -531,171 +535,187 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
   SampleRow<T, CHUNKS> row;
   row.V = V;
   row.each = (int)(((uint32_t)V + 8 * kSampleThreads - 1) / (8 * kSampleThreads));
-  for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
-    row.x = logits + b * ld;
-    const float heat = temperature ? temperature[b] : 1.0f;
-    const int32_t k = top_k ? top_k[b] : 0;
-    const float low = min_p ? min_p[b] : 0.0f;
-    SampleSettings s{k > 0 && k < V ? (uint64_t)k : 0, top_p ? top_p[b] : 1.0f, u[b],
-                     uniform(low > 0.0f ? ldexp(fmin((double)low, 1.0), digits) : 0.0)};
-    row.load();
-    float best = -infinity;  // of this lane
-    row.all([&](uint32_t, int, float x) { best = fmaxf(best, x); });
-    const uint32_t best_key = Keys<T>::of(best);
-    const uint32_t wave_best = wave_min(best_key), wave_worst = ~wave_min(~best_key);
-    if (lane == 0) {
-      sh.tops[wave] = wave_best;
-      sh.worst[wave] = wave_worst;
-    }
-    if (t == 0) sh.listed = 0;
-    __syncthreads();
-    uint32_t top_key = uniform(sh.tops[0]);
+  const uint32_t b = blockIdx.x;
+  row.x = logits + b * ld;
+  const float heat = temperature ? temperature[b] : 1.0f;
+  const int32_t k = top_k ? top_k[b] : 0;
+  const float low = min_p ? min_p[b] : 0.0f;
+  SampleSettings s{k > 0 && k < V ? (uint64_t)k : 0, top_p ? top_p[b] : 1.0f, u[b],
+                   uniform(low > 0.0f ? ldexp(fmin((double)low, 1.0), digits) : 0.0)};
+  row.load();
+  float best = -infinity;  // of this lane
+  row.all([&](uint32_t, int, float x) { best = fmaxf(best, x); });
+  const uint32_t best_key = Keys<T>::of(best);
+  const uint32_t wave_best = wave_min(best_key), wave_worst = ~wave_min(~best_key);
+  if (lane == 0) {
+    sh.tops[wave] = wave_best;
+    sh.worst[wave] = wave_worst;
+  }
+  if (t == 0) sh.listed = 0;
+  __syncthreads();
+  uint32_t top_key = uniform(sh.tops[0]);
 #pragma unroll
-    for (int i = 1; i < kSampleWaves; ++i) {
-      const uint32_t other = uniform(sh.tops[i]);
-      top_key = other < top_key ? other : top_key;
+  for (int i = 1; i < kSampleWaves; ++i) {
+    const uint32_t other = uniform(sh.tops[i]);
+    top_key = other < top_key ? other : top_key;
+  }
+  const float top = uniform(Keys<T>::logit(top_key));
+  const bool greedy = !(heat > 0.0f);
+  if (top == -infinity) {
+    if (t == 0) {
+      z[b] = -1;
+      prob[b] = 0.0f;
     }
-    const float top = uniform(Keys<T>::logit(top_key));
-    const bool greedy = !(heat > 0.0f);
-    if (top == -infinity) {
-      if (t == 0) {
-        z[b] = -1;
-        prob[b] = 0.0f;
-      }
-      __syncthreads();
-      continue;
-    }
-    if (greedy || top == infinity) {
-      // The largest, or infinite ones, which all have the same weight and no other has any:
-      // the rules leave the first of them by number.
-      uint64_t stay = 1, point = 0;
-      const Found f = search(
-          sh, 0, (uint32_t)V - 1, 32,
-          [&](uint64_t all) {
-            if (!greedy) {
-              stay = s.k && s.k < all ? s.k : all;
-              stay = s.p < 1.0f ? share_of(stay, s.p) : stay;
-              point = point_of(stay, s.u);
-            }
-            return point + 1;
-          },
-          [&](auto add) {
-            row.all([&](uint32_t at, int j, float x) {
-              if (x == top) add(at + j, one);
-            });
+    return;
+  }
+  if (greedy || top == infinity) {
+    // The largest, or infinite ones, which all have the same weight and no other has any:
+    // the rules leave the first of them by number.
+    uint64_t stay = 1, point = 0;
+    const Found f = search(
+        sh, 0, (uint32_t)V - 1, 32,
+        [&](uint64_t all) {
+          if (!greedy) {
+            stay = s.k && s.k < all ? s.k : all;
+            stay = s.p < 1.0f ? share_of(stay, s.p) : stay;
+            point = point_of(stay, s.u);
+          }
+          return point + 1;
+        },
+        [&](auto add) {
+          row.all([&](uint32_t at, int j, float x) {
+            if (x == top) add(at + j, one);
           });
-      if (t == 0) {
-        z[b] = (int32_t)f.key;
-        prob[b] = (float)(1.0 / (double)stay);
-      }
-      __syncthreads();
-      continue;
-    }
-    const double per = uniform(1.4426950408889634 / (double)heat);
-    // (2^-(F + 2) is nothing; rounded downwards, so that no logit with a weight is left out)
-    const double nothing = (double)top - (double)(digits + 2) / per;
-    // the largest float that is at most v, and below the top
-    const auto below = [&](double v) {
-      float x = (float)fmax(v, -3.4028234663852886e38);
-      x = (double)x > v ? nextafterf(x, -infinity) : x;
-      return uniform(x < top ? x : nextafterf(top, -infinity));
-    };
-    const float least = below(nothing);
-    const Weights weights{uniform((double)top), per, uniform(0x1.8p52 + (double)digits), least};
-
-    const auto list = [&](uint32_t number, float x) {
-      const uint32_t n = atomicAdd(&sh.listed, 1);
-      if (n < (uint32_t)kListed) sh.list.place[n] = (uint64_t)Keys<T>::of(x) << 32 | number;
-    };
-
-    // ---- few: a list
-    const bool all_listed = V <= kListed;
-    if (all_listed || (s.k && s.k <= kFewest)) {
-      float bound = -3.4028234663852886e38f;
-      if (!all_listed) {
-        uint32_t worst_key = 0;
-        for (int i = 0; i < kSampleWaves; ++i) worst_key = sh.worst[i] > worst_key ? sh.worst[i] : worst_key;
-        const uint32_t end = Keys<T>::of(-infinity) - 1;
-        worst_key = uniform(worst_key < end ? worst_key : end);
-        const Found f = search(
-            sh, top_key, worst_key, 2, [&](uint64_t) { return s.k; },
-            [&](auto add) { add(best_key, one); });
-        // (not there: fewer lanes than k hold any)
-        if (f.there) bound = uniform(Keys<T>::logit(f.key));
-      }
-      __syncthreads();  // bins and list share their memory
-      if (all_listed) {
-        const float x = t < V ? T::up(row.x[t]) : -infinity;
-        sh.list.place[t] = x > -infinity ? (uint64_t)Keys<T>::of(x) << 32 | (uint32_t)t : ~0ull;
-      } else {
-        row.all([&](uint32_t at, int j, float x) {
-          if (x >= bound) list(at + j, x);
         });
-      }
-      __syncthreads();
-      const int n = all_listed ? V : (int)uniform(sh.listed);
-      if (n <= kListed) {
-        if (n <= kCompared)
-          choose_compared<T>(sh, n, weights, s, z + b, prob + b);
-        else
-          choose_sorted<T>(sh, n, all_listed, weights, s, z + b, prob + b);
-        __syncthreads();
-        continue;
-      }
+    if (t == 0) {
+      z[b] = (int32_t)f.key;
+      prob[b] = (float)(1.0 / (double)stay);
     }
+    return;
+  }
+  const double per = uniform(1.4426950408889634 / (double)heat);
+  // (2^-(F + 2) is nothing; rounded downwards, so that no logit with a weight is left out)
+  const double nothing = (double)top - (double)(digits + 2) / per;
+  // the largest float that is at most v, and below the top
+  const auto below = [&](double v) {
+    float x = (float)fmax(v, -3.4028234663852886e38);
+    x = (double)x > v ? nextafterf(x, -infinity) : x;
+    return uniform(x < top ? x : nextafterf(top, -infinity));
+  };
+  const float least = below(nothing);
+  const Weights weights{uniform((double)top), per, uniform(0x1.8p52 + (double)digits), least};
 
-    // ---- many: cuts
-    Stay stay{weights.least, 0};
-    bool known = false;  // sh.kept holds the stretches' sums of what stays
-    // The bins reach down to the lowest logit that has a weight; at high temperatures, where
-    // all may have one, to the row's lowest.
-    float lowest = least;
-    if (heat > 2.0f) {
-      float mine = top;
-      row.all([&](uint32_t, int, float x) { mine = x > least ? fminf(mine, x) : mine; });
-      const uint32_t key = ~wave_min(~Keys<T>::of(mine));
-      __syncthreads();  // `tops` is read
-      if (lane == 0) sh.tops[wave] = key;
-      __syncthreads();
-      for (int i = 0; i < kSampleWaves; ++i) mine = fminf(mine, Keys<T>::logit(sh.tops[i]));
-      lowest = uniform(mine);
+  const auto list = [&](uint32_t number, float x) {
+    const uint32_t n = atomicAdd(&sh.listed, 1);
+    if (n < (uint32_t)kListed) sh.list.place[n] = (uint64_t)Keys<T>::of(x) << 32 | number;
+  };
+
+  // ---- few: a list
+  const bool all_listed = V <= kListed;
+  if (all_listed || (s.k && s.k <= kFewest)) {
+    float bound = -3.4028234663852886e38f;
+    if (!all_listed) {
+      uint32_t worst_key = 0;
+      for (int i = 0; i < kSampleWaves; ++i) worst_key = sh.worst[i] > worst_key ? sh.worst[i] : worst_key;
+      const uint32_t end = Keys<T>::of(-infinity) - 1;
+      worst_key = uniform(worst_key < end ? worst_key : end);
+      const Found f = search(
+          sh, top_key, worst_key, 2, [&](uint64_t) { return s.k; },
+          [&](auto add) { add(best_key, one); });
+      // (not there: fewer lanes than k hold any)
+      if (f.there) bound = uniform(Keys<T>::logit(f.key));
     }
-    const float per_bin = uniform((float)(kSpaced - 1) / (top - lowest));
-    const auto bin_of = [&](float x) {
-      return (uint32_t)fminf((top - x) * per_bin, (float)(kSpaced - 1));
-    };
-    // Cuts after the token, in their order, up to which the amounts reach target(sum of all).
-    const auto cut = [&](auto target_of, auto amount) {
-      uint64_t target = 0;
-      const auto target_once = [&](uint64_t all) { return target = uniform(target_of(all)); };
+    __syncthreads();  // bins and list share their memory
+    if (all_listed) {
+      const float x = t < V ? T::up(row.x[t]) : -infinity;
+      sh.list.place[t] = x > -infinity ? (uint64_t)Keys<T>::of(x) << 32 | (uint32_t)t : ~0ull;
+    } else {
+      row.all([&](uint32_t at, int j, float x) {
+        if (x >= bound) list(at + j, x);
+      });
+    }
+    __syncthreads();
+    const int n = all_listed ? V : (int)uniform(sh.listed);
+    if (n <= kListed) {
+      if (n <= kCompared)
+        choose_compared<T>(sh, n, weights, s, z + b, prob + b);
+      else
+        choose_sorted<T>(sh, n, all_listed, weights, s, z + b, prob + b);
+      return;
+    }
+  }
+
+  // ---- many: cuts
+  Stay stay{weights.least, 0};
+  bool known = false;  // sh.kept holds the stretches' sums of what stays
+  // The bins reach down to the lowest logit that has a weight.
+  float lowest = top;
+  if (s.k || s.p < 1.0f) {
+    row.all([&](uint32_t, int, float x) { lowest = x > least ? fminf(lowest, x) : lowest; });
+    const uint32_t key = ~wave_min(~Keys<T>::of(lowest));
+    __syncthreads();  // `tops` is read
+    if (lane == 0) sh.tops[wave] = key;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSampleWaves; ++i) lowest = fminf(lowest, Keys<T>::logit(sh.tops[i]));
+    lowest = uniform(lowest);
+  }
+  struct Spaced {  // bins evenly spaced from `from` on, and one of them
+    float from, scale, high, low;
+    int at;
+    __device__ __forceinline__ int bin(float x) const {
+      return (int)fminf((from - x) * scale, (float)(kSpaced - 1));
+    }
+    // bin `which`; high and low: its logits, and a hundredth of a bin around them for
+    // the roundings
+    __device__ __forceinline__ void choose(int which) {
+      const double width = 1.0 / (double)scale;
+      at = which;
+      high = uniform((float)((double)from - ((double)which - 0.01) * width));
+      low = uniform(which == kSpaced - 1 ? -__builtin_inff()
+                                         : (float)((double)from - ((double)which + 1.01) * width));
+    }
+    __device__ __forceinline__ bool has(float x) const {
+      return x <= high && x >= low && bin(x) == at;
+    }
+  };
+  // Cuts after the token, in their order, up to which the amounts reach target(sum of all).
+  const auto cut = [&](auto target_of, auto amount) {
+    uint64_t target = 0, before = 0;
+    known = false;
+    Spaced bins{top, uniform((float)(kSpaced - 1) / (top - lowest)), 0.0f, 0.0f, 0}, last = bins;
+    // the bin, then, where it holds too many, a bin of the bin
+    for (int level = 0; level < 2; ++level) {
+      const auto member = [&](uint32_t at, int j, float x) {
+        return stay(x, at, j) && (level == 0 || last.has(x));
+      };
       __syncthreads();  // what was there is read
       for (int i = t; i < kSampleWaves * kSpaced; i += kSampleThreads) (&sh.spaced[0][0])[i] = 0;
       if (t == 0) sh.listed = 0;
       __syncthreads();
       row.all([&](uint32_t at, int j, float x) {
-        if (stay(x, at, j)) atomicAdd(&sh.spaced[wave][bin_of(x)], (unsigned long long)amount(x));
+        if (member(at, j, x)) atomicAdd(&sh.spaced[wave][bins.bin(x)], (unsigned long long)amount(x));
       });
       __syncthreads();
       uint64_t mine = 0;  // (`reached` takes two to a lane: bin t is its bin 2 t)
 #pragma unroll
       for (int i = 0; i < kSampleWaves; ++i) mine += sh.spaced[i][t];
-      const Found f = reached(sh, 0, mine, 0, target_once);
-      known = false;
+      const Found f = reached(sh, before, mine, 0, [&](uint64_t all) {
+        if (level == 0) target = uniform(target_of(all));
+        return target;
+      });
       if (!f.there) return;
+      bins.choose((int)f.key / 2);
+      before = f.before;
       // the stretches' sums up to the bin
-      const int bin_at = (int)f.key / 2;
       uint64_t kept = 0;
-      for (int i = lane; i < bin_at; i += 64) kept += sh.spaced[wave][i];
+      for (int i = lane; i < bins.at; i += 64) kept += sh.spaced[wave][i];
       kept = wave_inclusive_sum(kept);
-      if (lane == 63) sh.kept[wave] = kept;
+      if (lane == 63) sh.kept[wave] = level == 0 ? kept : sh.kept[wave] + kept;
       __syncthreads();  // bins and list share their memory
-      // (the bin's logits, and a hundredth of a bin around them for the roundings)
-      const double bin = 1.0 / (double)per_bin;
-      const float high = uniform((float)((double)top - ((double)bin_at - 0.01) * bin));
-      const float low_end = bin_at == kSpaced - 1 ? -infinity : (float)((double)top - ((double)bin_at + 1.01) * bin);
-      const float low = uniform(low_end);
       row.all([&](uint32_t at, int j, float x) {
-        if (x <= high && x >= low && stay(x, at, j) && (int)bin_of(x) == bin_at) list(at + j, x);
+        if (x <= bins.high && x >= bins.low && member(at, j, x) && bins.bin(x) == bins.at)
+          list(at + j, x);
       });
       __syncthreads();
       const int n = (int)uniform(sh.listed);
@@ -705,134 +725,141 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
           const Compared c = compared<T>(sh, n, amount);
           place = c.place;
           if (c.part == 0) amount_at = c.amount;
-          upto = f.before + c.before + amount_at;
+          upto = before + c.before + amount_at;
         } else {
-          place = sorted(t < n ? sh.list.place[t] : ~0ull, sort_width(n), sh.list.weight);
+          place = sorted(t < n ? sh.list.place[t] : ~0ull, n, sh.list.weight);
           if (t < n) amount_at = amount(Keys<T>::logit((uint32_t)(place >> 32)));
           uint64_t all;
-          upto = f.before + block_inclusive_sum(sh, 1, amount_at, &all);
+          upto = before + block_inclusive_sum(sh, 1, amount_at, &all);
         }
         if (upto - amount_at < target && target <= upto) sh.pick_at = place;
         __syncthreads();
-        const uint64_t last = uniform((uint64_t)sh.pick_at);
-        if (amount_at && place <= last)
-          atomicAdd(&sh.kept[(uint32_t)place / (512u * (uint32_t)row.each)], (unsigned long long)amount_at);
-        stay = Stay{uniform(Keys<T>::logit((uint32_t)(last >> 32))), (uint32_t)last + 1};
+        const uint64_t end = uniform((uint64_t)sh.pick_at);
+        if (amount_at && place <= end)
+          atomicAdd(&sh.kept[(uint32_t)place / (512u * (uint32_t)row.each)],
+                    (unsigned long long)amount_at);
+        stay = Stay{uniform(Keys<T>::logit((uint32_t)(end >> 32))), (uint32_t)end + 1};
         known = true;
         return;
       }
-      const Found g = search(
-          sh, top_key, Keys<T>::of(-infinity) - 1, 32, [&](uint64_t) { return target; },
-          [&](auto add) {
-            row.all([&](uint32_t at, int j, float x) {
-              if (stay(x, at, j)) add(Keys<T>::of(x), [&] { return amount(x); });
-            });
+      last = bins;
+      const float low = last.low > lowest ? last.low : lowest;
+      bins = Spaced{last.high, uniform((float)(kSpaced - 1) / (last.high - low)), 0.0f, 0.0f, 0};
+    }
+    const Found g = search(
+        sh, top_key, Keys<T>::of(-infinity) - 1, 32, [&](uint64_t) { return target; },
+        [&](auto add) {
+          row.all([&](uint32_t at, int j, float x) {
+            if (stay(x, at, j)) add(Keys<T>::of(x), [&] { return amount(x); });
           });
-      const float at = uniform(Keys<T>::logit(g.key));
-      const uint64_t each = uniform(amount(at)), many = (target - g.before + each - 1) / each;
-      const uint32_t end = at == stay.last ? stay.end : 0x7FFFFFFFu;
-      const Found h = search(
-          sh, 0, (uint32_t)V - 1, 32, [&](uint64_t) { return many; },
-          [&](auto add) {
-            row.all([&](uint32_t first, int j, float x) {
-              if (x == at && first + j < end) add(first + j, one);
-            });
+        });
+    const float at = uniform(Keys<T>::logit(g.key));
+    const uint64_t each = uniform(amount(at)), many = (target - g.before + each - 1) / each;
+    const uint32_t end = at == stay.last ? stay.end : 0x7FFFFFFFu;
+    const Found h = search(
+        sh, 0, (uint32_t)V - 1, 32, [&](uint64_t) { return many; },
+        [&](auto add) {
+          row.all([&](uint32_t first, int j, float x) {
+            if (x == at && first + j < end) add(first + j, one);
           });
-      stay = Stay{at, h.key + 1};
-    };
-    if (s.k) cut([&](uint64_t) { return s.k; }, [](float) { return (uint64_t)1; });
-    const auto weight_of = [&](float x) { return Weights::steps(weights.of(x, true)); };
-    if (s.p < 1.0f) cut([&](uint64_t all) { return share_of(all, s.p); }, weight_of);
+        });
+    stay = Stay{at, h.key + 1};
+  };
+  if (s.k) cut([&](uint64_t) { return s.k; }, [](float) { return (uint64_t)1; });
+  const auto weight_of = [&](float x) { return Weights::steps(weights.of(x, true)); };
+  if (s.p < 1.0f) cut([&](uint64_t all) { return share_of(all, s.p); }, weight_of);
 
-    // ---- the choice
-    // (a lane's weights add up to 2^53 at most, exactly in double)
-    const auto staying = [&](float x) {
-      const double w = weights.of(x, true);
-      return w >= s.floor ? Weights::rounded(w) : 0.0;
-    };
-    // min_p: what is far enough below its logit is not asked for its weight
-    if (s.floor > 0.0) {
-      const double at = log2(s.floor) - (double)digits;
-      const float bar = below((double)top + (at - 1e-9) / per);
-      if (bar > stay.last) {
-        stay = Stay{bar, 0};
-        known = false;
-      } else {
-        known = known && (double)weight_of(stay.last) >= s.floor;
-      }
-    }
-    uint64_t total = 0;
-    if (known && s.p < 1.0f) {
-      __syncthreads();
+  // ---- the choice
+  // (a lane's weights add up to 2^53 at most, exactly in double)
+  const auto staying = [&](float x) {
+    const double w = weights.of(x, true);
+    return w >= s.floor ? Weights::rounded(w) : 0.0;
+  };
+  // min_p: what is far enough below its logit is not asked for its weight
+  if (s.floor > 0.0) {
+    const double at = log2(s.floor) - (double)digits;
+    const float bar = below((double)top + (at - 1e-9) / per);
+    if (bar > stay.last) {
+      stay = Stay{bar, 0};
+      known = false;
     } else {
-      // Those that stay are often few: a wavefront puts them in a row and takes the weights
-      // of 64 at a time (256 x 100,000 with min_p: 82 us against 88).
-      __syncthreads();  // `kept`, and what was where the queue is, are read
-      float *queue = sh.queue[wave];
-      uint32_t put = 0, taken = 0;
-      double mine = 0.0;
-      row.chunks([&](uint32_t at, const typename SampleRow<T, CHUNKS>::chunk &c) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float x = row.element(c, j);
-          const bool in = stay(x, at, j);
-          const uint64_t lanes = __builtin_amdgcn_ballot_w64(in);
-          const uint32_t before = __builtin_amdgcn_mbcnt_hi(
-              (uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0));
-          if (in) queue[(put + before) % kQueue] = x;
-          put += (uint32_t)__builtin_popcountll(lanes);
-        }
-        for (; put - taken >= 64; taken += 64) mine += staying(queue[(taken + lane) % kQueue]);
+      known = known && (double)weight_of(stay.last) >= s.floor;
+    }
+  }
+  uint64_t total = 0;
+  if (known && s.p < 1.0f) {
+    __syncthreads();
+  } else {
+    // Those that stay are often few: a wavefront puts them in a row and takes the weights
+    // of 64 at a time (256 x 100,000 with min_p: 82 us against 88).
+    __syncthreads();  // `kept`, and what was where the queue is, are read
+    float *queue = sh.queue[wave];
+    uint32_t put = 0, taken = 0;
+    double mine = 0.0;
+    if (!s.k && !(s.p < 1.0f) && s.floor == 0.0) {
+      row.all([&](uint32_t at, int j, float x) {
+        if (stay(x, at, j)) mine += staying(x);
       });
-      if ((uint32_t)lane < put - taken) mine += staying(queue[(taken + lane) % kQueue]);
-      const uint64_t sum = wave_inclusive_sum((uint64_t)mine);
-      if (lane == 63) sh.kept[wave] = sum;
-      __syncthreads();
-    }
-#pragma unroll
-    for (int i = 0; i < kSampleWaves; ++i) total += uniform((uint64_t)sh.kept[i]);
-    uint64_t point = uniform(point_of(total, s.u));
-    // the wavefront whose stretch holds it
-    int holder = 0;
-    for (; holder < kSampleWaves - 1; ++holder) {
-      const uint64_t sum = uniform((uint64_t)sh.kept[holder]);
-      if (point < sum) break;
-      point -= sum;
-    }
-    // its chunks, one to a wavefront at a time, lanes and elements
-    for (int first = 0, turn = 0; first < row.each; first += kSampleWaves, turn ^= 1) {
-      const typename SampleRow<T, CHUNKS>::chunk c = row.read(holder, first + wave);
-      const uint32_t at = row.first(holder, first + wave);
-      double sum = 0.0;
+    } else row.chunks([&](uint32_t at, const typename SampleRow<T, CHUNKS>::chunk &c) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float x = row.element(c, j);
-        if (stay(x, at, j)) sum += staying(x);
-        if (j & 1) __builtin_amdgcn_sched_barrier(0);
+        const bool in = stay(x, at, j);
+        const uint64_t lanes = __builtin_amdgcn_ballot_w64(in);
+        const uint32_t before = __builtin_amdgcn_mbcnt_hi(
+            (uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0));
+        if (in) queue[(put + before) % kQueue] = x;
+        put += (uint32_t)__builtin_popcountll(lanes);
       }
-      uint64_t all;
-      const uint64_t own = (uint64_t)sum, upto = block_inclusive_sum(sh, turn, own, &all);
-      if (point >= all) {
-        point -= all;
-        continue;
-      }
-      if (upto - own <= point && point < upto) {
-        uint64_t rest = point - (upto - own);
-#pragma unroll 1
-        for (int j = 0; j < 8; ++j) {
-          const float x = T::up(row.x[at + j < (uint32_t)V ? at + j : (uint32_t)V - 1]);
-          const uint64_t w = at + j < (uint32_t)V && stay(x, at, j) ? (uint64_t)staying(x) : 0;
-          if (rest < w) {
-            z[b] = (int32_t)(at + j);
-            prob[b] = (float)((double)w / (double)total);
-            break;
-          }
-          rest -= w;
-        }
-      }
-      break;
-    }
+      for (; put - taken >= 64; taken += 64) mine += staying(queue[(taken + lane) % kQueue]);
+    });
+    if ((uint32_t)lane < put - taken) mine += staying(queue[(taken + lane) % kQueue]);
+    const uint64_t sum = wave_inclusive_sum((uint64_t)mine);
+    if (lane == 63) sh.kept[wave] = sum;
     __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < kSampleWaves; ++i) total += uniform((uint64_t)sh.kept[i]);
+  uint64_t point = uniform(point_of(total, s.u));
+  // the wavefront whose stretch holds it
+  int holder = 0;
+  for (; holder < kSampleWaves - 1; ++holder) {
+    const uint64_t sum = uniform((uint64_t)sh.kept[holder]);
+    if (point < sum) break;
+    point -= sum;
+  }
+  // its chunks, one to a wavefront at a time, lanes and elements
+  for (int first = 0, turn = 0; first < row.each; first += kSampleWaves, turn ^= 1) {
+    const typename SampleRow<T, CHUNKS>::chunk c = row.read(holder, first + wave);
+    const uint32_t at = row.first(holder, first + wave);
+    double sum = 0.0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float x = row.element(c, j);
+      if (stay(x, at, j)) sum += staying(x);
+      if (j & 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    uint64_t all;
+    const uint64_t own = (uint64_t)sum, upto = block_inclusive_sum(sh, turn, own, &all);
+    if (point >= all) {
+      point -= all;
+      continue;
+    }
+    if (upto - own <= point && point < upto) {
+      uint64_t rest = point - (upto - own);
+#pragma unroll 1
+      for (int j = 0; j < 8; ++j) {
+        const float x = T::up(row.x[at + j < (uint32_t)V ? at + j : (uint32_t)V - 1]);
+        const uint64_t w = at + j < (uint32_t)V && stay(x, at, j) ? (uint64_t)staying(x) : 0;
+        if (rest < w) {
+          z[b] = (int32_t)(at + j);
+          prob[b] = (float)((double)w / (double)total);
+          break;
+        }
+        rest -= w;
+      }
+    }
+    break;
   }
 }
 
