@@ -11,7 +11,8 @@
 //
 // direct_product_kernel: a tile of 16 rows and 16 channels to a workgroup, whose wavefronts
 // share the length of K and read what they multiply straight into registers; their sums
-// meet in LDS (whole numbers: in any order the same).  For up to 16 rows.
+// meet in LDS (whole numbers: in any order the same).  For up to 16 rows, and for lines too
+// short or too far apart for the other.
 //
 // tiled_product_kernel: larger tiles, through LDS.
 #pragma once
@@ -39,19 +40,40 @@ struct ProductArgs {
   int32_t N, K;
 };
 
-// 16 bytes at p, of which only the first n are read where n < 16 (the rest: 0).
-__device__ __forceinline__ ints4 load_bytes(const int8_t *p, int n) {
-  if (n >= 16) return *reinterpret_cast<const ints4_any *>(p);
+// The 16 bytes of a line of K >= 16 from byte `at` on, zero from its end on, in two steps:
+// where the line ends among them those that end with it are loaded, and moved down later.
+// So loads have no branch that others would wait in.
+__device__ __forceinline__ ints4 load_piece(const int8_t *line, int at, int K) {
+  const int from = at <= K - 16 ? at : at < K ? K - 16 : 0;
+  return *reinterpret_cast<const ints4_any *>(line + from);
+}
+
+__device__ __forceinline__ ints4 own_piece(const ints4 &v, int at, int K) {
+  const int down = at <= K - 16 ? 0 : at < K ? 8 * (16 - (K - at)) : 128;  // bits
+  uint64_t low = (uint64_t)(uint32_t)v[1] << 32 | (uint32_t)v[0];
+  uint64_t high = (uint64_t)(uint32_t)v[3] << 32 | (uint32_t)v[2];
+  low = down >= 64 ? high : low;
+  high = down >= 64 ? 0 : high;
+  const int rest = down & 63;
+  low = rest ? low >> rest | high << (64 - rest) : low;
+  high >>= rest;
+  low = down == 128 ? 0 : low;
+  return ints4{(int)low, (int)(low >> 32), (int)high, (int)(high >> 32)};
+}
+
+// The same of a line of any length.
+__device__ __forceinline__ ints4 piece_of_any(const int8_t *line, int at, int K) {
+  if (K >= 16) return own_piece(load_piece(line, at, K), at, K);
   ints4 v = {0, 0, 0, 0};
 #pragma unroll
   for (int j = 0; j < 16; ++j)
-    if (j < n) v[j / 4] |= (int)((uint32_t)(uint8_t)p[j] << (8 * (j % 4)));
+    if (at + j < K) v[j / 4] |= (int)((uint32_t)(uint8_t)line[at + j] << (8 * (j % 4)));
   return v;
 }
 
 // The wavefronts of a workgroup share the length of K.
 template <typename T>
-__global__ __launch_bounds__(512) void direct_product_kernel(ProductArgs<T> a, uint32_t col_tiles,
+__global__ __launch_bounds__(256) void direct_product_kernel(ProductArgs<T> a, uint32_t col_tiles,
                                                              int64_t tiles) {
   constexpr int kTile = 16, kPitch = kTile + 4;
   __shared__ int32_t joined[kTile * kPitch];
@@ -68,7 +90,8 @@ __global__ __launch_bounds__(512) void direct_product_kernel(ProductArgs<T> a, u
     for (int i = (int)threadIdx.x; i < kTile * kPitch; i += (int)blockDim.x) joined[i] = 0;
     const int64_t m_in = m0 + line < a.M ? m0 + line : a.M - 1;
     const int64_t n_in = n0 + line < a.N ? n0 + line : a.N - 1;
-    const int8_t *q = a.q + m_in * a.ldq + 16 * part, *w = a.w + n_in * a.ldw + 16 * part;
+    const int8_t *q_line = a.q + m_in * a.ldq, *w_line = a.w + n_in * a.ldw;
+    const int8_t *q = q_line + 16 * part, *w = w_line + 16 * part;
     ints4 sum = {0, 0, 0, 0};
     // (loads first: a matrix instruction keeps the compiler from unrolling a loop)
     const auto steps_at = [&](auto count, int s) {
@@ -89,9 +112,9 @@ __global__ __launch_bounds__(512) void direct_product_kernel(ProductArgs<T> a, u
     if (s + 2 <= whole) steps_at(Count<2>(), s), s += 2;
     if (s < whole) steps_at(Count<1>(), s);
     if (from < to && whole < to) {
-      const int n = a.K - whole * kStep - 16 * part;
-      sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(load_bytes(w + whole * kStep, n),
-                                                  load_bytes(q + whole * kStep, n), sum, 0, 0, 0);
+      const int at = whole * kStep + 16 * part;
+      sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(piece_of_any(w_line, at, a.K),
+                                                  piece_of_any(q_line, at, a.K), sum, 0, 0, 0);
     }
     __syncthreads();  // cleared
     if (from < to) {
@@ -115,8 +138,8 @@ __global__ __launch_bounds__(512) void direct_product_kernel(ProductArgs<T> a, u
 // A workgroup takes BM rows by BN channels: WM x WN wavefronts with (BM / WM) x
 // (BN / WN) of them each, GROUPS times over, the groups sharing the length of K.  It
 // passes by in stages of 128 bytes for each group, each line of which goes from memory to
-// LDS without passing registers, STAGES - 1 of them ahead of the one that is multiplied.  A
-// line's 16-byte pieces lie in LDS in the order piece ^ (line % 8): a matrix operand's
+// LDS without passing registers while the one before it is multiplied.  A line's 16-byte
+// pieces lie in LDS in the order piece ^ (line % 8): a matrix operand's
 // 16 lines would otherwise be in the same banks.  Lines past the last are the last one
 // again (their sums are not stored); pieces past K are piece 0 again, and the rows'
 // operand is cleared there.  ANY: lines that do not start at 16 bytes, or K that is no
@@ -134,18 +157,15 @@ constexpr int kStage = 128;
 typedef __attribute__((address_space(3))) void *lds_pointer;
 typedef const __attribute__((address_space(1))) void *global_pointer;
 
-// Waits until at most N of this wavefront's loads are on their way, and all it asked of
-// LDS is done; then for the other wavefronts.
-template <int N>
+// Waits for what this wavefront asked of memory and of LDS, then for the other wavefronts.
 __device__ __forceinline__ void arrive() {
-  static_assert(N < 64, "six bits");
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (0 << 8) | ((N >> 4) << 14));
+  __builtin_amdgcn_s_waitcnt(7 << 4);  // vmcnt(0), lgkmcnt(0)
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
 
-template <typename T, int BM, int BN, int WM, int WN, int GROUPS, int STAGES, bool ANY>
+template <typename T, int BM, int BN, int WM, int WN, int GROUPS, bool ANY>
 __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tiled_product_kernel(ProductArgs<T> a,
                                                                                uint32_t row_tiles,
                                                                                uint32_t tiles) {
@@ -157,12 +177,10 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tiled_product_kernel(Pr
   constexpr int kBytes = (BM + BN) * GROUPS * kStage;  // of a stage
   constexpr int kFirstW = BM * GROUPS;                 // lines of a stage before the weights'
   static_assert(kQ * 8 * kWaves == BM * GROUPS && kW * 8 * kWaves == BN * GROUPS, "whole loads");
-  static_assert(STAGES >= 2 && STAGES <= 4 && (!ANY || STAGES == 2), "stages");
   static_assert(GROUPS == 1 || (GROUPS - 1) * BM * BN * 4 <= kBytes, "room for the groups' sums");
   // one array to a stage: the compiler then knows that a stage is not written while
   // another one is read
-  __shared__ __attribute__((aligned(16))) int8_t stage0[kBytes], stage1[kBytes],
-      stage2[STAGES > 2 ? kBytes : 16], stage3[STAGES > 3 ? kBytes : 16];
+  __shared__ __attribute__((aligned(16))) int8_t stage0[kBytes], stage1[kBytes];
   const int lane = (int)threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int group = wave / (WM * WN), place = wave % (WM * WN);
@@ -189,38 +207,37 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tiled_product_kernel(Pr
       w_at[i] = (uint32_t)((r < most ? r : most) * a.ldw);
     }
   };
-  // f(address in memory, line of the stage, its first byte's place in K) of this lane's loads
+  // f(number, line in memory, line of the stage, byte of the line) of this lane's loads
   const auto each_load = [&](int stage, auto f) {
     const int8_t *q = a.q + m0 * a.ldq, *w = a.w + n0 * a.ldw;
 #pragma unroll
     for (int i = 0; i < kQ; ++i) {
       const int at = (stage * GROUPS + (wave * kQ + i) * 8 / BM) * kStage + piece;
-      f(i, q + (q_at[i] + (uint32_t)(at < a.K ? at : 0)), (wave * kQ + i) * 8, at);
+      f(i, q + q_at[i], (wave * kQ + i) * 8, at);
     }
 #pragma unroll
     for (int i = 0; i < kW; ++i) {
       const int at = (stage * GROUPS + (wave * kW + i) * 8 / BN) * kStage + piece;
-      f(kQ + i, w + (w_at[i] + (uint32_t)(at < a.K ? at : 0)), kFirstW + (wave * kW + i) * 8, at);
+      f(kQ + i, w + w_at[i], kFirstW + (wave * kW + i) * 8, at);
     }
   };
   const auto bring = [&](int s, int8_t *to) {
-    each_load(turned(s), [&](int, const int8_t *from, int first, int) {
-      __builtin_amdgcn_global_load_lds((global_pointer)from, (lds_pointer)(to + first * kStage), 16,
-                                       0, 0);
+    each_load(turned(s), [&](int, const int8_t *from, int first, int at) {
+      __builtin_amdgcn_global_load_lds((global_pointer)(from + (at < a.K ? at : 0)),
+                                       (lds_pointer)(to + first * kStage), 16, 0, 0);
     });
   };
-  ints4 held[ANY ? kQ + kW : 1];
+  ints4 held[ANY ? kQ + kW : 1];  // a stage on its way through registers
   const auto fetch = [&](int s) {
-    const int stage = turned(s);
-    if ((stage + 1) * GROUPS * kStage <= a.K)
-      each_load(stage, [&](int i, const int8_t *from, int, int) {
-        held[i] = *reinterpret_cast<const ints4_any *>(from);
-      });
-    else
-      each_load(stage, [&](int i, const int8_t *from, int, int at) { held[i] = load_bytes(from, a.K - at); });
+    each_load(turned(s), [&](int i, const int8_t *from, int, int at) {
+      held[i] = load_piece(from, at, a.K);
+    });
   };
-  const auto keep = [&](int8_t *to) {
-    each_load(0, [&](int i, const int8_t *, int first, int) {
+  const auto keep = [&](int s, int8_t *to) {
+    const int stage = turned(s);
+    if ((stage + 1) * GROUPS * kStage > a.K)
+      each_load(stage, [&](int i, const int8_t *, int, int at) { held[i] = own_piece(held[i], at, a.K); });
+    each_load(stage, [&](int i, const int8_t *, int first, int) {
       *reinterpret_cast<ints4 *>(to + first * kStage + lane * 16) = held[i];
     });
   };
@@ -249,27 +266,25 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tiled_product_kernel(Pr
           sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(y[j], x[i], sum[i][j], 0, 0, 0);
     }
   };
-  // stage s, in `here`; the stage STAGES - 1 after it goes to `free`, which was read last
-  const auto step = [&](int s, const int8_t *here, int8_t *free) {
-    const bool more = s + STAGES - 1 < stages;
+  // stage s, in `here`; the next one goes to `there`, which was read last (through registers
+  // no further ahead either: with the stage after it on its way too 4,000 x 4,001 x 4,001
+  // took a fifth longer)
+  const auto step = [&](int s, const int8_t *here, int8_t *there) {
+    const bool more = s + 1 < stages;
+    arrive();
     if constexpr (ANY) {
-      arrive<0>();
       if (more) fetch(s + 1);
       multiply(s, here);
-      if (more) keep(free);
+      if (more) keep(s + 1, there);
     } else {
-      if (s + STAGES - 2 < stages)
-        arrive<(STAGES - 2) * (kQ + kW)>();
-      else
-        arrive<0>();
-      if (more) bring(s + STAGES - 1, free);
+      if (more) bring(s + 1, there);
       multiply(s, here);
     }
   };
   const auto first_stage = [&](int8_t *to) {
     if constexpr (ANY) {
       fetch(0);
-      keep(to);
+      keep(0, to);
     } else {
       bring(0, to);
     }
@@ -279,28 +294,15 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tiled_product_kernel(Pr
   take(tile);
   first_stage(stage0);
   while (true) {
-    if (STAGES > 2 && stages > 1) bring(1, stage1);
-    if (STAGES > 3 && stages > 2) bring(2, stage2);
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j) sum[i][j] = ints4{0, 0, 0, 0};
-    for (int s = 0; s < stages; s += STAGES) {
-      if constexpr (STAGES == 2) {
-        step(s, stage0, stage1);
-        if (s + 1 < stages) step(s + 1, stage1, stage0);
-      } else if constexpr (STAGES == 3) {
-        step(s, stage0, stage2);
-        if (s + 1 < stages) step(s + 1, stage1, stage0);
-        if (s + 2 < stages) step(s + 2, stage2, stage1);
-      } else {
-        step(s, stage0, stage3);
-        if (s + 1 < stages) step(s + 1, stage1, stage0);
-        if (s + 2 < stages) step(s + 2, stage2, stage1);
-        if (s + 3 < stages) step(s + 3, stage3, stage2);
-      }
+    for (int s = 0; s < stages; s += 2) {
+      step(s, stage0, stage1);
+      if (s + 1 < stages) step(s + 1, stage1, stage0);
     }
-    arrive<0>();  // everyone has read the last stage
+    arrive();  // everyone has read the last stage
     if constexpr (GROUPS > 1) {  // the first group adds the others' sums to its own
       ints4 *room = reinterpret_cast<ints4 *>(stage1) + (size_t)place * MT * NT * 64 + lane;
       constexpr int kGroup = BM * BN / 4;
@@ -310,7 +312,7 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tiled_product_kernel(Pr
 #pragma unroll
           for (int j = 0; j < NT; ++j) room[(group - 1) * kGroup + (i * NT + j) * 64] = sum[i][j];
       }
-      arrive<0>();
+      arrive();
       if (group == 0) {
 #pragma unroll
         for (int g = 0; g < GROUPS - 1; ++g)
@@ -319,7 +321,7 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tiled_product_kernel(Pr
 #pragma unroll
             for (int j = 0; j < NT; ++j) sum[i][j] += room[g * kGroup + (i * NT + j) * 64];
       }
-      arrive<0>();  // read, before rows go out through the same memory
+      arrive();  // read, before rows go out through the same memory
     }
     const int64_t m_out = m0 + first_q, n_out = n0 + first_w;
     tile += gridDim.x;
@@ -379,7 +381,6 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tiled_product_kernel(Pr
       __builtin_amdgcn_wave_barrier();
     }
     if (!more) break;
-    if (STAGES > 2) arrive<0>();  // everyone has read what the next stage's loads overwrite
   }
 }
 
