@@ -7,7 +7,13 @@ table (tied), whose gradient therefore has two parts: the dense one of the
 output product, and the one of the words that were looked up, which
 ``embed_grad`` adds to it.
 
-    python examples/language_model.py
+With ``normed`` the output is added to the last word's embedding and normed before
+the output product (``add_norm``, its backward pass ``norm_grad``).  ``answer`` writes
+with the table in 8 bits: the rows in 8 bits (``add_norm_int8`` or ``quantise_rows``), the
+output product of whole numbers (``project_int8``), the rules, and a word by top-k, top-p
+and a uniform number (``sample_logits``).
+
+    python examples/language_model.py [--full]
 """
 from __future__ import annotations
 
@@ -21,7 +27,7 @@ import paper_1505_03851_amd as lda  # noqa: E402
 
 VOCABULARY, SPECIAL, SUCCESSORS = 1000, 10, 4  # words below SPECIAL are never written
 CONTEXT, WIDTH, HIDDEN = 4, 64, 256
-P_DROP, SEED = 0.1, 20150513
+P_DROP, SEED, EPS = 0.1, 20150513, 1e-6
 
 
 class Dropout(torch.autograd.Function):
@@ -37,6 +43,27 @@ class Dropout(torch.autograd.Function):
         return lda.dropout(grad.contiguous(), *ctx.args), None, None, None
 
 
+class Norm(torch.autograd.Function):
+    """(y, h): h = x + residual, normed and weighted."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, eps):
+        ctx.set_materialize_grads(False)
+        y, h = lda.add_norm(x.contiguous(), weight, eps, residual=residual.contiguous())
+        ctx.save_for_backward(h, weight)
+        ctx.eps = eps
+        return y, h
+
+    @staticmethod
+    def backward(ctx, grad, grad_h):
+        h, weight = ctx.saved_tensors
+        if grad is None:  # only h is used
+            return grad_h, grad_h, None, None
+        dx, dw = lda.norm_grad(grad.contiguous(), h, weight, ctx.eps,
+                               residual_grad=None if grad_h is None else grad_h.contiguous())
+        return dx, dx, dw, None
+
+
 def corpus(sequences: int, length: int, g: torch.Generator):
     """(successors [V][4], words int32 [sequences][length])."""
     after = torch.randint(SPECIAL, VOCABULARY, (VOCABULARY, SUCCESSORS), device="cuda", generator=g)
@@ -49,23 +76,32 @@ def corpus(sequences: int, length: int, g: torch.Generator):
 
 
 class Model:
-    def __init__(self, g: torch.Generator):
+    def __init__(self, g: torch.Generator, normed: bool = False):
         def weight(*shape):
             w = torch.randn(shape, device="cuda", generator=g) * shape[0] ** -0.5
             return w.requires_grad_()
         self.table = weight(VOCABULARY, WIDTH)
         self.inner = weight(CONTEXT * WIDTH, HIDDEN)
         self.outer = weight(HIDDEN, WIDTH)
+        self.gain = torch.ones(WIDTH, device="cuda").requires_grad_() if normed else None
 
     def parameters(self):
-        return [self.table, self.inner, self.outer]
+        return [self.table, self.inner, self.outer] + ([] if self.gain is None else [self.gain])
 
-    def logits(self, rows, dropout=None):
-        """rows [B * CONTEXT][WIDTH], the context's embeddings -> [B][V]."""
+    def output(self, rows, dropout=None):
+        """(output [B][WIDTH], last word's embedding) of rows [B * CONTEXT][WIDTH], the
+        context's embeddings."""
         h = torch.relu(rows.view(-1, CONTEXT * WIDTH) @ self.inner)
         if dropout is not None:
             h = Dropout.apply(h, *dropout)
-        return (h @ self.outer) @ self.table.t()
+        return h @ self.outer, rows.view(-1, CONTEXT, WIDTH)[:, -1]
+
+    def logits(self, rows, dropout=None):
+        """rows [B * CONTEXT][WIDTH], the context's embeddings -> [B][V]."""
+        out, last = self.output(rows, dropout)
+        if self.gain is not None:
+            out, _ = Norm.apply(out, last, self.gain, EPS)
+        return out @ self.table.t()
 
 
 def train(model: Model, words, steps: int, batch: int, g: torch.Generator) -> list[float]:
@@ -120,21 +156,60 @@ def generate(model: Model, prompts, length: int, temperature: float = 0.8):
     return history, torch.stack(chances, 1)
 
 
-def main(steps: int = 400, batch: int = 512, sequences: int = 64, length: int = 24) -> dict:
+@torch.no_grad()
+def answer(model: Model, prompts, length: int, g: torch.Generator, temperature: float = 0.8):
+    """As ``generate``, with the table in 8 bits and words by uniform numbers from ``g``."""
+    B, start = prompts.shape
+    history = torch.zeros((B, start + length), dtype=torch.int32, device="cuda")
+    history[:, :start] = prompts
+    lengths = torch.full((B,), start, dtype=torch.int32, device="cuda")
+    special = torch.zeros(VOCABULARY, device="cuda")
+    special[:SPECIAL] = -torch.inf
+
+    def each(value, dtype=torch.float32):
+        return torch.full((B,), value, dtype=dtype, device="cuda")
+    rules = dict(history=history, lengths=lengths, prompt=lengths.clone(), repetition=each(1.05),
+                 bias=special)
+    table, scale = lda.quantise_rows(model.table)
+    chances = []
+    for t in range(start, start + length):
+        rows = lda.embed(model.table, history[:, t - CONTEXT:t].reshape(-1), WIDTH ** 0.5)
+        out, last = model.output(rows)
+        if model.gain is None:
+            q, s = lda.quantise_rows(out)
+        else:
+            q, s, _ = lda.add_norm_int8(out, model.gain, EPS, residual=last)
+        logits = lda.project_int8(q, s, table, scale, dtype=torch.float32)
+        lda.penalise_logits(logits, **rules, out=logits)
+        z, prob = lda.sample_logits(logits, torch.rand(B, device="cuda", generator=g),
+                                    temperature=each(temperature), top_k=each(20, torch.int32),
+                                    top_p=each(0.95), min_p=each(0.02))
+        history[:, t] = z
+        lengths += 1
+        chances.append(prob)
+    return history, torch.stack(chances, 1)
+
+
+def main(steps: int = 400, batch: int = 512, sequences: int = 64, length: int = 24,
+         normed: bool = False, eight_bits: bool = False) -> dict:
     g = torch.Generator(device="cuda")
     g.manual_seed(SEED)
     after, words = corpus(2000, 64, g)
-    model = Model(g)
+    model = Model(g, normed)
     losses = train(model, words, steps, batch, g)
     prompts = words[:sequences, :CONTEXT].contiguous()
-    history, chances = generate(model, prompts, length)
+    if eight_bits:
+        history, chances = answer(model, prompts, length, g)
+    else:
+        history, chances = generate(model, prompts, length)
     follows = (after[history[:, CONTEXT - 1:-1].long()] == history[:, CONTEXT:, None]).any(2)
     return dict(first=losses[0], last=sum(losses[-20:]) / 20, words=history,
                 follows=float(follows.float().mean()), chance=float(chances.mean()))
 
 
 if __name__ == "__main__":
-    r = main()
+    full = "--full" in sys.argv[1:]  # normed, and answering in 8 bits
+    r = main(normed=full, eight_bits=full)
     print(f"loss {r['first']:.2f} -> {r['last']:.2f} (log {SUCCESSORS} is 1.39)")
     print(f"{100 * r['follows']:.1f}% of the generated words follow the word before them in the "
           f"corpus; mean probability of a draw {r['chance']:.2f}")
