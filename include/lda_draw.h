@@ -624,7 +624,7 @@ int lda_draw_logits(const void *logits, int64_t ld_logits, int64_t B, int32_t V,
  * row) / 127.  A row of zeros has the scale 0; one with a NaN or an infinity has
  * a NaN for a scale and zeros for numbers.  scale is not used for other types.
  * eps is above 0 in fp32, finite (LDA_ERR_VALUE).  out (not in 8 bits) and sum may
- * be x or residual themselves (same ld), but not each other.  N = 0 is a no-op; N up
+ * be x or residual themselves (same ld), but not each other (LDA_ERR_VALUE).  N = 0 is a no-op; N up
  * to LDA_MAX_N.  Squares are summed in fp32: rows whose squares are above its
  * range have no norm.
  */

@@ -195,6 +195,7 @@ extern "C" int lda_add_norm(const void *x, int64_t ld_x, const void *residual,
     return LDA_ERR_VALUE;
   if (ld_x < 0 || ld_out < D || (residual && ld_residual < 0) || (sum && ld_sum < D))
     return LDA_ERR_VALUE;
+  if (sum && sum == out) return LDA_ERR_VALUE;
   const bool bits8 = out_dtype == LDA_I8;
   if ((weight_dtype != dtype && weight_dtype != LDA_F32) || (!bits8 && out_dtype != dtype))
     return LDA_ERR_UNSUPPORTED;

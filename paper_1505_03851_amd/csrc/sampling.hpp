@@ -667,13 +667,13 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       return (int)fminf((from - x) * scale, (float)(kSpaced - 1));
     }
     // bin `which`; high and low: its logits, and a hundredth of a bin around them for
-    // the roundings
+    // the roundings.  The last one also has those further than a float's range from the first.
     __device__ __forceinline__ void choose(int which) {
       const double width = 1.0 / (double)scale;
       at = which;
-      high = uniform((float)((double)from - ((double)which - 0.01) * width));
-      low = uniform(which == kSpaced - 1 ? -__builtin_inff()
-                                         : (float)((double)from - ((double)which + 1.01) * width));
+      const bool end = which == kSpaced - 1;
+      high = uniform(end ? __builtin_inff() : (float)((double)from - ((double)which - 0.01) * width));
+      low = uniform(end ? -__builtin_inff() : (float)((double)from - ((double)which + 1.01) * width));
     }
     __device__ __forceinline__ bool has(float x) const {
       return x <= high && x >= low && bin(x) == at;
@@ -683,7 +683,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
   const auto cut = [&](auto target_of, auto amount) {
     uint64_t target = 0, before = 0;
     known = false;
-    Spaced bins{top, uniform((float)(kSpaced - 1) / (top - lowest)), 0.0f, 0.0f, 0}, last = bins;
+    Spaced bins{top, uniform((float)((kSpaced - 1) / ((double)top - (double)lowest))), 0.0f, 0.0f, 0},
+        last = bins;
     // the bin, then, where it holds too many, a bin of the bin
     for (int level = 0; level < 2; ++level) {
       const auto member = [&](uint32_t at, int j, float x) {
@@ -743,6 +744,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
         return;
       }
       last = bins;
+      if (last.at == kSpaced - 1) break;
       const float low = last.low > lowest ? last.low : lowest;
       bins = Spaced{last.high, uniform((float)(kSpaced - 1) / (last.high - low)), 0.0f, 0.0f, 0};
     }

@@ -21,7 +21,7 @@ def st():
     return {k[8:]: v for k, v in STATUS.items() if k != "LDA_OK"}
 
 
-def norm(lib, x=A, ldx=16, r=A, ldr=16, w=A, out=A, ldo=16, total=A, ldt=16, scale=A, N=10, D=16,
+def norm(lib, x=A, ldx=16, r=A, ldr=16, w=A, out=A, ldo=16, total=2 * A, ldt=16, scale=A, N=10, D=16,
          dtype=F32, wt=F32, ot=F32, eps=1e-6):
     return lib.lda_add_norm(x, ldx, r, ldr, w, out, ldo, total, ldt, scale, N, D, dtype, wt, ot,
                             eps, None)
@@ -54,7 +54,8 @@ def test_norm_refusals(lib, st):
         assert norm(lib, **kw) == st["UNSUPPORTED"], kw
     for kw in (dict(dtype=I8), dict(dtype=-1), dict(wt=I8), dict(ot=4), dict(ldx=-1), dict(ldr=-2),
                dict(ldo=15), dict(ldt=15), dict(ldo=15, ot=I8), dict(eps=0.0), dict(eps=-1e-6),
-               dict(eps=float("nan")), dict(eps=float("inf")), dict(eps=1e-60), dict(eps=1e60)):
+               dict(eps=float("nan")), dict(eps=float("inf")), dict(eps=1e-60), dict(eps=1e60),
+               dict(total=A)):
         assert norm(lib, **kw) == st["VALUE"], kw
     for key in ("x", "w", "out"):
         assert norm(lib, **{key: None}) == st["NULL"], key
