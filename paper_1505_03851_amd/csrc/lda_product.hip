@@ -79,7 +79,7 @@ int launch_product(const ProductArgs<T> &a, hipStream_t s) {
   } while (0)
   if (a.M > 64 && t128 >= 160) {
     const int64_t rounds = (t256 + kUnits - 1) / kUnits, halves = (t128 + 2 * kUnits - 1) / (2 * kUnits);
-    if (lines ? 9 * rounds <= 5 * halves : a.K >= 1024 && 3 * rounds <= 2 * halves)
+    if (lines ? 9 * rounds <= 5 * halves : a.K >= 512 && 3 * rounds <= 2 * halves)
       LDA_TILES(256, 256, 2, 4, 1);
     else
       LDA_TILES(128, 128, 2, 4, 1);

@@ -145,9 +145,11 @@ __global__ __launch_bounds__(256) void direct_product_kernel(ProductArgs<T> a, u
 // operand is cleared there.  ANY: lines that do not start at 16 bytes, or K that is no
 // multiple of 16, pass through registers.
 //
-// Workgroups start at different stages, each XCD's at others: lines often lie a
-// power of two apart, so that the same stage of all of them is in a few of the memory's
-// channels.
+// Workgroups start at different stages: lines often lie a power of two apart, so that the
+// same stage of all of them is in a few of the memory's channels (64 x 100,000 x 4,096 112 us
+// where all start at the first, 256 x 8,192 37 against 24).  Tiles of 128 and more, which
+// share lines through their XCD's L2, start alike within an XCD (8,192 x 8,192 x 4,096 238 us;
+// each elsewhere 255, all alike 244).
 //
 // A workgroup takes tile after tile, the next one's first stage on its way while this
 // one's sums go out: by rows through LDS, whole lines of memory at a time.
@@ -188,7 +190,7 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tiled_product_kernel(Pr
   const int first_q = place / WN * kRows, first_w = place % WN * kCols;
   const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
   const int stages = (a.K + kStage * GROUPS - 1) / (kStage * GROUPS);
-  const int turn = (int)((blockIdx.x % 8 * 4 + blockIdx.x / 8) % (uint32_t)stages);
+  const int turn = (int)((blockIdx.x % 8 * 4 + (BM >= 128 ? 0 : blockIdx.x / 8)) % (uint32_t)stages);
   const auto turned = [&](int s) { return s + turn < stages ? s + turn : s + turn - stages; };
 
   int64_t m0, n0;
