@@ -646,7 +646,8 @@ int lda_add_norm(const void *x, int64_t ld_x, const void *residual, int64_t ld_r
  * ld).  Sums are fp32 in an order that depends on N and D alone: the same call
  * gives the same bits.  N = 0: dweight is cleared (or, accumulating, left).  `workspace`:
  * device memory, 8-byte aligned, at least lda_norm_grad_workspace_bytes(N, D)
- * bytes (LDA_ERR_WORKSPACE), free to use again once the call's kernels are done.
+ * bytes (LDA_ERR_WORKSPACE), free to use again once the call's kernels are done; NULL
+ * will do where that is 0 (a few rows).
  */
 size_t lda_norm_grad_workspace_bytes(int64_t N, int32_t D);
 int lda_norm_grad(const void *grad, int64_t ld_grad, const void *h, int64_t ld_h,

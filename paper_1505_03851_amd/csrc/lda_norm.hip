@@ -128,11 +128,20 @@ int launch_quantise(const void *x, int64_t ldx, int8_t *q, int64_t ldq, float *s
 }
 
 // The workgroups that share the rows of a gradient, each with a strip's sums of D: as
-// many as the GPU holds at 16 wavefronts to a compute unit.
+// many as the GPU holds at 16 wavefronts to a compute unit.  One, which needs no second
+// launch (3 us of a small call's 14), for up to eight turns of its rows.
 int32_t strips_of(int64_t N, int32_t D) {
-  const int64_t rows = !in_registers(D) ? 1 : D <= 1024 ? 4 : D <= 2048 ? 2 : 1;  // at a time
+  if (N == 0) return 0;  // nothing is read: there is no workspace either
+  if (!in_registers(D)) return (int32_t)(N < 256 ? N : 256);
+  const int64_t rows = D <= 1024 ? 4 : D <= 2048 ? 2 : 1;  // at a time
+  if (N <= 8 * rows) return 1;
   const int64_t most = D <= 4096 ? 1024 : D <= 8192 ? 512 : 256, all = (N + rows - 1) / rows;
   return (int32_t)(all < most ? all : most);
+}
+
+// Whether the strips' sums are added up by a launch of their own, in a workspace.
+bool joins_strips(int64_t N, int32_t D) {
+  return N == 0 || !in_registers(D) || strips_of(N, D) > 1;
 }
 
 template <typename T>
@@ -142,8 +151,10 @@ int launch_norm_grad(const void *grad, int64_t ldg, const void *h, int64_t ldh,
                      bool accumulate, float *part, hipStream_t s) {
   using S = typename T::store;
   const int32_t strips = strips_of(N, D);
-  const NormGradArgs<T> a{(const S *)grad, (const S *)h, (const S *)residual, weight, (S *)dx, part,
-                          ldg, ldh, ldr, ldx, N, D, (float)eps, weight_float};
+  const bool joins = joins_strips(N, D);
+  const NormGradArgs<T> a{(const S *)grad, (const S *)h, (const S *)residual, weight, (S *)dx,
+                          joins ? part : dw, !joins && accumulate, ldg, ldh, ldr, ldx, N, D,
+                          (float)eps, weight_float};
   if (N > 0 && !in_registers(D))
     norm_grad_long_kernel<T><<<(unsigned)strips, kLongThreads, 0, s>>>(a);
   else if (N > 0) {
@@ -171,6 +182,7 @@ int launch_norm_grad(const void *grad, int64_t ldg, const void *h, int64_t ldh,
 #undef LDA_NORM_GRAD
 #undef LDA_NORM_GRAD_BY
   }
+  if (!joins) return launch_status();
   const int64_t tiles = ((int64_t)D + 63) / 64;
   join_strips_kernel<<<(unsigned)(tiles < (1 << 16) ? tiles : 1 << 16), 1024, 0, s>>>(
       part, strips, D, dw, accumulate);
@@ -218,7 +230,7 @@ extern "C" int lda_add_norm(const void *x, int64_t ld_x, const void *residual,
 
 extern "C" size_t lda_norm_grad_workspace_bytes(int64_t N, int32_t D) {
   if (N <= 0 || D <= 0 || N > LDA_MAX_N) return 0;
-  return 4 * (size_t)strips_of(N, D) * (size_t)D;
+  return joins_strips(N, D) ? 4 * (size_t)strips_of(N, D) * (size_t)D : 0;
 }
 
 extern "C" int lda_norm_grad(const void *grad, int64_t ld_grad, const void *h, int64_t ld_h,
@@ -233,12 +245,14 @@ extern "C" int lda_norm_grad(const void *grad, int64_t ld_grad, const void *h, i
   if (ld_grad < 0 || ld_h < 0 || (residual_grad && ld_residual < 0) || ld_dx < D)
     return LDA_ERR_VALUE;
   if (weight_dtype != dtype && weight_dtype != LDA_F32) return LDA_ERR_UNSUPPORTED;
-  if (!dweight || (N > 0 && (!grad || !h || !weight || !dx || !workspace))) return LDA_ERR_NULL;
+  const size_t need = lda_norm_grad_workspace_bytes(N, D);
+  if (!dweight || (N > 0 && (!grad || !h || !weight || !dx)) || (need > 0 && !workspace))
+    return LDA_ERR_NULL;
   if (!aligned(grad, size) || !aligned(h, size) || !aligned(residual_grad, size) ||
       !aligned(weight, weight_size) || !aligned(dx, size) || !aligned(dweight, 4) ||
       !aligned(workspace, 8))
     return LDA_ERR_ALIGN;
-  if (workspace_bytes < lda_norm_grad_workspace_bytes(N, D)) return LDA_ERR_WORKSPACE;
+  if (workspace_bytes < need) return LDA_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
 #define LDA_RUN(T)                                                                              \
   launch_norm_grad<T>(grad, ld_grad, h, ld_h, residual_grad, ld_residual, weight, dx, ld_dx,    \

@@ -344,7 +344,8 @@ struct NormGradArgs {
   const typename T::store *grad, *h, *residual;
   const void *weight;
   typename T::store *dx;
-  float *part;  // [workgroups][D]: the strips' sums of dw
+  float *part;  // [workgroups][D]: the strips' sums of dw, or dw itself where there is one
+  bool add;     // to what is there (one strip)
   int64_t ldg, ldh, ldr, ldx, N;
   int32_t D;
   float eps;
@@ -452,10 +453,18 @@ __global__ __launch_bounds__(WAVES <= 4 ? kNormThreads : 64 * WAVES) void norm_g
       }
       __syncthreads();
     }
-    for (int c = (int)threadIdx.x; c < a.D; c += kThreads) part[c] = joined[c];
+    for (int c = (int)threadIdx.x; c < a.D; c += kThreads) part[c] = a.add ? part[c] + joined[c] : joined[c];
   } else {
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) store_columns<F32>(part, c[u], dw[u]);
+    for (int u = 0; u < kUnits; ++u) {
+      if (a.add) {
+        float before[8];
+        load_columns<F32>(part, c[u], before);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dw[u][j] += before[j];
+      }
+      store_columns<F32>(part, c[u], dw[u]);
+    }
   }
 }
 

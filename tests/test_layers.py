@@ -75,14 +75,16 @@ def test_norm_grad_refusals(lib, st):
     for kw in (dict(dtype=I8), dict(wt=9), dict(ldg=-1), dict(ldh=-1), dict(ldr=-1), dict(ldx=15),
                dict(eps=0.0), dict(eps=float("nan"))):
         assert grad(lib, **kw) == st["VALUE"], kw
-    for key in ("g", "h", "w", "dx", "dw", "ws"):
+    for key in ("g", "h", "w", "dx", "dw"):
         assert grad(lib, **{key: None}) == st["NULL"], key
+    assert grad(lib, N=100, ws=None) == st["NULL"]
     assert grad(lib, N=0, dw=None) == st["NULL"]  # dweight is cleared
     for key in ("g", "h", "r", "w", "dx", "dw"):
         assert grad(lib, **{key: A + 2}) == st["ALIGN"], key
     assert grad(lib, ws=A + 4) == st["ALIGN"]
-    need = lib.lda_norm_grad_workspace_bytes(10, 16)
-    assert need >= 64 and grad(lib, size=need - 1) == st["WORKSPACE"]
+    need = lib.lda_norm_grad_workspace_bytes(100, 16)
+    assert need >= 64 and grad(lib, N=100, size=need - 1) == st["WORKSPACE"]
+    assert lib.lda_norm_grad_workspace_bytes(10, 16) == 0  # a few rows need none
     for bad in ((0, 16), (-1, 16), (10, 0), (10, -1), (2 ** 33, 16)):
         assert lib.lda_norm_grad_workspace_bytes(*bad) == 0
     assert lib.lda_norm_grad_workspace_bytes(2 ** 32 - 65536, 2 ** 31 - 1) > 2 ** 40

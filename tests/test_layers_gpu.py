@@ -702,7 +702,8 @@ def test_binding_refusals():
         (ValueError, lambda: lda.norm_grad(x, x[:3], w)),
         (ValueError, lambda: lda.norm_grad(x, x, w, accumulate=True)),
         (TypeError, lambda: lda.norm_grad(x, x, w, weight_out=w.bfloat16())),
-        (lda.LdaError, lambda: lda.norm_grad(x, x, w, workspace=torch.empty(8, dtype=torch.uint8, **dev))),
+        (lda.LdaError, lambda: lda.norm_grad(x.repeat(20, 1), x.repeat(20, 1), w,
+                                             workspace=torch.empty(8, dtype=torch.uint8, **dev))),
         (TypeError, lambda: lda.quantise_rows(q)),
         (TypeError, lambda: lda.project_int8(x, s, q, s)),
         (TypeError, lambda: lda.project_int8(q, s, x, s)),
