@@ -47,13 +47,14 @@ def _run(cmd: list[str], verbose: bool) -> None:
 def _compile(src: str | list[str], lib: str, verbose: bool, extra: list[str] | None) -> str:
     srcs = [src] if isinstance(src, str) else list(src)
     flags = [*FLAGS, *(extra or [])]
+    compiling = [f for f in flags if f != "-shared"]
     if len(srcs) == 1:
         _run([HIPCC, *flags, *srcs, "-o", lib + ".tmp"], verbose)
     else:  # the sources at once, then the library of what they gave
         with tempfile.TemporaryDirectory() as folder:
             objects = [os.path.join(folder, os.path.basename(s) + ".o") for s in srcs]
             with concurrent.futures.ThreadPoolExecutor(len(srcs)) as pool:
-                jobs = [pool.submit(_run, [HIPCC, *flags, "-c", s, "-o", o], verbose)
+                jobs = [pool.submit(_run, [HIPCC, *compiling, "-c", s, "-o", o], verbose)
                         for s, o in zip(srcs, objects)]
                 for job in jobs:
                     job.result()
