@@ -679,8 +679,21 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       return x <= high && x >= low && bin(x) == at;
     }
   };
+  // What min_p cuts off, by logits: up to `bar` all, from `pass` on nothing.  (The weight
+  // itself decides between, a 1e-9 of its logarithm.)
+  float bar = least, pass = least;
+  if (s.floor > 0.0) {
+    const double at = log2(s.floor) - (double)digits, up = (double)top + (at + 1e-9) / per;
+    bar = below((double)top + (at - 1e-9) / per);
+    pass = (float)up;
+    pass = uniform((double)pass < up ? nextafterf(pass, infinity) : pass);
+    pass = pass < top ? pass : top;
+  }
   // Cuts after the token, in their order, up to which the amounts reach target(sum of all).
-  const auto cut = [&](auto target_of, auto amount) {
+  // `floors`: the amounts are weights, and min_p follows at once, so that the sums of what
+  // stays are known without another pass over the row: where its bin comes before the
+  // target's, that bin's tokens are the ones it decides on.
+  const auto cut = [&](auto target_of, auto amount, bool floors) {
     uint64_t target = 0, before = 0;
     known = false;
     Spaced bins{top, uniform((float)((kSpaced - 1) / ((double)top - (double)lowest))), 0.0f, 0.0f, 0},
@@ -706,7 +719,16 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
         return target;
       });
       if (!f.there) return;
-      bins.choose((int)f.key / 2);
+      int chosen = (int)f.key / 2;
+      bool by_floor = false;
+      if (floors && level == 0 && bar > least) {
+        const int first = bins.bin(pass), end = bins.bin(nextafterf(bar, infinity));
+        if (first < chosen) {
+          by_floor = floors = first == end;  // (else min_p's border lies over two bins)
+          if (by_floor) chosen = first;
+        }
+      }
+      bins.choose(chosen);
       before = f.before;
       // the stretches' sums up to the bin
       uint64_t kept = 0;
@@ -720,6 +742,18 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       });
       __syncthreads();
       const int n = (int)uniform(sh.listed);
+      if (by_floor) {
+        stay = Stay{bar, 0};
+        known = n <= kListed;
+        if (t < n && known) {
+          const uint64_t place = sh.list.place[t];
+          const double w = weights.of(Keys<T>::logit((uint32_t)(place >> 32)), true);
+          if (w >= s.floor)
+            atomicAdd(&sh.kept[(uint32_t)place / (512u * (uint32_t)row.each)],
+                      (unsigned long long)Weights::steps(w));
+        }
+        return;
+      }
       if (n <= kListed) {
         uint64_t place, amount_at = 0, upto;
         if (n <= kCompared) {
@@ -736,11 +770,12 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
         if (upto - amount_at < target && target <= upto) sh.pick_at = place;
         __syncthreads();
         const uint64_t end = uniform((uint64_t)sh.pick_at);
-        if (amount_at && place <= end)
+        if (amount_at && place <= end &&
+            (!floors || weights.of(Keys<T>::logit((uint32_t)(place >> 32)), true) >= s.floor))
           atomicAdd(&sh.kept[(uint32_t)place / (512u * (uint32_t)row.each)],
                     (unsigned long long)amount_at);
         stay = Stay{uniform(Keys<T>::logit((uint32_t)(end >> 32))), (uint32_t)end + 1};
-        known = true;
+        known = floors && (level == 0 || s.floor == 0.0);
         return;
       }
       last = bins;
@@ -767,9 +802,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
         });
     stay = Stay{at, h.key + 1};
   };
-  if (s.k) cut([&](uint64_t) { return s.k; }, [](float) { return (uint64_t)1; });
+  if (s.k) cut([&](uint64_t) { return s.k; }, [](float) { return (uint64_t)1; }, false);
   const auto weight_of = [&](float x) { return Weights::steps(weights.of(x, true)); };
-  if (s.p < 1.0f) cut([&](uint64_t all) { return share_of(all, s.p); }, weight_of);
+  if (s.p < 1.0f) cut([&](uint64_t all) { return share_of(all, s.p); }, weight_of, true);
 
   // ---- the choice
   // (a lane's weights add up to 2^53 at most, exactly in double)
@@ -777,19 +812,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
     const double w = weights.of(x, true);
     return w >= s.floor ? Weights::rounded(w) : 0.0;
   };
-  // min_p: what is far enough below its logit is not asked for its weight
-  if (s.floor > 0.0) {
-    const double at = log2(s.floor) - (double)digits;
-    const float bar = below((double)top + (at - 1e-9) / per);
-    if (bar > stay.last) {
-      stay = Stay{bar, 0};
-      known = false;
-    } else {
-      known = known && (double)weight_of(stay.last) >= s.floor;
-    }
-  }
+  if (!known && bar > stay.last) stay = Stay{bar, 0};
   uint64_t total = 0;
-  if (known && s.p < 1.0f) {
+  if (known) {
     __syncthreads();
   } else {
     // Those that stay are often few: a wavefront puts them in a row and takes the weights

@@ -185,6 +185,48 @@ def test_sample_of_the_largest_range():
     _check(x, u, t, k, p)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("V", [3000, 20_000, 150_000])
+def test_sample_where_two_cuts_meet(dtype, V):
+    """min_p before the place where top_p ends, at it and after it, a little and by far, with
+    few and many logits around it, and with a top_k that ends before both or after them."""
+    g = np.random.default_rng(V)
+    B = 42
+    p = g.uniform(0.03, 0.99, B).astype(np.float32)
+    # the weights of logits that are evenly spaced: what top_p leaves ends at a weight of 1 - p
+    m = np.exp(np.log1p(-p) + np.resize([-3, -0.3, -0.02, 0.0, 0.02, 0.3, 3], B))
+    m = np.minimum(m, 1.0).astype(np.float32)
+    t, u = np.ones(B, dtype=np.float32), g.random(B).astype(np.float32)
+    x = _rounded(g.uniform(-16, 0, (B, V)), dtype)
+    x[:, g.integers(0, V, V // 5)] = -np.inf
+    args = dict(dtype=dtype, what=(dtype, V))
+    _check(x, u, t, None, p, m, **args)
+    _check(x, g.random(B).astype(np.float32), t, (g.uniform(0.01, 0.3, B) * V).astype(np.int32),
+           p, m, **args)
+    # half of all logits at one place, most often where one of the two ends
+    at = _rounded(np.log(np.where(g.random(B) < 0.5, m, 1 - p)), dtype)
+    x = np.where(g.random((B, V)) < 0.5, at[:, None], x)
+    _check(x, u, t, None, p, m, **args)
+
+
+def test_sample_min_p_between_two_bins():
+    """A min_p whose logit is, but for 1e-9 of it, the border between two of the bins that
+    top_p sums the weights in: 1,023 of them lie evenly between the largest and the lowest."""
+    j = np.arange(64, 1024)
+    t = (j / 64 / np.log(2)).astype(np.float32)  # exp(-(j / 64) / t) = 0.5
+    off = np.abs(t.astype(float) * np.log(2) / (j / 64) - 1)
+    t = t[off < 6e-10]
+    B, V = len(t), 2500
+    assert B >= 5
+    g = np.random.default_rng(23)
+    x = _rounded(-g.uniform(0, 1023 / 64, (B, V)), "float32")
+    x[:, 7], x[:, 1900] = 0.0, -1023 / 64
+    m = np.full(B, 0.5, dtype=np.float32)
+    for p in (0.999, 0.9, 0.6, 0.3):
+        _check(x, g.random(B).astype(np.float32), t, None, np.full(B, p, dtype=np.float32), m,
+               what=p)
+
+
 @pytest.mark.parametrize("V", [1024, 1025, 8192, 8193, 32_768, 32_769, 65_536, 65_537, 131_072, 131_080])
 def test_sample_row_lengths(V):
     """Around the lengths where rows fill lists, chunks and registers: every choice near the end."""
