@@ -396,9 +396,10 @@ struct SampleSettings {
 
 // Of up to 256 listed tokens: each compared with all others.  The lanes of a list's width
 // (wavefronts of `part` 0) get their token's place, its amount (amount(logit)), its rank and
-// the amounts of those before it; sh.list.weight holds the amounts.
+// the amounts of those before it; sh.list.weight holds the amounts.  A lane compares its token
+// with those from `begin` to `end`: one after the other, so that a read of LDS brings two.
 struct Compared {
-  int i, part, parts;
+  int i, part, begin, end;
   uint64_t place, amount, before;
   uint32_t rank;
 };
@@ -407,8 +408,10 @@ template <typename T, typename Amount>
 __device__ __forceinline__ Compared compared(SampleShared &sh, int n, Amount amount) {
   const int t = (int)threadIdx.x;
   const int width = n <= 64 ? 64 : n <= 128 ? 128 : 256;  // (a wavefront's lanes share a `part`)
-  Compared c{t & (width - 1), (int)uniform((uint32_t)t / (uint32_t)width), kSampleThreads / width,
-             0, 0, 0, 0};
+  const int part = (int)uniform((uint32_t)t / (uint32_t)width);
+  const int share = (int)(((uint32_t)n * (uint32_t)width + kSampleThreads - 1) / kSampleThreads);
+  const int begin = part * share, end = begin + share < n ? begin + share : n;
+  Compared c{t & (width - 1), part, begin, end, 0, 0, 0, 0};
   if (t < kCompared) {
     sh.mass[t] = sh.before[t] = 0;
     sh.rank[t] = 0;
@@ -422,11 +425,13 @@ __device__ __forceinline__ Compared compared(SampleShared &sh, int n, Amount amo
   __syncthreads();
   uint32_t rank = 0;
   uint64_t mass = 0;
-  for (int j = c.part; j < n; j += c.parts)
-    if (sh.list.place[j] < c.place) {
-      ++rank;
-      mass += sh.list.weight[j];
-    }
+#pragma unroll 8
+  for (int j = c.begin; j < c.end; ++j) {
+    const uint64_t other = sh.list.weight[j];
+    const bool earlier = sh.list.place[j] < c.place;
+    rank += earlier ? 1 : 0;
+    mass += earlier ? other : 0;
+  }
   if (c.i < n && rank) {
     atomicAdd(&sh.rank[c.i], rank);
     atomicAdd(&sh.mass[c.i], (unsigned long long)mass);
@@ -459,7 +464,8 @@ __device__ void choose_compared(SampleShared &sh, int n, const Weights &weights,
   __syncthreads();
   const uint32_t number = (uint32_t)c.place;
   uint64_t before = 0, all = 0;
-  for (int j = c.part; j < n; j += c.parts) {
+#pragma unroll 8
+  for (int j = c.begin; j < c.end; ++j) {
     const uint64_t other = sh.list.weight[j];
     all += other;
     before += (uint32_t)sh.list.place[j] < number ? other : 0;
@@ -660,23 +666,43 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
     for (int i = 0; i < kSampleWaves; ++i) lowest = fminf(lowest, Keys<T>::logit(sh.tops[i]));
     lowest = uniform(lowest);
   }
-  struct Spaced {  // bins evenly spaced from `from` on, and one of them
-    float from, scale, high, low;
+  // Bins evenly spaced from `from` on, down to `to` (which x is not below), and one of them.
+  // Reckoned in double, whose x - top a weight needs too: x - from times the scale, rounded to
+  // a whole number by the last place of 2^52, at most (from - to) scale, which rounds to the last.
+  struct Spaced {
+    double from, scale;
+    float high, low;
     int at;
+    __device__ __forceinline__ Spaced(double f, double to)
+        : from(f), scale(uniform(f > to ? (kSpaced - 1) / (to - f) : 0.0)), high(0), low(0), at(0) {}
     __device__ __forceinline__ int bin(float x) const {
-      return (int)fminf((from - x) * scale, (float)(kSpaced - 1));
+      return (int)__builtin_bit_cast(words2, fma((double)x - from, scale, 0x1.8p52))[0];
     }
     // bin `which`; high and low: its logits, and a hundredth of a bin around them for
-    // the roundings.  The last one also has those further than a float's range from the first.
+    // the roundings (all logits, where the bins have no width)
     __device__ __forceinline__ void choose(int which) {
-      const double width = 1.0 / (double)scale;
+      const double width = 1.0 / scale;
       at = which;
-      const bool end = which == kSpaced - 1;
-      high = uniform(end ? __builtin_inff() : (float)((double)from - ((double)which - 0.01) * width));
-      low = uniform(end ? -__builtin_inff() : (float)((double)from - ((double)which + 1.01) * width));
+      high = uniform(scale < 0.0 ? (float)(from + ((double)which - 0.51) * width) : __builtin_inff());
+      low = uniform(scale < 0.0 ? (float)(from + ((double)which + 0.51) * width) : -__builtin_inff());
     }
+    __device__ __forceinline__ bool wide() const { return !(high - low < __builtin_inff()); }
     __device__ __forceinline__ bool has(float x) const {
       return x <= high && x >= low && bin(x) == at;
+    }
+  };
+  // f(place, logit) of a chunk's logits that are among(place, logit), the lanes' next ones
+  // side by side: few, so that a branch for each logit would be taken for one lane.
+  const auto each_of = [&](const typename SampleRow<T, CHUNKS>::chunk &c, auto among, auto f) {
+    uint32_t places = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) places |= among(j, row.element(c, j)) ? 1u << j : 0;
+    for (; places; places &= places - 1) {
+      const int j = __builtin_ctz(places);
+      float x = row.element(c, 0);
+#pragma unroll
+      for (int i = 1; i < 8; ++i) x = i == j ? row.element(c, i) : x;
+      f(j, x);
     }
   };
   // What min_p cuts off, by logits: up to `bar` all, from `pass` on nothing.  (The weight
@@ -696,8 +722,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
   const auto cut = [&](auto target_of, auto amount, bool floors) {
     uint64_t target = 0, before = 0;
     known = false;
-    Spaced bins{top, uniform((float)((kSpaced - 1) / ((double)top - (double)lowest))), 0.0f, 0.0f, 0},
-        last = bins;
+    Spaced bins(weights.top, (double)lowest), last = bins;
     // the bin, then, where it holds too many, a bin of the bin
     for (int level = 0; level < 2; ++level) {
       const auto member = [&](uint32_t at, int j, float x) {
@@ -707,9 +732,17 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       for (int i = t; i < kSampleWaves * kSpaced; i += kSampleThreads) (&sh.spaced[0][0])[i] = 0;
       if (t == 0) sh.listed = 0;
       __syncthreads();
-      row.all([&](uint32_t at, int j, float x) {
-        if (member(at, j, x)) atomicAdd(&sh.spaced[wave][bins.bin(x)], (unsigned long long)amount(x));
-      });
+      const auto add = [&](auto in) {
+        row.all([&](uint32_t at, int j, float x) {
+          if (in(at, j, x)) atomicAdd(&sh.spaced[wave][bins.bin(x)], (unsigned long long)amount(x));
+        });
+      };
+      // (a first cut asks no numbers, and its bins share a weight's steps: the sums of 49,999
+      // floats' weights take 16 us against 19)
+      if (level == 0 && stay.end == 0)
+        add([&](uint32_t, int, float x) { return x >= stay.above; });
+      else
+        add(member);
       __syncthreads();
       uint64_t mine = 0;  // (`reached` takes two to a lane: bin t is its bin 2 t)
 #pragma unroll
@@ -722,7 +755,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       int chosen = (int)f.key / 2;
       bool by_floor = false;
       if (floors && level == 0 && bar > least) {
-        const int first = bins.bin(pass), end = bins.bin(nextafterf(bar, infinity));
+        const int first = bins.bin(fmaxf(pass, lowest)),
+                  end = bins.bin(fmaxf(nextafterf(bar, infinity), lowest));
         if (first < chosen) {
           by_floor = floors = first == end;  // (else min_p's border lies over two bins)
           if (by_floor) chosen = first;
@@ -732,13 +766,28 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       before = f.before;
       // the stretches' sums up to the bin
       uint64_t kept = 0;
-      for (int i = lane; i < bins.at; i += 64) kept += sh.spaced[wave][i];
+#pragma unroll
+      for (int i = 0; i < kSpaced; i += 64) {
+        const uint64_t sum = sh.spaced[wave][i + lane];
+        kept += i + lane < bins.at ? sum : 0;
+      }
       kept = wave_inclusive_sum(kept);
       if (lane == 63) sh.kept[wave] = level == 0 ? kept : sh.kept[wave] + kept;
       __syncthreads();  // bins and list share their memory
-      row.all([&](uint32_t at, int j, float x) {
-        if (x <= bins.high && x >= bins.low && member(at, j, x) && bins.bin(x) == bins.at)
-          list(at + j, x);
+      // (most chunks have none: what is next to the bin's middle decides, without a branch for
+      // each; 49,999 floats 2.5 us against 4)
+      const float middle = uniform(bins.wide() ? 0.0f : 0.5f * bins.high + 0.5f * bins.low);
+      const float reach =
+          uniform(bins.wide() ? infinity : fmaxf(bins.high - middle, middle - bins.low));
+      row.chunks([&](uint32_t at, const typename SampleRow<T, CHUNKS>::chunk &c) {
+        float nearest = infinity;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) nearest = fminf(nearest, fabsf(row.element(c, j) - middle));
+        if (!(nearest <= reach)) return;
+        each_of(c, [&](int, float x) { return fabsf(x - middle) <= reach; }, [&](int j, float x) {
+          if (x <= bins.high && x >= bins.low && member(at, j, x) && bins.bin(x) == bins.at)
+            list(at + j, x);
+        });
       });
       __syncthreads();
       const int n = (int)uniform(sh.listed);
@@ -779,9 +828,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
         return;
       }
       last = bins;
-      if (last.at == kSpaced - 1) break;
-      const float low = last.low > lowest ? last.low : lowest;
-      bins = Spaced{last.high, uniform((float)(kSpaced - 1) / (last.high - low)), 0.0f, 0.0f, 0};
+      if (last.wide()) break;
+      bins = Spaced((double)last.high, (double)fmaxf(last.low, lowest));
     }
     const Found g = search(
         sh, top_key, Keys<T>::of(-infinity) - 1, 32, [&](uint64_t) { return target; },
@@ -872,18 +920,21 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       point -= all;
       continue;
     }
-    if (upto - own <= point && point < upto) {
-      uint64_t rest = point - (upto - own);
-#pragma unroll 1
-      for (int j = 0; j < 8; ++j) {
-        const float x = T::up(row.x[at + j < (uint32_t)V ? at + j : (uint32_t)V - 1]);
-        const uint64_t w = at + j < (uint32_t)V && stay(x, at, j) ? (uint64_t)staying(x) : 0;
-        if (rest < w) {
-          z[b] = (int32_t)(at + j);
-          prob[b] = (float)((double)w / (double)total);
-          break;
-        }
-        rest -= w;
+    const uint64_t owner = __builtin_amdgcn_ballot_w64(upto - own <= point && point < upto);
+    if (owner) {  // its wavefront takes the lane's eight side by side
+      const int from = __builtin_ctzll(owner);
+      const uint64_t gone = upto - own;
+      const uint64_t rest =
+          point - ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(gone >> 32), from) << 32 |
+                   (uint32_t)__builtin_amdgcn_readlane((int)gone, from));
+      const uint32_t v = (uint32_t)__builtin_amdgcn_readlane((int)at, from) + (uint32_t)lane;
+      const bool one_of = lane < 8 && v < (uint32_t)V;
+      const float x = T::up(row.x[one_of ? v : 0]);
+      const uint64_t w = one_of && stay(x, v, 0) ? (uint64_t)staying(x) : 0;
+      const uint64_t sum_to = wave_inclusive_sum(w);
+      if (sum_to - w <= rest && rest < sum_to) {
+        z[b] = (int32_t)v;
+        prob[b] = (float)((double)w / (double)total);
       }
     }
     break;
