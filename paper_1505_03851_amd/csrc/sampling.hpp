@@ -21,7 +21,9 @@
 //     weight for top_p) to 1,024 bins in LDS, evenly spaced in x over the logits that have a
 //     weight; those of the bin where the running sum reaches its target go to a list, which
 //     is compared or sorted.  Where they are more than 1,024 (equal logits, most often) bins
-//     narrow down on the logit's bits instead, then on the tokens' numbers.
+//     narrow down on the logit's bits instead, then on the tokens' numbers.  min_p is
+//     applied with top_p's cut, by its own bin; up to 1,024 tokens that top_k leaves go
+//     to a list at once.
 //   * Each wavefront holds a stretch of the row and has bins of its own, so the sums of the
 //     stretches' weights that stay are there after the last cut.  z is found by them, then by
 //     the stretch's chunks, one to a wavefront, lanes and elements.
@@ -722,6 +724,49 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
   const auto cut = [&](auto target_of, auto amount, bool floors) {
     uint64_t target = 0, before = 0;
     known = false;
+    // among the n tokens of the list, `before` before them (n <= kListed)
+    const auto of_list = [&](int n, bool whole, bool sums) {
+      uint64_t place, amount_at = 0, upto;
+      if (n <= kCompared && !whole) {
+        const Compared c = compared<T>(sh, n, amount);
+        place = c.place;
+        if (c.part == 0) amount_at = c.amount;
+        upto = before + c.before + amount_at;
+      } else {
+        place = sorted(t < n ? sh.list.place[t] : ~0ull, n, sh.list.weight);
+        if (t < n) amount_at = amount(Keys<T>::logit((uint32_t)(place >> 32)));
+        uint64_t all;
+        upto = before + block_inclusive_sum(sh, 1, amount_at, &all);
+        if (whole) target = uniform(target_of(all));
+      }
+      if (upto - amount_at < target && target <= upto) sh.pick_at = place;
+      __syncthreads();
+      const uint64_t end = uniform((uint64_t)sh.pick_at);
+      if (amount_at && place <= end &&
+          (!floors || weights.of(Keys<T>::logit((uint32_t)(place >> 32)), true) >= s.floor))
+        atomicAdd(&sh.kept[(uint32_t)place / (512u * (uint32_t)row.each)],
+                  (unsigned long long)amount_at);
+      stay = Stay{uniform(Keys<T>::logit((uint32_t)(end >> 32))), (uint32_t)end + 1};
+      known = floors && (sums || s.floor == 0.0);
+    };
+    // What a small top_k leaves is a list as it is (256 x 100,000 with all settings 60 us, 63 by
+    // bins here too).
+    if (floors && s.k && s.k <= kListed) {
+      __syncthreads();  // what was there is read
+      if (t == 0) sh.listed = 0;
+      if (t < kSampleWaves) sh.kept[t] = 0;
+      __syncthreads();
+      row.chunks([&](uint32_t at, const typename SampleRow<T, CHUNKS>::chunk &c) {
+        each_of(c, [&](int j, float x) { return stay(x, at, j); },
+                [&](int j, float x) { list(at + j, x); });
+      });
+      __syncthreads();
+      const int n = (int)uniform(sh.listed);
+      if (n <= kListed) {
+        of_list(n, true, true);
+        return;
+      }
+    }
     Spaced bins(weights.top, (double)lowest), last = bins;
     // the bin, then, where it holds too many, a bin of the bin
     for (int level = 0; level < 2; ++level) {
@@ -804,27 +849,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
         return;
       }
       if (n <= kListed) {
-        uint64_t place, amount_at = 0, upto;
-        if (n <= kCompared) {
-          const Compared c = compared<T>(sh, n, amount);
-          place = c.place;
-          if (c.part == 0) amount_at = c.amount;
-          upto = before + c.before + amount_at;
-        } else {
-          place = sorted(t < n ? sh.list.place[t] : ~0ull, n, sh.list.weight);
-          if (t < n) amount_at = amount(Keys<T>::logit((uint32_t)(place >> 32)));
-          uint64_t all;
-          upto = before + block_inclusive_sum(sh, 1, amount_at, &all);
-        }
-        if (upto - amount_at < target && target <= upto) sh.pick_at = place;
-        __syncthreads();
-        const uint64_t end = uniform((uint64_t)sh.pick_at);
-        if (amount_at && place <= end &&
-            (!floors || weights.of(Keys<T>::logit((uint32_t)(place >> 32)), true) >= s.floor))
-          atomicAdd(&sh.kept[(uint32_t)place / (512u * (uint32_t)row.each)],
-                    (unsigned long long)amount_at);
-        stay = Stay{uniform(Keys<T>::logit((uint32_t)(end >> 32))), (uint32_t)end + 1};
-        known = floors && (level == 0 || s.floor == 0.0);
+        of_list(n, false, level == 0);
         return;
       }
       last = bins;

@@ -211,10 +211,11 @@ def test_sample_where_two_cuts_meet(dtype, V):
 
 def test_sample_min_p_between_two_bins():
     """A min_p whose logit is, but for 1e-9 of it, the border between two of the bins that
-    top_p sums the weights in: 1,023 of them lie evenly between the largest and the lowest."""
-    j = np.arange(64, 1024)
-    t = (j / 64 / np.log(2)).astype(np.float32)  # exp(-(j / 64) / t) = 0.5
-    off = np.abs(t.astype(float) * np.log(2) / (j / 64) - 1)
+    top_p sums the weights in, half way between two of the 1,024 evenly spaced logits from
+    the largest to the lowest."""
+    border = (np.arange(64, 1023) + 0.5) / 64
+    t = (border / np.log(2)).astype(np.float32)  # exp(-border / t) = 0.5
+    off = np.abs(t.astype(float) * np.log(2) / border - 1)
     t = t[off < 6e-10]
     B, V = len(t), 2500
     assert B >= 5
