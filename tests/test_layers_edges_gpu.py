@@ -228,6 +228,20 @@ def test_sample_min_p_between_two_bins():
                what=p)
 
 
+def test_sample_at_extreme_temperatures():
+    """An infinite temperature makes all logits' weights one, the smallest leaves the largest."""
+    g = np.random.default_rng(5)
+    B, V = 24, 5000
+    x = _rounded(g.normal(0, 3, (B, V)), "float32")
+    t = np.resize(np.array([np.inf, 3e38, 1e-30, 1e-45], dtype=np.float32), B)
+    u = g.random(B).astype(np.float32)
+    p = np.resize(np.array([0.3, 0.77, 1.0], dtype=np.float32), B)
+    m = np.repeat(np.array([0.0, 0.4, 1.0], dtype=np.float32), B // 3)
+    k = np.repeat(np.array([0, 700, 3000, 0], dtype=np.int32), B // 4)
+    for args in ((t, None, p), (t, None, p, m), (t, k, p, m), (t, k)):
+        _check(x, u, *args, what=len(args))
+
+
 @pytest.mark.parametrize("V", [1024, 1025, 8192, 8193, 32_768, 32_769, 65_536, 65_537, 131_072, 131_080])
 def test_sample_row_lengths(V):
     """Around the lengths where rows fill lists, chunks and registers: every choice near the end."""
