@@ -621,7 +621,8 @@ int lda_draw_logits(const void *logits, int64_t ld_logits, int64_t B, int32_t V,
  * that type or LDA_F32 (weight_dtype).  out [N][D] is of type out_dtype: dtype, or
  * LDA_I8: then row n is held as whole numbers from -127 to 127 that stand for
  * themselves times scale[n] (fp32 [N]): scale = (the largest magnitude of the
- * row) / 127.  A row of zeros has the scale 0; one with a NaN or an infinity has
+ * row) / 127, and the numbers are those that lda_quantise_rows gives of out in
+ * fp32.  A row of zeros has the scale 0; one with a NaN or an infinity has
  * a NaN for a scale and zeros for numbers.  scale is not used for other types.
  * eps is above 0 in fp32, finite (LDA_ERR_VALUE).  out (not in 8 bits) and sum may
  * be x or residual themselves (same ld), but not each other (LDA_ERR_VALUE).  N = 0 is a no-op; N up

@@ -78,12 +78,7 @@ __device__ __forceinline__ Steps steps_of(uint32_t top_bits) {
   return s;
 }
 
-// A value that was rounded on its way (the norm's): the nearest step.
-__device__ __forceinline__ int step_of(float y, const Steps &s) {
-  return (int)rintf(y * s.shift * (127.0f * s.inverse));
-}
-
-// A value as it was given.  127 x / top is half a step above a whole number for every
+// The nearest step of a value.  127 x / top is half a step above a whole number for every
 // x = top / 2, and for many x where top's digits have a factor 127, so the side of
 // the half is decided exactly.  16-bit x: 127 x is exact, and one correction of the
 // quotient by its remainder (exact too) rounds it rightly; the nearest half is then
@@ -101,6 +96,26 @@ __device__ __forceinline__ int exact_step_of(float x, const Steps &s) {
     const float above = __builtin_fmaf(-(f + 0.5f), s.top, p) + low;
     const int q = (int)f;
     return s.inverse > 0.0f ? q + ((above > 0.0f || (above == 0.0f && (q & 1))) ? 1 : 0) : 0;
+  }
+}
+
+// The same of 8 floats (the norm's, which were rounded on their way and are seldom next to a
+// half), in the low bytes of q.  Two roundings leave the quotient off by 127 * 2 * 2^-24 at
+// most, so only within 2^-16 of a half is the side decided exactly: about one in 64 times of a
+// wavefront's 512 columns.
+__device__ __forceinline__ void exact_steps_of(const float (&x)[8], const Steps &s, int (&q)[8]) {
+  constexpr float kWhole = 0x1.8p23f;  // what rounds to whole numbers, in the last bits
+  const float per = 127.0f * s.inverse;
+  float furthest = 0.0f;  // from a whole number
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float v = x[j] * s.shift, t = __builtin_fmaf(v, per, kWhole);
+    furthest = fmaxf(furthest, fabsf(__builtin_fmaf(v, per, -(t - kWhole))));
+    q[j] = __builtin_bit_cast(int, t);
+  }
+  if (furthest > 0.5f - 0x1p-16f || !(s.inverse > 0.0f)) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = exact_step_of<F32>(x[j], s);
   }
 }
 
@@ -263,8 +278,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kNormThreads : 64 * WAVES) void norm_k
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
       int q[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) q[j] = steps.inverse > 0.0f ? step_of(h[u][j], steps) : 0;
+      exact_steps_of(h[u], steps, q);
       store_step_columns((int8_t *)a.out + row * a.ldo, c[u], q);
     }
   }
@@ -323,16 +337,15 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(NormArgs<T> a) 
       load(col, n, h);
       load_weight<T>(a.weight, a.weight_float, col, n, w);
       if (a.sum) store_elements<T, 8>(a.sum + row * a.lds + col, n, h);
-      int q[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        h[j] = h[j] * s * w[j];
-        q[j] = BITS8 && steps.inverse > 0.0f ? step_of(h[j], steps) : 0;
-      }
-      if (BITS8)
+      for (int j = 0; j < 8; ++j) h[j] = h[j] * s * w[j];
+      if (BITS8) {
+        int q[8];
+        exact_steps_of(h, steps, q);
         store_steps((int8_t *)a.out + row * a.ldo + col, n, q);
-      else
+      } else {
         store_elements<T, 8>((S *)a.out + row * a.ldo + col, n, h);
+      }
     }
   }
 }

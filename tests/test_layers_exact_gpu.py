@@ -1,0 +1,48 @@
+"""What one operator of the way from a layer's last activations to the next token gives has to
+equal, bit for bit, what another way to the same numbers gives."""
+import numpy as np
+import pytest
+
+from test_layers_gpu import SIZES, _norm_inputs
+from test_tokens_gpu import TYPES, _gpu, _lda
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- the norm's 8 bits: those of its rows in float
+
+
+@pytest.mark.parametrize("N,D", [*SIZES, (2000, 600), (500, 3000), (100, 12_000), (60, 20_000)])
+def test_norm_bits_are_those_of_its_rows(N, D):
+    """The rows as add_norm gives them in float, put into 8 bits by quantise_rows, which decides
+    every half exactly: of a million columns about fifteen are so near to one that a rounding on the
+    way would move them."""
+    import torch
+    lda = _lda()
+    for residual in (True, False):
+        x, r, w = _norm_inputs(N, D, "float32", "float32", residual)
+        args = _gpu(x, "float32"), _gpu(w, "float32"), 1e-5
+        more = None if r is None else _gpu(r, "float32")
+        y = lda.add_norm(*args, residual=more)
+        want = lda.quantise_rows(y[0] if residual else y)
+        got = lda.add_norm_int8(*args, residual=more)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [40, 700, 3000, 5003, 20_001])
+def test_norm_bits_at_halves(dtype, D):
+    """Rows of one magnitude under weights that are halves of the 127th part of the largest, so
+    that nearly every column is next to a half; and 16-bit rows as the same rows in float."""
+    import torch
+    lda = _lda()
+    g = np.random.default_rng(D)
+    w = (g.integers(-127, 127, D) + 0.5).astype(np.float32)
+    w[D // 3] = 127
+    sign = g.choice([-1.0, 1.0], (12, D))
+    x = sign * np.resize([1.0, 0.75, 1.25, 3.0, 0.1015625, 30.0], (12, 1))
+    rows, weight = _gpu(x, dtype), _gpu(w)
+    got = lda.add_norm_int8(rows, weight)
+    want = lda.quantise_rows(lda.add_norm(rows.float(), weight))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert bool((got[0].abs().amax(1) == 127).all())
