@@ -254,9 +254,10 @@ def project_int8(q, scale, weight, weight_scale, bias=None, dtype=None,
     """out[m][n] = (sum over k of q[m][k] * weight[n][k]) * scale[m] * weight_scale[n]
     + bias[n] (lda_project_int8): rows and weights as ``quantise_rows`` and
     ``add_norm_int8`` give them.  q int8 [M][K] (or a contiguous tensor of any shape) with
-    ``scale`` float32 of its shape without the last dimension; weight int8 [N][K],
-    weight_scale float32 [N], bias float32 [N].  ``out``, or a new tensor of type
-    ``dtype`` (None: bfloat16).  ``stream``: where it runs (None: the current stream)."""
+    ``scale`` float32 of its shape without the last dimension (a vector is contiguous; of
+    more dimensions one that is not is copied); weight int8 [N][K], weight_scale float32 [N],
+    bias float32 [N].  ``out``, or a new tensor of type ``dtype`` (None: bfloat16).
+    ``stream``: where it runs (None: the current stream)."""
     dev = q.get_device()
     a = q if q.dim() == 2 else _matrix(q, "q")
     M, K, ldq = _rows(a, "q", dev, _I8)
@@ -267,7 +268,9 @@ def project_int8(q, scale, weight, weight_scale, bias=None, dtype=None,
         _lib._check(_UNSUPPORTED)
     if not isinstance(scale, _Tensor) or scale.shape != q.shape[:-1]:
         raise ValueError(f"scale must be a tensor of the shape {tuple(q.shape[:-1])}")
-    s = _vector(scale if scale.dim() == 1 else scale.reshape(-1), "scale", _F32, M, dev)
+    # (one of several dimensions may be a copy here, which has to live until the launch)
+    steps = scale if scale.dim() == 1 else scale.contiguous().view(-1)
+    s = _vector(steps, "scale", _F32, M, dev)
     ws = _vector(weight_scale, "weight_scale", _F32, N, dev)
     b = None if bias is None else _vector(bias, "bias", _F32, N, dev)
     if _recording() and (scale.requires_grad or weight_scale.requires_grad

@@ -1,0 +1,51 @@
+"""The binding of the operators between a layer's last activations and the next token, on the CPU:
+what a call of the library is given, with the library's call put aside."""
+import ctypes
+
+import numpy as np
+import pytest
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The binding on CPU tensors: [(name, arguments)] of what would be launched."""
+    from paper_1505_03851_amd import _layers
+    made = []
+    monkeypatch.setattr(_layers, "_run", lambda name, dev, *args: made.append((name, args)))
+    return made
+
+
+def _floats(address, n):
+    return np.ctypeslib.as_array(ctypes.cast(address, ctypes.POINTER(ctypes.c_float)), (n,))
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_project_scale_lives_until_the_launch(monkeypatch, given):
+    """A scale of several dimensions that is not contiguous is copied: the copy's memory is not to
+    be handed out again, for the output above all, before the kernel is launched."""
+    import weakref
+
+    import torch
+
+    from paper_1505_03851_amd import _layers
+    scale = torch.arange(6 * 500, dtype=torch.float32).view(6, 500).t()  # [500][6]
+    q = torch.zeros(500, 6, 8, dtype=torch.int8)
+    w, ws = torch.zeros(5, 8, dtype=torch.int8), torch.ones(5)
+    seen, launched = {}, []
+    vector = _layers._vector
+
+    def watched(t, name, *args):
+        seen[name] = weakref.ref(t), t.data_ptr()
+        return vector(t, name, *args)
+
+    def run(name, dev, *args):
+        alive, address = seen["scale"]
+        assert alive() is not None, "the scale is freed before the launch"
+        assert args[2] == address
+        assert np.array_equal(_floats(args[2], 3000), scale.reshape(-1).numpy())
+        launched.append(name)
+    monkeypatch.setattr(_layers, "_vector", watched)
+    monkeypatch.setattr(_layers, "_run", run)
+    out = torch.empty(500, 6, 5) if given else None
+    y = _layers.project_int8.__wrapped__(q, scale, w, ws, dtype=torch.float32, out=out)
+    assert launched == ["lda_project_int8"] and y.shape == (500, 6, 5)

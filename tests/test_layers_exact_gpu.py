@@ -46,3 +46,28 @@ def test_norm_bits_at_halves(dtype, D):
     want = lda.quantise_rows(lda.add_norm(rows.float(), weight))
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     assert bool((got[0].abs().amax(1) == 127).all())
+
+
+# ---- the product: a scale of any layout
+
+
+@pytest.mark.parametrize("T,B,N,K", [(2, 300, 1, 64), (300, 2, 1, 64), (64, 33, 1, 4096), (8, 70, 40, 200),
+                                     (3, 700, 130, 512)])
+def test_project_scale_of_any_layout(T, B, N, K):
+    """Scales that are a transposed tensor, or every other column of one, against contiguous ones,
+    at outputs of a scale's own size among others."""
+    import torch
+    lda = _lda()
+    g = torch.Generator(device="cuda").manual_seed(T)
+    q = torch.randint(-128, 128, (T, B, K), dtype=torch.int8, device="cuda", generator=g)
+    w = torch.randint(-128, 128, (N, K), dtype=torch.int8, device="cuda", generator=g)
+    ws = torch.rand(N, device="cuda", generator=g)
+    scale = torch.rand(T, B, device="cuda", generator=g)
+    want = lda.project_int8(q, scale, w, ws, dtype=torch.float32)
+    wide = torch.stack([scale, -scale], 2).view(T, 2 * B)
+    for view in (scale.t().contiguous().t(), wide[:, ::2]):
+        assert not view.is_contiguous() or 1 in (T, B)
+        for _ in range(20):
+            assert torch.equal(lda.project_int8(q, view, w, ws, dtype=torch.float32), want)
+        out = torch.empty_like(want)
+        assert torch.equal(lda.project_int8(q, view, w, ws, out=out), want)
