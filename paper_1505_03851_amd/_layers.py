@@ -82,6 +82,15 @@ def _weight(t, dtype, D: int, dev: int) -> tuple[int, int]:
     return _vector(t, "weight", dtype if own else _F32, D, dev), DTYPES[dtype] if own else 0
 
 
+def _scales(t, shape, n: int, dev: int) -> int:
+    """The address of the rows' scales, ``out[1]``, to overwrite."""
+    if not isinstance(t, _Tensor) or t.shape != shape:
+        raise ValueError(f"out[1] must be a tensor of the shape {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError("out[1] must be contiguous")
+    return _vector(t.view(-1), "out[1]", _F32, n, dev)
+
+
 def _norm(x, weight, eps, residual, out, sum_out, bits8):
     if _recording() and (x.requires_grad or (isinstance(weight, _Tensor) and weight.requires_grad)
                          or (isinstance(residual, _Tensor) and residual.requires_grad)):
@@ -101,9 +110,7 @@ def _norm(x, weight, eps, residual, out, sum_out, bits8):
         else:
             q, scale = out
             to = _like(q, "out[0]", x, dev, _I8, (N, D), True)
-            if not isinstance(scale, _Tensor) or scale.shape != x.shape[:-1]:
-                raise ValueError(f"out[1] must be a tensor of the shape {tuple(x.shape[:-1])}")
-            steps = _vector(scale.view(-1), "out[1]", _F32, N, dev)
+            steps = _scales(scale, x.shape[:-1], N, dev)
             written += out
         result = (q, scale)
     else:
@@ -237,9 +244,7 @@ def quantise_rows(x, out=None) -> tuple[torch.Tensor, torch.Tensor]:
     else:
         q, scale = out
         to = _like(q, "out[0]", x, dev, _I8, (N, D), True)
-        if not isinstance(scale, _Tensor) or scale.shape != x.shape[:-1]:
-            raise ValueError(f"out[1] must be a tensor of the shape {tuple(x.shape[:-1])}")
-        steps = _vector(scale.view(-1), "out[1]", _F32, N, dev)
+        steps = _scales(scale, x.shape[:-1], N, dev)
         if scale.requires_grad:
             _cut_off("out")
     _run("lda_quantise_rows", dev, a.data_ptr(), ld, *to, steps, N, D, DTYPES[x.dtype])

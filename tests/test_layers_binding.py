@@ -49,3 +49,20 @@ def test_project_scale_lives_until_the_launch(monkeypatch, given):
     out = torch.empty(500, 6, 5) if given else None
     y = _layers.project_int8.__wrapped__(q, scale, w, ws, dtype=torch.float32, out=out)
     assert launched == ["lda_project_int8"] and y.shape == (500, 6, 5)
+
+
+def test_scales_to_overwrite_that_are_not_contiguous(calls):
+    """Refused as other vectors are, in the binding's words, before anything is launched."""
+    import torch
+
+    from paper_1505_03851_amd import _layers
+    x, w = torch.zeros(4, 6, 8), torch.ones(8)
+    q, scale = torch.zeros(4, 6, 8, dtype=torch.int8), torch.zeros(6, 4).t()
+    for call in (lambda: _layers.quantise_rows.__wrapped__(x, out=(q, scale)),
+                 lambda: _layers.add_norm_int8.__wrapped__(x, w, out=(q, scale))):
+        with pytest.raises(ValueError, match="contiguous"):
+            call()
+    assert not calls
+    _layers.quantise_rows.__wrapped__(x, out=(q, torch.zeros(4, 6)))
+    _layers.add_norm_int8.__wrapped__(x, w, out=(q, torch.zeros(4, 6)))
+    assert [name for name, _ in calls] == ["lda_quantise_rows", "lda_add_norm"]
