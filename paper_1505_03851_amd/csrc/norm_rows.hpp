@@ -414,8 +414,11 @@ __global__ __launch_bounds__(WAVES <= 4 ? kNormThreads : 64 * WAVES) void norm_g
     for (int u = 0; u < kUnits; ++u)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        d[u][j] = there && j >= c[u].skip ? T::up(now.d[u].v[j]) : 0.0f;
-        h[u][j] = j >= c[u].skip ? T::up(now.h[u].v[j]) : 0.0f;
+        // (h too where there is no row: what was loaded in its place, the last row again, another
+        // wavefront may just be writing over with an infinite dx)
+        const bool own = there && j >= c[u].skip;
+        d[u][j] = own ? T::up(now.d[u].v[j]) : 0.0f;
+        h[u][j] = own ? T::up(now.h[u].v[j]) : 0.0f;
         square = __builtin_fmaf(h[u][j], h[u][j], square);
         along = __builtin_fmaf(d[u][j] * w[u][j], h[u][j], along);
       }

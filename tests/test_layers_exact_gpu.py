@@ -48,6 +48,68 @@ def test_norm_bits_at_halves(dtype, D):
     assert bool((got[0].abs().amax(1) == 127).all())
 
 
+# ---- the norm's gradient, in place
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,D", [(1, 7), (3, 64), (5, 300), (33, 512), (2050, 1000), (31, 1024), (9, 1500),
+                                 (4099, 2048), (7, 4096), (66, 5003), (9, 16_000), (5, 17_003)])
+def test_norm_grad_over_its_inputs(dtype, N, D):
+    """dx over the gradient, over h and over the residual's gradient: the bits of dx elsewhere."""
+    lda = _lda()
+    h, r, w = _norm_inputs(N, D, dtype, "float32")
+    dy = _norm_inputs(N + 1, D, dtype, "float32")[0][:N]
+    weight = _gpu(w, "float32")
+    for residual in (True, False):
+        def inputs():
+            return _gpu(dy, dtype), _gpu(h, dtype), _gpu(r, dtype) if residual else None
+        a, b, c = inputs()
+        dx, dw = lda.norm_grad(a, b, weight, residual_grad=c)
+        for i in range(3 if residual else 2):
+            args = inputs()
+            got = lda.norm_grad(args[0], args[1], weight, residual_grad=args[2], out=args[i])
+            assert got[0] is args[i]
+            _same(got[0], dx)
+            _same(got[1], dw)
+
+
+def _same(a, b):
+    import torch
+    assert torch.equal(torch.nan_to_num(a, 5.0, 6.0, 7.0), torch.nan_to_num(b, 5.0, 6.0, 7.0))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("bad", [float("inf"), float("nan"), "overflow"])
+@pytest.mark.parametrize("N,D", [(1, 40), (5, 300), (6, 1024), (4097, 520), (3, 1400), (1027, 2000)])
+def test_norm_grad_over_h_of_an_infinite_last_row(dtype, bad, N, D):
+    """The last row's dx is infinite or NaN, by the residual's gradient or by its type's range, and
+    written over h while other wavefronts, whose rows are past the last, load that row in place of
+    theirs: the weight's gradient, which is finite, has no part in it."""
+    import torch
+    lda = _lda()
+    h, r, w = _norm_inputs(N, D, dtype, "float32")
+    dy = _norm_inputs(N + 1, D, dtype, "float32")[0][:N]
+    weight = _gpu(w, "float32")
+    largest = float(torch.finfo(_gpu(dy, dtype).dtype).max)
+
+    def inputs():
+        grad, rows, rest = _gpu(dy, dtype), _gpu(h, dtype), _gpu(r, dtype)
+        rest[-1] = largest if bad == "overflow" else bad
+        if bad == "overflow":  # s (grad weight - ...) of the largest's size on top of it
+            grad[-1] = largest / 4 * torch.sign(weight)
+            rows[-1] *= 2.0 ** -6
+        return grad, rows, rest
+    a, b, c = inputs()
+    dx, dw = lda.norm_grad(a, b, weight, residual_grad=c)
+    assert bad == "overflow" or bool(torch.isfinite(dw).all())
+    assert not torch.isfinite(dx[-1]).all()
+    for _ in range(10):
+        grad, rows, rest = inputs()
+        got = lda.norm_grad(grad, rows, weight, residual_grad=rest, out=rows)
+        _same(got[0], dx)
+        _same(got[1], dw)
+
+
 # ---- the product: a scale of any layout
 
 
