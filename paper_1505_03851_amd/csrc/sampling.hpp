@@ -707,12 +707,14 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       f(j, x);
     }
   };
-  // What min_p cuts off, by logits: up to `bar` all, from `pass` on nothing.  (The weight
-  // itself decides between, a 1e-9 of its logarithm.)
+  // What min_p cuts off, by logits: up to `bar` all, from `pass` on nothing.  The weight itself
+  // decides between: 1e-9 of its logarithm, and two roundings of a logit as large as the top, which
+  // are more of the logarithm where logits lie far from 0 and close together.
   float bar = least, pass = least;
   if (s.floor > 0.0) {
-    const double at = log2(s.floor) - (double)digits, up = (double)top + (at + 1e-9) / per;
-    bar = below((double)top + (at - 1e-9) / per);
+    const double at = log2(s.floor) - (double)digits, off = 0x1p-51 * fabs((double)top);
+    const double up = (double)top + (at + 1e-9) / per + off;
+    bar = below((double)top + (at - 1e-9) / per - off);
     pass = (float)up;
     pass = uniform((double)pass < up ? nextafterf(pass, infinity) : pass);
     pass = pass < top ? pass : top;

@@ -3,7 +3,7 @@ equal, bit for bit, what another way to the same numbers gives."""
 import numpy as np
 import pytest
 
-from test_layers_gpu import SIZES, _norm_inputs
+from test_layers_gpu import SIZES, _check, _norm_inputs
 from test_tokens_gpu import TYPES, _gpu, _lda
 
 pytestmark = pytest.mark.gpu
@@ -133,3 +133,41 @@ def test_project_scale_of_any_layout(T, B, N, K):
             assert torch.equal(lda.project_int8(q, view, w, ws, dtype=torch.float32), want)
         out = torch.empty_like(want)
         assert torch.equal(lda.project_int8(q, view, w, ws, out=out), want)
+
+
+# ---- sampling: what min_p cuts off
+
+
+def _floors_next_to_a_weight(n):
+    """(largest logits, next floats below, temperatures, floors): a weight of 2^-1 to 2^-6 and a float
+    within 1e-10 to 4e-9 of it, above or below.  A logit is a float, 2^-25 to 2^-23 of the largest
+    below it, so the logarithm of a weight, taken from the logit in double, is off by up to 6 2^-28
+    of itself: less than that is next to nothing, and 1e-9 is not."""
+    g = np.random.default_rng(3)
+    tops = g.choice(np.float32([1e6, 3e5, -7e6, 1234567.0, 1e20, -2.5, 64.0]), 400_000)
+    nexts = np.nextafter(tops, np.float32(-np.inf))
+    apart = tops.astype(float) - nexts.astype(float)
+    t = (apart / (g.uniform(1, 6, len(tops)) * np.log(2))).astype(np.float32)
+    w = np.exp(-apart / t.astype(float))
+    m = w.astype(np.float32)
+    off = np.abs(m.astype(float) - w)
+    take = np.nonzero((off > 1e-10) & (off < 4e-9))[0][:n]
+    assert len(take) == n
+    return tops[take], nexts[take], t[take], m[take]
+
+
+@pytest.mark.parametrize("V", [700, 1500, 3000])
+@pytest.mark.parametrize("share", [None, 0.97, 0.999999])
+def test_sample_floors_next_to_a_weight(V, share):
+    """Half of the floors are next above a weight, which goes, the others next below, which stays:
+    among few tokens and many, alone and before the place where top_p ends."""
+    B = 1200
+    top, following, t, m = _floors_next_to_a_weight(B)
+    g = np.random.default_rng(V)
+    x = np.repeat(following[:, None], V, 1)
+    for _ in range(2):  # the others one to three floats further down, with weights of their own
+        x = np.where(g.random((B, V)) < 0.6, np.nextafter(x, np.float32(-np.inf)), x)
+    x = np.where(g.random((B, V)) < 0.5, np.float32(-np.inf), x)
+    x[:, V // 3], x[:, V // 2], x[:, 2 * V // 3] = top, following, following
+    p = None if share is None else np.full(B, share, dtype=np.float32)
+    _check(x.astype(float), g.random(B).astype(np.float32), t, None, p, m, what=(V, share))
