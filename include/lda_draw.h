@@ -702,8 +702,8 @@ int lda_project_int8(const int8_t *q, int64_t ld_q, const float *scale, const in
  * z = -1 and prob = 0.
  * Weights are computed in fp64 and held as whole multiples of 2^-F of the
  * largest, F = 46 up to V = 131,072 and 63 - ceil(log2 V) above: their sums are exact, so
- * a row's token does not depend on its place, nor on how the work is split.  A
- * weight that rounds to 0 is never chosen.
+ * a row's token does not depend on its place, nor on how the work is split.  min_p
+ * is asked of a weight before it is rounded so.  A weight that rounds to 0 is never chosen.
  * Rules on the logits (lda_penalise_logits) come before; B up to LDA_LOGITS_MAX_ROWS.
  */
 int lda_sample_logits(const void *logits, int64_t ld_logits, int64_t B, int32_t V, int32_t dtype,

@@ -393,7 +393,7 @@ __device__ __forceinline__ uint64_t point_of(uint64_t all, float u) {
 struct SampleSettings {
   uint64_t k;  // 0: none
   float p, u;
-  double floor;  // in steps
+  double floor;  // min_p in steps: of weights as they are, before they are rounded to whole ones
 };
 
 // Of up to 256 listed tokens: each compared with all others.  The lanes of a list's width
@@ -449,8 +449,12 @@ template <typename T>
 __device__ void choose_compared(SampleShared &sh, int n, const Weights &weights,
                                 const SampleSettings &s, int32_t *z, float *prob) {
   const int t = (int)threadIdx.x;
-  const Compared c = compared<T>(
-      sh, n, [&](float x) { return Weights::steps(weights.of(x, x > weights.least)); });
+  bool heavy = false;  // at least min_p, which is asked of a weight before it is rounded
+  const Compared c = compared<T>(sh, n, [&](float x) {
+    const double w = weights.of(x, x > weights.least);
+    heavy = w >= s.floor;
+    return Weights::steps(w);
+  });
   uint64_t weight = c.amount;
   if (c.part == 0) {
     weight = s.k == 0 || c.rank < s.k ? weight : 0;
@@ -460,7 +464,7 @@ __device__ void choose_compared(SampleShared &sh, int n, const Weights &weights,
   __syncthreads();
   if (c.part == 0) {
     const bool stays = !(s.p < 1.0f) || c.before < share_of(sh.total, s.p);
-    weight = stays && (double)weight >= s.floor ? weight : 0;
+    weight = stays && heavy ? weight : 0;
     sh.list.weight[c.i] = weight;
   }
   __syncthreads();

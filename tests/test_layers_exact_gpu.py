@@ -171,3 +171,37 @@ def test_sample_floors_next_to_a_weight(V, share):
     x[:, V // 3], x[:, V // 2], x[:, 2 * V // 3] = top, following, following
     p = None if share is None else np.full(B, share, dtype=np.float32)
     _check(x.astype(float), g.random(B).astype(np.float32), t, None, p, m, what=(V, share))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_sample_floors_between_two_steps(dtype):
+    """min_p is asked of a weight as it is, not of the whole multiple of 2^-46 that it is held as,
+    whatever the row's length and so its way: a u of 1 takes the last token that stays.  Weights of
+    10.6 and 10.4 steps (to 2^-20 of them in float) against floors on both sides of them."""
+    import torch
+    lda = _lda()
+    x, m, want = [], [], []
+    for steps, floor in ((10.6, 10.75), (10.6, 10.55), (10.4, 10.3), (10.4, 10.45), (0.75, 0.8),
+                         (0.75, 0.7), (5.5, 5.5 - 2.0 ** -16), (5.5, 5.5 + 2.0 ** -16)):
+        x.append(np.log(steps * 2.0 ** -46))
+        m.append(floor * 2.0 ** -46)
+        want.append(steps >= floor)
+    if dtype == "bfloat16":  # (whole logits: weights of 17.9 and 6.58 steps)
+        x = [-29.0, -29.0, -30.0, -30.0]
+        w = np.exp(x)
+        m = [w[0] * (1 + 2e-3), w[0] * (1 - 2e-3), w[2] * (1 + 2e-3), w[2] * (1 - 2e-3)]
+        want = [False, True, False, True]
+    B = len(x)
+    for V in (3, 60, 200, 256, 257, 900, 1024, 1025, 3000, 20_000):
+        rows = torch.full((B, V), -float("inf"), device="cuda")
+        rows[:, 0] = 0.0
+        rows[:, V // 2] = -1.0
+        rows[:, V - 1] = torch.tensor(x, device="cuda")
+        floor = torch.tensor(m, dtype=torch.float32, device="cuda")
+        for k, p in ((None, None), (3, None), (700, None), (None, 1 - 2.0 ** -24), (3, 1 - 2.0 ** -24)):
+            z, _ = lda.sample_logits(
+                rows.to(getattr(torch, dtype)), torch.ones(B, device="cuda"), min_p=floor,
+                top_k=None if k is None else torch.full((B,), k, dtype=torch.int32, device="cuda"),
+                top_p=None if p is None else torch.full((B,), p, device="cuda"))
+            last = [V - 1 if stays and p is None else V // 2 for stays in want]
+            assert z.tolist() == last, (V, k, p)
