@@ -93,8 +93,9 @@ struct Weights {
   // ten Chebyshev points (off by 2^-50.6 of itself at most), its exponent raised by n + F.
   // Where not `there` (which x must be above `least` for) a number that rounds to 0.
   __device__ __forceinline__ double of(float x, bool there) const {
-    const double y = ((double)x - top) * per;
-    const double m = y + shift, f = y - (m - shift);
+    // (y's product fused by name: a token has the same weight, to the last bit, wherever this is
+    // inlined, or sums of bins and of rows would not be the same)
+    const double d = (double)x - top, m = fma(d, per, shift), f = fma(d, per, -(m - shift));
     double p = fma_by(7.070977866508138e-09, f, 1.0205905413765595e-07);
     p = fma_by(p, f, 1.3215451633221434e-06);
     p = fma_by(p, f, 1.5252672924850737e-05);

@@ -205,3 +205,33 @@ def test_sample_floors_between_two_steps(dtype):
                 top_p=None if p is None else torch.full((B,), p, device="cuda"))
             last = [V - 1 if stays and p is None else V // 2 for stays in want]
             assert z.tolist() == last, (V, k, p)
+
+
+# ---- sampling: a row is the same wherever its tokens are
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sample_of_a_row_among_others(dtype):
+    """200 logits alone, with nothing after them and between them, so that they are compared,
+    sorted, cut by bins and found in other stretches: the same token and the same bits of its
+    probability."""
+    import torch
+    lda = _lda()
+    B, n = 400, 200
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = (torch.randn(B, n, device="cuda", generator=g) * 3).to(getattr(torch, dtype))
+
+    def draw(low, high):
+        return torch.rand(B, device="cuda", generator=g) * (high - low) + low
+    u, t, p, m = draw(0, 1), draw(0.2, 3), draw(0.3, 1.1), 10 ** draw(-6, -0.3)
+    k = torch.randint(0, n, (B,), dtype=torch.int32, device="cuda", generator=g)
+    for rules in ({}, dict(top_p=p), dict(min_p=m), dict(top_k=k, top_p=p, min_p=m),
+                  dict(top_p=p, min_p=m)):
+        want = lda.sample_logits(x, u, temperature=t, **rules)
+        for V, apart in ((257, 1), (1000, 1), (1000, 5), (2000, 1), (2000, 10), (40_000, 200),
+                         (131_072, 600), (70_000, 3)):
+            wide = torch.full((B, V), -float("inf"), dtype=x.dtype, device="cuda")
+            first = (V - n * apart) // 2
+            wide[:, first:first + n * apart:apart] = x
+            z, prob = lda.sample_logits(wide, u, temperature=t, **rules)
+            assert torch.equal((z - first) // apart, want[0]) and torch.equal(prob, want[1]), (V, rules)
