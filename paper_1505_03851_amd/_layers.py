@@ -334,6 +334,8 @@ def sample_logits(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
     else:
         z, prob = out
         to = _vector(z, "out[0]", _I32, B, dev), _vector(prob, "out[1]", _F32, B, dev)
+        if prob.requires_grad:
+            _cut_off("out")
     _run("lda_sample_logits", dev, logits.data_ptr(), ld, B, V, DTYPES[logits.dtype], numbers, heat,
          k, p, floor, *to)
     if given:

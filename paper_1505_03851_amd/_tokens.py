@@ -391,6 +391,8 @@ def draw_logits(logits, seed, position, temperature=None, min_p=None, history=No
     else:
         z, prob = out
         to = _vector(z, "out[0]", _I32, B, dev), _vector(prob, "out[1]", _F32, B, dev)
+        if prob.requires_grad:
+            _cut_off("out")
     need = draw_logits_workspace_bytes(B, V)
     if workspace is not None:
         _require(workspace, "workspace", _U8, 1)

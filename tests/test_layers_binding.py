@@ -66,3 +66,26 @@ def test_scales_to_overwrite_that_are_not_contiguous(calls):
     _layers.quantise_rows.__wrapped__(x, out=(q, torch.zeros(4, 6)))
     _layers.add_norm_int8.__wrapped__(x, w, out=(q, torch.zeros(4, 6)))
     assert [name for name, _ in calls] == ["lda_quantise_rows", "lda_add_norm"]
+
+
+def test_draws_over_tensors_that_require_a_gradient(calls, monkeypatch):
+    """Refused where gradients are recorded, as every other tensor to overwrite is."""
+    import torch
+
+    from paper_1505_03851_amd import _layers, _tokens
+    monkeypatch.setattr(_tokens, "_run", lambda name, dev, *args: calls.append((name, args)))
+    monkeypatch.setattr(_tokens, "draw_logits_workspace_bytes", lambda B, V: 0)
+    x, u = torch.zeros(3, 50), torch.zeros(3)
+    z, prob = torch.zeros(3, dtype=torch.int32), torch.zeros(3, requires_grad=True)
+    seed = torch.zeros(3, dtype=torch.int64)
+    for call in (lambda p: _layers.sample_logits.__wrapped__(x, u, out=(z, p)),
+                 lambda p: _tokens.draw_logits.__wrapped__(x, seed, z, out=(z, p))):
+        with pytest.raises(ValueError, match="gradient"):
+            call(prob)
+        assert not calls and prob._version == 0
+        with torch.no_grad():
+            call(prob)
+        call(prob.detach().clone())
+        assert len(calls) == 2
+        calls.clear()
+        prob = torch.zeros(3, requires_grad=True)
