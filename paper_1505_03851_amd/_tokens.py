@@ -8,8 +8,9 @@ call allocates belong to the stream it runs on.  A tensor that a call is given t
 write into counts as changed in place: a backward pass that saved what it held
 raises.  No call records a gradient: where gradients are recorded, one whose
 result would have one (embed, embed_grad, dropout, penalise_logits) refuses
-tensors that require it.  ``embed_grad`` and ``dropout`` are the backward passes,
-for a torch.autograd.Function or a training loop to call.
+tensors that require it, and, recorded or not, forward-mode dual tensors.
+``embed_grad`` and ``dropout`` are the backward passes, for a
+torch.autograd.Function or a training loop to call.
 """
 from __future__ import annotations
 
@@ -17,6 +18,7 @@ import ctypes
 import functools
 
 import torch
+from torch.autograd import forward_ad as _forward
 
 from . import _lib
 from ._lib import _require
@@ -66,6 +68,21 @@ def bind(lib: ctypes.CDLL) -> None:
 # on the host as on the GPU.  What fails goes on to the checks that say why.
 
 
+_DRAWN = ("draw_logits", "sample_logits")  # whose results have no gradient
+
+
+def _no_tangents(fn, args, kw) -> None:
+    """Refuses forward-mode dual tensors, whose tangents the result would not have."""
+    names = fn.__code__.co_varnames
+    for name, value in (*zip(names, args), *kw.items()):
+        if fn.__name__ in _DRAWN and name != "out":
+            continue
+        for t in value if isinstance(value, (tuple, list)) else (value,):
+            if isinstance(t, _Tensor) and _forward.unpack_dual(t).tangent is not None:
+                raise ValueError(f"{name} has a tangent, which is not recorded here: call this with "
+                                 "the tensor that unpack_dual gives")
+
+
 def _entry(fn):
     """``fn`` in the context of its first tensor's device, and of the stream the
     call is given: what it allocates and launches belongs to that stream."""
@@ -73,6 +90,8 @@ def _entry(fn):
 
     @functools.wraps(fn)
     def call(*args, stream=None, **kw):
+        if _forward._current_level >= 0:
+            _no_tangents(fn, args, kw)
         first = args[0] if args else kw.get(name)
         if type(first) is _Tensor and stream is None:
             dev = first.get_device()

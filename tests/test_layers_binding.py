@@ -89,3 +89,34 @@ def test_draws_over_tensors_that_require_a_gradient(calls, monkeypatch):
         assert len(calls) == 2
         calls.clear()
         prob = torch.zeros(3, requires_grad=True)
+
+
+def test_forward_mode_tangents_are_refused(calls, monkeypatch):
+    """A dual tensor does not require a gradient, and its tangent would be lost without a word."""
+    import torch
+    import torch.autograd.forward_ad as forward
+
+    import paper_1505_03851_amd as lda
+    from paper_1505_03851_amd import _layers, _tokens
+    x, v, h = torch.zeros(2, 8), torch.ones(8), torch.zeros(2, 8)
+    q, s, ids = torch.zeros(2, 8, dtype=torch.int8), torch.ones(2), torch.zeros(2, dtype=torch.int32)
+    with forward.dual_level():
+        def dual(t):
+            return forward.make_dual(t, torch.ones_like(t))
+        for call in (
+                lambda: lda.add_norm(dual(x), v), lambda: lda.add_norm(x, dual(v)),
+                lambda: lda.add_norm(x=dual(x), weight=v), lambda: lda.add_norm(x, v, residual=dual(h)),
+                lambda: lda.add_norm(x, v, out=dual(h)), lambda: lda.add_norm_int8(dual(x), v),
+                lambda: lda.add_norm_int8(x, v, out=(q, dual(s))),
+                lambda: lda.norm_grad(x, dual(h), v), lambda: lda.quantise_rows(dual(x)),
+                lambda: lda.project_int8(q, dual(s), q, s), lambda: lda.embed(dual(x), ids),
+                lambda: lda.embed_grad(dual(x), ids, 5), lambda: lda.dropout(dual(x), 0.5, 1),
+                lambda: lda.penalise_logits(dual(x)), lambda: lda.penalise_logits(x, bias=dual(v)),
+                lambda: lda.sample_logits(x, s, out=(ids, dual(s)))):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+        # what has none goes on to the next check, and so does what a token is drawn from
+        for call in (lambda: lda.add_norm(x, v), lambda: lda.sample_logits(dual(x), s),
+                     lambda: lda.draw_logits(dual(x), ids.long(), ids)):
+            with pytest.raises(ValueError, match="on the GPU"):
+                call()
