@@ -673,7 +673,8 @@ int lda_quantise_rows(const void *x, int64_t ld_x, int8_t *q, int64_t ld_q, floa
  * q int8 [M][K], weight int8 [N][K] (a channel's weights contiguous); scale [M],
  * weight_scale [N] and bias [N] (NULL: none) fp32; out [M][N] of element type `dtype`.
  * All int8 numbers are taken, -128 too.  The sum is exact; it is rounded to fp32, multiplied
- * by the two scales in this order, the bias added, and rounded to the output's type.  K up to
+ * by scale, then by weight_scale with the bias added before that product is rounded, and rounded
+ * to the output's type: a row gives the same bits alone and among others.  K up to
  * LDA_PROJECT_MAX_K (LDA_ERR_UNSUPPORTED above: the sum would pass 32 bits); M up
  * to LDA_MAX_N.  A row with a NaN for a scale gives NaN.
  */

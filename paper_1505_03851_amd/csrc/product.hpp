@@ -40,6 +40,12 @@ struct ProductArgs {
   int32_t N, K;
 };
 
+// What a sum becomes: the second product and the bias (0: none) rounded together, by name, so
+// that a row is the same alone and among others, whichever kernel takes it.
+__device__ __forceinline__ float scaled(float sum, float scale, float weight_scale, float bias) {
+  return __builtin_fmaf(sum * scale, weight_scale, bias);
+}
+
 // The 16 bytes of a line of K >= 16 from byte `at` on, zero from its end on, in two steps:
 // where the line ends among them those that end with it are loaded, and moved down later.
 // So loads have no branch that others would wait in.
@@ -125,9 +131,9 @@ __global__ __launch_bounds__(256) void direct_product_kernel(ProductArgs<T> a, u
     for (int i = (int)threadIdx.x; i < kTile * kTile; i += (int)blockDim.x) {
       const int64_t m = m0 + i / kTile, n = n0 + i % kTile;
       if (m >= a.M || n >= a.N) continue;
-      float v = (float)joined[i / kTile * kPitch + i % kTile] * a.scale[m] * a.weight_scale[n];
-      if (a.bias) v += a.bias[n];
-      a.out[m * a.ldo + n] = T::down(v);
+      const float sum_mn = (float)joined[i / kTile * kPitch + i % kTile];
+      a.out[m * a.ldo + n] =
+          T::down(scaled(sum_mn, a.scale[m], a.weight_scale[n], a.bias ? a.bias[n] : 0.0f));
     }
     __syncthreads();  // read before the next tile clears it
   }
@@ -359,7 +365,8 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tiled_product_kernel(Pr
         for (int j = 0; j < NT; ++j) {
           Packed<T, 4> v;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) v.v[r] = T::down((float)sum[i][j][r] * s * ws[j][r] + b[j][r]);
+          for (int r = 0; r < 4; ++r)
+            v.v[r] = T::down(scaled((float)sum[i][j][r], s, ws[j][r], b[j][r]));
           *reinterpret_cast<Packed<T, 4> *>(room + (16 * i - r0 + line) * kPitch +
                                             (16 * j + 4 * part) * (int)sizeof(S)) = v;
         }

@@ -135,6 +135,31 @@ def test_project_scale_of_any_layout(T, B, N, K):
         assert torch.equal(lda.project_int8(q, view, w, ws, out=out), want)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,K", [(7, 10), (50, 64), (1000, 130), (4096, 512), (300, 1024), (900, 2000),
+                                 (5000, 2048), (17_000, 256)])
+def test_project_row_alone_and_among_others(dtype, N, K):
+    """Bit for bit, by the kernel for a few rows and by those of every tile, aligned or not."""
+    import torch
+    lda = _lda()
+    g = torch.Generator(device="cuda").manual_seed(N)
+    M = 2100
+    q = torch.randint(-128, 128, (M, K), dtype=torch.int8, device="cuda", generator=g)
+    w = torch.randint(-128, 128, (N, K), dtype=torch.int8, device="cuda", generator=g)
+    s = torch.rand(M, device="cuda", generator=g) / 100
+    ws = torch.rand(N, device="cuda", generator=g) / 100
+    bias = torch.randn(N, device="cuda", generator=g)
+    odd = torch.zeros(M, K + 1, dtype=torch.int8, device="cuda")[:, 1:]  # lines at any byte
+    odd.copy_(q)
+    for b in (bias, None):
+        def product(rows, n):
+            return lda.project_int8(rows[:n], s[:n], w, ws, bias=b, dtype=getattr(torch, dtype))
+        want = product(q, M)
+        for n in (1, 5, 16, 17, 40, 64, 100, 300, 700):
+            assert torch.equal(product(q, n), want[:n]), n
+            assert torch.equal(product(odd, n), want[:n]), n
+
+
 # ---- sampling: what min_p cuts off
 
 
