@@ -47,12 +47,12 @@ constexpr int64_t kLongBlocks = 512;
     }                       \
   } while (0)
 
-// Rows of 16 bits pass the caches by where a call reads and writes more than they hold:
-// 16,384 x 4,096 bfloat16 with a residual (537 MB) 88 us against 94, its gradient 111 against
-// 119, 32,768 x 2,048 without one (403 MB) 86 against 96; below, what the launch before wrote
-// may still be there: 16,384 x 4,096 without a residual (268 MB) 44 against 39, 8,192 x 4,096
-// with one (268 MB) 45 against 39.  A lane's 32 bytes of floats are two accesses to one line:
-// 204 against 192.
+// Rows of 16 bits pass the caches by where a call reads and writes more than they hold (times
+// of a call among others): 16,384 x 4,096 bfloat16 with a residual (537 MB) 87.6 us against 94,
+// its gradient 109 against 118, without one (403 MB) 84 against 88; below, what the launch before
+// wrote may still be there: the norm of 16,384 x 4,096 without a residual (268 MB) 46 against 39,
+// of 8,192 x 4,096 with one (268 MB) 45 against 40.  A lane's 32 bytes of floats are two accesses
+// to one line: 16,384 x 4,096 with a residual 202 against 189, its gradient 209 against 207.
 template <typename T>
 bool past_caches(int64_t rows, int64_t columns, int arrays) {
   const int64_t size = (int64_t)sizeof(typename T::store);

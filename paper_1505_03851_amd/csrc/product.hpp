@@ -152,10 +152,10 @@ __global__ __launch_bounds__(256) void direct_product_kernel(ProductArgs<T> a, u
 // multiple of 16, pass through registers.
 //
 // Workgroups start at different stages: lines often lie a power of two apart, so that the
-// same stage of all of them is in a few of the memory's channels (64 x 100,000 x 4,096 112 us
-// where all start at the first, 256 x 8,192 37 against 24).  Tiles of 128 and more, which
-// share lines through their XCD's L2, start alike within an XCD (8,192 x 8,192 x 4,096 238 us;
-// each elsewhere 255, all alike 244).
+// same stage of all of them is in a few of the memory's channels (64 x 100,000 x 4,096 110 us
+// where all start at the first, 92 here, 256 x 8,192 36 against 21).  Tiles of 128 and more, which
+// share lines through their XCD's L2, start alike within an XCD (8,192 x 8,192 x 4,096 on the
+// same operands again and again 236 us; each elsewhere 256, all alike 238).
 //
 // A workgroup takes tile after tile, the next one's first stage on its way while this
 // one's sums go out: by rows through LDS, whole lines of memory at a time.

@@ -756,7 +756,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(
       stay = Stay{uniform(Keys<T>::logit((uint32_t)(end >> 32))), (uint32_t)end + 1};
       known = floors && (sums || s.floor == 0.0);
     };
-    // What a small top_k leaves is a list as it is (256 x 100,000 with all settings 60 us, 63 by
+    // What a small top_k leaves is a list as it is (256 x 100,000 with all settings 61 us, 63 by
     // bins here too).
     if (floors && s.k && s.k <= kListed) {
       __syncthreads();  // what was there is read
